@@ -206,6 +206,43 @@ int llmq_bf16_gemm_tn(const void* A_bf16, const void* B_bf16, int64_t R, int64_t
                       void* c_bf16, int accumulate, void* stream);
 
 /*
+ * FP8 with a scale for each block of 128 values along the contraction, for tensors whose rows or columns differ so much in size that one scale a
+ * tensor (llmq_amax) leaves the small ones few bits.
+ *
+ *   A scale is a power of two, kept as one byte: the byte b stands for d = 2^(b-127), the smallest power of two with amax / d <= FMAX of
+ *   the format (448 or 57344), amax the largest magnitude of the block; not below 2^-127 (b = 0), and b = 127 for a block of zeros.
+ *     q = cast( x / d ),  round to nearest even; nothing is clipped and x / d is exact, so q d is x rounded to the format's bits.
+ *   A block that holds an Inf or NaN has b = 255: the contractions that read it give NaN, its codes are unspecified.
+ *
+ *   The bytes of an operand [rows, T] (T the contraction) are kept K step by K step of 128, the rows of a step in groups of 128:
+ *     byte of (row r, step k) at  k * rows128 + 128 (r / 128) + 8 (r % 16) + (r / 16) % 8,   rows128 = rows rounded up to a multiple of 128,
+ *   which is the order the matrix cores' registers take them in.  llmq_block_scales_bytes(rows, T) = rows128 * ceil(T / 128).  Bytes of rows that do
+ *   not exist are written (127, or their block's) and never matter.
+ *
+ * llmq_quantize_fp8_blocks: x [rows, cols] BF16 in one pass, without an absmax pass before it.
+ *   block_rows 1:    q [rows, cols] with a scale for each row and 128 columns, and q_t [cols, rows] (the transposed tensor, for contractions over the rows of
+ *                    x) with a scale for each column and 128 rows; the codes of the two are different ones.
+ *   block_rows 128:  blocks of 128 x 128, whose codes and scales q and q_t share: weights, which are read along both dimensions.
+ *   s and s_t: scale bytes of q as an operand [rows, T = cols] and of q_t as an operand [cols, T = rows].  Every row of a block of 128 x 128 has a copy of its
+ *   byte, so operands of either kind are read alike.  q and s may be NULL together, or q_t and s_t; one pair must be there.
+ *   Other values of block_rows: LLMQ_ERR_FLAGS.  All pointers 16-byte aligned.  Multiples of 128 rows and columns are fastest.
+ *
+ * llmq_fp8_gemm_blocks: c[r,cc] = bf16( sum_t A[r,t] dA[r,t/128] B[cc,t] dB[cc,t/128] )   (+ c[r,cc] first when accumulate != 0, one rounding)
+ *   A [R,T] and B [C,T], rows of T contiguous bytes, any mix of formats; sA, sB their scale bytes.  Products are exact, sums in binary32 on the matrix
+ *   cores.  d_amax_c as in llmq_fp8_gemm_tn.  Error of each element bounded as there, by 2^-7 of the sum of the products' magnitudes.  Fastest with R and C
+ *   multiples of 256 and T a multiple of 128 (16 at least).  T < 16, T or C >= 2^22 and scales of 2 GB take a slow generic kernel, which has R < 2^21 and
+ *   C < 2^28 (LLMQ_ERR_SHAPE otherwise).
+ *   forward         Y = X W^T     A = q of X,      B = q of W
+ *   input gradient  dX = dY W     A = q of dY,     B = q_t of W
+ *   weight gradient dW = dY^T X   A = q_t of dY,   B = q_t of X
+ */
+size_t llmq_block_scales_bytes(int64_t rows, int64_t cols);
+int llmq_quantize_fp8_blocks(const void* x_bf16, int64_t rows, int64_t cols, int fmt, int block_rows,
+                             uint8_t* q, uint8_t* s, uint8_t* q_t, uint8_t* s_t, void* stream);
+int llmq_fp8_gemm_blocks(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* B, const uint8_t* sB, int fmtB,
+                         int64_t R, int64_t C, int64_t T, void* c_bf16, int accumulate, float* d_amax_c, void* stream);
+
+/*
  * Workspace of the three linear-layer calls below, for one (M, N, K).  It holds the FP8 copies
  *   Xq [M,K], Wq [N,K], dYq [M,N], then 12 KB of scratch for the LLMQ_JIT_* flags, then
  *   Xq_t [K,M], Wq_t [K,N], dYq_t [N,M],

@@ -296,11 +296,67 @@ PyObject* rmsnorm_codes(PyObject* const* args, Py_ssize_t n) {
 LLMQ_BINDING(rmsnorm_apply_fp8) { return rmsnorm_codes<false>(args, n); }
 LLMQ_BINDING(rmsnorm_apply_fp8_slabs) { return rmsnorm_codes<true>(args, n); }
 
+// Tensors of the current device only, whose stream the call takes
+struct HereArgs : Args {
+    int device;
+    explicit HereArgs(const Args& args) : Args(args), device(-1) {
+        PyObject* d = PyObject_CallNoArgs(g_get_device);
+        if (d) { device = (int)PyLong_AsLong(d); Py_DECREF(d); }
+        if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }
+    }
+    const at::Tensor* here(int i, at::ScalarType type) {
+        const at::Tensor* t = tensor(i, type);
+        if (t && t->device().index() != device) { ok = false; return nullptr; }
+        return t;
+    }
+    // (numel -1: any; required: not None)
+    void* pointer(int i, at::ScalarType type, int64_t numel, bool required) {
+        if (a[i] == Py_None) { if (required) ok = false; return nullptr; }
+        const at::Tensor* t = here(i, type);
+        if (t && numel >= 0 && t->numel() != numel) { ok = false; return nullptr; }
+        return t ? t->data_ptr() : nullptr;
+    }
+    uint8_t* codes(int i, int64_t numel, bool required) { return static_cast<uint8_t*>(pointer(i, kU8, numel, required)); }
+};
+
+LLMQ_BINDING(quantize_fp8_blocks) {
+    return run(args, n, 7, [](Args& args_) {
+        HereArgs a(args_);
+        int64_t rows = 0, cols = 0;
+        a.dims(0, kBf16, rows, cols);
+        void* x = a.pointer(0, kBf16, -1, true);
+        const int fmt = a.i32(1), block_rows = a.i32(2);
+        uint8_t *q = a.codes(3, rows * cols, false), *s = a.codes(4, (int64_t)llmq_block_scales_bytes(rows, cols), false);
+        uint8_t *qt = a.codes(5, rows * cols, false), *st = a.codes(6, (int64_t)llmq_block_scales_bytes(cols, rows), false);
+        args_.ok = a.ok;
+        return [=](void* stream) { return llmq_quantize_fp8_blocks(x, rows, cols, fmt, block_rows, q, s, qt, st, stream); };
+    });
+}
+
+LLMQ_BINDING(fp8_gemm_blocks) {
+    return run(args, n, 9, [](Args& args_) {
+        HereArgs a(args_);
+        int64_t R = 0, T = 0, C = 0, T2 = 0, R2 = 0, C2 = 0;
+        a.dims(0, kU8, R, T);
+        a.dims(3, kU8, C, T2);
+        a.dims(6, kBf16, R2, C2);
+        if (T != T2 || R2 != R || C2 != C) a.ok = false;
+        uint8_t *A = a.codes(0, -1, true), *sA = a.codes(1, (int64_t)llmq_block_scales_bytes(R, T), true);
+        const int fmt_a = a.i32(2), fmt_b = a.i32(5);
+        uint8_t *B = a.codes(3, -1, true), *sB = a.codes(4, (int64_t)llmq_block_scales_bytes(C, T), true);
+        void* c = a.pointer(6, kBf16, -1, true);
+        const int accumulate = a.truth(7);
+        float* amax = static_cast<float*>(a.pointer(8, kF32, 1, false));
+        args_.ok = a.ok;
+        return [=](void* stream) { return llmq_fp8_gemm_blocks(A, sA, fmt_a, B, sB, fmt_b, R, C, T, c, accumulate, amax, stream); };
+    });
+}
+
 #define LLMQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {LLMQ_METHOD(linear_fwd), LLMQ_METHOD(linear_dgrad), LLMQ_METHOD(linear_wgrad), LLMQ_METHOD(amax), LLMQ_METHOD(quantize_fp8),
                            LLMQ_METHOD(quantize_fp8_slabs), LLMQ_METHOD(bf16_gemm_tn), LLMQ_METHOD(swiglu_fwd), LLMQ_METHOD(swiglu_fwd_fp8),
                            LLMQ_METHOD(swiglu_fwd_fp8_slabs), LLMQ_METHOD(swiglu_bwd), LLMQ_METHOD(rmsnorm_fwd), LLMQ_METHOD(rmsnorm_apply_fp8),
-                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), {nullptr, nullptr, 0, nullptr}};
+                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

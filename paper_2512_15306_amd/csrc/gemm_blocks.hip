@@ -1,0 +1,73 @@
+// Choice of kernel and entry point of the contraction with block scales.
+#include "gemm_blocks.h"
+
+#include "api_checks.h"
+
+namespace llmq {
+
+
+
+// The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
+// times by a few percent.  Tiles with sides of 192 and 320 are not built: a wave's rows would not start at a multiple of 64, where a register holds the
+// scales of whole groups of four blocks.
+static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, bool with_amax, int num_cus) {
+    BlocksPlan plan{0, {0, 0, kNoEdge}};
+    const int64_t steps = (T + BK - 1) / BK, rounded = ((R > C ? R : C) + 127) / 128 * 128;
+    // 32-bit offsets from the first row of a tile, of operands, scales and output; sixteen bytes in every row of an operand
+    if (T < 16 || T >= (1ll << 22) || C >= (1ll << 22) || steps * rounded >= 0x7FFFF000ll) return plan;
+    const bool aligned_rows = T % 16 == 0;
+    auto form = [&](int ni, int nj) {
+        const bool whole = R % (64 * ni) == 0 && C % (64 * nj) == 0 && T % BK == 0;
+        return TilePlan{ni, nj, whole ? kNoEdge : aligned_rows ? kEdge : kEdgeUnaligned};
+    };
+    // (256 x 256 tiles whose chunks go through registers would spill accumulators)
+    auto built = [&](const TilePlan& p) { return p.edge != kEdgeUnaligned || p.ni * p.nj < 16; };
+    if (const char* e = tuning_env("LLMQ_GEMM_ANY_TILE")) {
+        if ((e[0] == '2' || e[0] == '4') && e[1] == 'x' && (e[2] == '2' || e[2] == '4')) {
+            plan.tile = form(e[0] - '0', e[2] - '0');
+            if (built(plan.tile)) return plan;
+            plan.tile = {0, 0, kNoEdge};
+        }
+        if (e[0] == '0') return plan;
+    }
+    plan.side = aligned_rows ? takes_mini(R, C, T, false, false, accumulate, with_amax, false, num_cus) : 0;
+    if (plan.side) return plan;
+    const bool ragged = R % 128 != 0 || C % 128 != 0 || T % BK != 0;
+    if (ragged && generic_is_faster(R, C, T, false, false, accumulate, with_amax, false, num_cus)) return plan;
+    if (((R + 127) / 128) * ((C + 127) / 128) <= resident_slots(num_cus, 2, 2) / 2) { plan.tile = form(2, 2); return plan; }
+    double best_us = 0.0;
+    for (int ni = 4; ni >= 2; ni -= 2)
+        for (int nj = 4; nj >= 2; nj -= 2) {
+            const int64_t tiles = ((R + 64 * ni - 1) / (64 * ni)) * ((C + 64 * nj - 1) / (64 * nj));
+            if (tiles > kMaxWorkgroups) continue;
+            const TilePlan p = form(ni, nj);
+            if (!built(p)) continue;
+            const double us = tile_us(p, tiles, steps, accumulate, C % 8 != 0, resident_slots(num_cus, ni, nj));
+            if (plan.tile.ni == 0 || us < best_us) { plan.tile = p; best_us = us; }
+        }
+    return plan;
+}
+
+}  // namespace llmq
+
+extern "C" int llmq_fp8_gemm_blocks(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* B, const uint8_t* sB, int fmtB, int64_t R, int64_t C,
+                                    int64_t T, void* c_bf16, int accumulate, float* d_amax_c, void* stream) {
+    if (!A || !sA || !B || !sB || !c_bf16) return LLMQ_ERR_NULL;
+    if (!dim_ok(R) || !dim_ok(C) || !dim_ok(T)) return LLMQ_ERR_SHAPE;
+    if (R * T >= kMaxElems || C * T >= kMaxElems || R * C >= kMaxElems) return LLMQ_ERR_SHAPE;
+    if (!fmt_ok(fmtA) || !fmt_ok(fmtB)) return LLMQ_ERR_FORMAT;
+    if (!aligned(A, 16) || !aligned(sA, 16) || !aligned(B, 16) || !aligned(sB, 16) || !aligned(c_bf16, 16) || !aligned(d_amax_c, 4)) return LLMQ_ERR_ALIGN;
+    const int cus = num_cus();
+    const llmq::BlocksPlan plan = llmq::plan_blocks(R, C, T, accumulate != 0, d_amax_c != nullptr, cus);
+    // the generic kernel's grid has a workgroup of 32 x 32 outputs for each of its two dimensions
+    if (plan.side == 0 && plan.tile.ni == 0 && (R >= (1ll << 21) || C >= (1ll << 28))) return LLMQ_ERR_SHAPE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    unsigned* amax = reinterpret_cast<unsigned*>(d_amax_c);
+    if (amax) llmq::launch_gemm_amax_reset(amax, s);
+    const llmq::BlocksOperands p{A, sA, B, sB, R, C, T, c_bf16, accumulate != 0, amax};
+    if (fmtA == LLMQ_E4M3 && fmtB == LLMQ_E4M3) llmq::launch_blocks<0, 0>(p, plan, s, cus);
+    else if (fmtA == LLMQ_E5M2 && fmtB == LLMQ_E4M3) llmq::launch_blocks<1, 0>(p, plan, s, cus);
+    else if (fmtA == LLMQ_E4M3 && fmtB == LLMQ_E5M2) llmq::launch_blocks<0, 1>(p, plan, s, cus);
+    else llmq::launch_blocks<1, 1>(p, plan, s, cus);
+    return hipGetLastError() == hipSuccess ? LLMQ_OK : LLMQ_ERR_DEVICE;
+}

@@ -1,0 +1,6 @@
+// The kernels of E5M2 x E4M3 operands with block scales.
+#include "gemm_blocks.h"
+
+namespace llmq {
+template void launch_blocks<1, 0>(const BlocksOperands&, const BlocksPlan&, hipStream_t, int);
+}

@@ -39,6 +39,8 @@
 #pragma once
 #include <stdlib.h>
 
+#include <type_traits>
+
 #include "gemm_choice.h"
 #include "llmq_device.h"
 #include "llmq_kernels.h"
@@ -141,6 +143,8 @@ struct GemmTuning {
     // The fused output absmax with the IEEE 754-2019 maximum (v_maximum3_f32: two elements per instruction, NaN
     // propagates) or, for comparison in the phase stamps only, with maxNum (v_max_f32 per element, NaN dropped).
     static constexpr bool kIeeeMaximum = true;
+    // Operands with a scale for each block of 128 contraction bytes (gemm_blocks.h).
+    static constexpr bool kBlockScales = false;
 };
 
 // For problems of at most one 128 x 128 tile per CU.  Alone on its CU, a workgroup of that size with two stages waits for its
@@ -256,18 +260,38 @@ __device__ inline void mma_block(v4f& c, const v8i& a, const v8i& b) {
     }
 }
 
+// The same with a scale for each row of a and b: a byte b stands for 2^(b - 127).  A lane hands over a register for its row (lane % 16) of each
+// operand, of which the instruction takes byte OA or OB; the 32 contraction bytes a lane holds all lie in one block of 128.
+template <int FA, int FB, bool IN_V, int OA, int OB>
+__device__ inline void mma_block_scaled(v4f& c, const v8i& a, const v8i& b, int sa, int sb) {
+    if constexpr (IN_V) {
+        asm("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0] cbsz:%9 blgp:%10"
+            : "+v"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa), "n"(OB & 1), "n"(OA & 1), "n"(OB >> 1), "n"(OA >> 1), "n"(FB), "n"(FA));
+    } else {
+        asm("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0] cbsz:%9 blgp:%10"
+            : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa), "n"(OB & 1), "n"(OA & 1), "n"(OB >> 1), "n"(OA >> 1), "n"(FB), "n"(FA));
+    }
+}
+
+// Scales of a K step, four block rows or columns of the wave tile to a register; NoScales: operands without.
+struct NoScales {};
+template <int WA, int WB>
+struct BlockScales { int a[WA], b[WB]; };
+
 // One quarter of a wave tile's MFMAs of a K step: the 16 x 16 blocks (I0 + i, J0 + j) of the accumulators from HI
 // fragments of A and HJ fragments of B (32 bytes per lane each: the 128-byte K step of 16 operand rows), i running
 // slowest (or j with J_OUTER: the set that was read last is then needed one fragment at a time).  After block update
 // number m the caller's side(IntTag<m>) issues whatever memory instructions are to travel with it; scheduling fences
 // keep that order (the written-out MFMA is invisible to the scheduler's instruction classes, so the order is fixed
 // here rather than asked for with group barriers).
-template <int FA, int FB, int I0, int J0, bool J_OUTER, int MI, int MJ, int HI, int HJ, class Side>
-__device__ inline void mma_quadrant(BlockAcc<MI, MJ>& acc, const v8i (&a)[HI], const v8i (&b)[HJ], Side&& side) {
+template <int FA, int FB, int I0, int J0, bool J_OUTER, int MI, int MJ, int HI, int HJ, class Scales, class Side>
+__device__ inline void mma_quadrant(BlockAcc<MI, MJ>& acc, const v8i (&a)[HI], const v8i (&b)[HJ], const Scales& sc, Side&& side) {
     static_for<HI * HJ>([&](auto tag) {
         constexpr int m = decltype(tag)::value;
         constexpr int i = J_OUTER ? m % HI : m / HJ, j = J_OUTER ? m / HI : m % HJ;
-        mma_block<FA, FB, (I0 + i >= kBlocksInFile || J0 + j >= kBlocksInFile)>(acc.t[I0 + i][J0 + j], a[i], b[j]);
+        constexpr bool in_v = I0 + i >= kBlocksInFile || J0 + j >= kBlocksInFile;
+        if constexpr (std::is_same_v<Scales, NoScales>) mma_block<FA, FB, in_v>(acc.t[I0 + i][J0 + j], a[i], b[j]);
+        else mma_block_scaled<FA, FB, in_v, (I0 + i) % 4, (J0 + j) % 4>(acc.t[I0 + i][J0 + j], a[i], b[j], sc.a[(I0 + i) / 4], sc.b[(J0 + j) / 4]);
         side(tag);
         __builtin_amdgcn_sched_barrier(0);
     });
@@ -444,7 +468,15 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     };
     stamp(0);
     // requested now, needed in the epilogue; BF16 operands carry no scales
-    const float scale_a = FA == kFmtBf16 ? 1.0f : *d_sA, scale_b = FB == kFmtBf16 ? 1.0f : *d_sB;
+    constexpr bool BS = V::kBlockScales;       // (their scales are in the products already)
+    float scale_a, scale_b;
+    if constexpr (BS && EDGE != kNoEdge) {
+        // A one that the compiler does not know: with a known one it moves accumulators to scratch memory in front of the guarded epilogue
+        asm("s_mov_b32 %0, 1.0" : "=s"(scale_a));
+        scale_b = scale_a;
+    } else {
+        scale_a = FA == kFmtBf16 || BS ? 1.0f : *d_sA, scale_b = FB == kFmtBf16 || BS ? 1.0f : *d_sB;
+    }
 
     // ---- global -> LDS.  Row-wise operand: one instruction moves 8 rows x 128 B; wave w moves rows
     // [RA w, RA (w+1)) of the A slab (B: RB) with LA (LB) instructions, four waves 16 NX rows with 2 NX; instruction j covers rows
@@ -638,6 +670,40 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc.t[i][j][e] = zero;
 
+    // Block scales: d_sA / d_sB point at the codes, a 128-row group's K step one contiguous piece in which byte 8 (row % 16) + row / 16 is the row's, so
+    // that a lane's row of four neighbouring blocks of 16 rows is one register.  A step's registers are requested two steps ahead, into those of
+    // the step that has just ended; two instructions, a step's newest loads.
+    static_assert(!BS || ((NI == 2 || NI == 4) && (NJ == 2 || NJ == 4) && MODE == kWholeTiles && FA != kFmtBf16), "a wave's rows start at a multiple of 64");
+    constexpr int WA = (MI + 3) / 4, WB = (MJ + 3) / 4, kScaleLoads = BS ? 2 : 0;
+    typedef std::conditional_t<BS, BlockScales<WA, WB>, NoScales> Scales;
+    Scales scales[2];
+    const int pitchA = (Rn + 127) & ~127, pitchB = (Cn + 127) & ~127;
+    auto rsrc_of_scales = [&](const float* d, int pitch, int first) {
+        const int all = ((T + BK - 1) / BK) * pitch;
+        return make_rsrc(reinterpret_cast<const uint8_t*>(d) + first, (unsigned)(all - first));
+    };
+    // (a tile's second group of 128 rows may lie behind the last one: those rows' products go nowhere, whatever bytes are found there)
+    const int firstA = tr * BM + (NI == 4 ? wr * 128 : 0), firstB = tc * BN + (NJ == 4 ? wc * 128 : 0);
+    const __amdgpu_buffer_rsrc_t rsSA = BS ? rsrc_of_scales(d_sA, pitchA, firstA < pitchA ? firstA : 0) : rsA, rsSB = BS ? rsrc_of_scales(d_sB, pitchB, firstB < pitchB ? firstB : 0) : rsB;
+    const int sc_voffA = 8 * (lane & 15) + (NI == 2 ? 4 * wr : 0), sc_voffB = 8 * (lane & 15) + (NJ == 2 ? 4 * (MJ == 4 ? wc : wc >> 1) : 0);
+    auto request_scales = [&](auto& sc, int step) {
+        if constexpr (BS) {
+            const int stepA = step < nk ? step * pitchA : kOutOfRange, stepB = step < nk ? step * pitchB : kOutOfRange;
+            if constexpr (WA == 2) {
+                const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rsSA, sc_voffA, stepA, 0));
+                sc.a[0] = v[0], sc.a[1] = v[1];
+            } else {
+                sc.a[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rsSA, sc_voffA, stepA, 0);
+            }
+            if constexpr (WB == 2) {
+                const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rsSB, sc_voffB, stepB, 0));
+                sc.b[0] = v[0], sc.b[1] = v[1];
+            } else {
+                sc.b[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rsSB, sc_voffB, stepB, 0);
+            }
+        }
+    };
+
     // Fragment sets: the low and high halves of the wave tile's block rows (A) and block columns (B).
     v8i aL[HI], aH[HI], bL[HJ], bH[HJ];
 
@@ -713,23 +779,29 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         constexpr int X0 = XH ? HI : 0, Y0 = XH ? 0 : HI;
         auto& aX = *(XH ? &aH : &aL);
         auto& aY = *(XH ? &aL : &aH);
-        mma_quadrant<FA, FB, X0, 0, false>(acc, aX, bL, [&](auto m) { readsA_of_slot(curA, IntTag<Y0>{}, aY, m); });
-        mma_quadrant<FA, FB, Y0, 0, false>(acc, aY, bL, [&](auto m) { readsB_of_slot(curB, IntTag<HJ>{}, bH, m); });
+        Scales sc = scales[parity];
+        if constexpr (BS && MJ == 2) {
+            // eight waves: a wave's two block columns are one half of the register (written out with its distance to the MFMAs that read it)
+            asm volatile("v_lshrrev_b32 %0, %1, %0\n\ts_nop 4" : "+v"(sc.b[0]) : "s"(16 * (wc & 1)));
+        }
+        mma_quadrant<FA, FB, X0, 0, false>(acc, aX, bL, sc, [&](auto m) { readsA_of_slot(curA, IntTag<Y0>{}, aY, m); });
+        mma_quadrant<FA, FB, Y0, 0, false>(acc, aY, bL, sc, [&](auto m) { readsB_of_slot(curB, IntTag<HJ>{}, bH, m); });
         // the direct-to-LDS loads of the previous step must have landed; its two touch loads, issued
         // after them, may still be in flight
         // (kEdgeUnaligned: the slab was written by ordinary LDS stores, which the barrier orders)
-        if constexpr (UA) {} else if constexpr (kTouch) wait_vmcnt<2>(); else wait_vmcnt<(ST - 2) * kLoadsPerStep>();
+        // (so may the requests for scales behind them; with four stages those of the two steps between are not counted, which waits a little longer)
+        if constexpr (UA) {} else if constexpr (kTouch) wait_vmcnt<2 + kScaleLoads>(); else wait_vmcnt<(ST - 2) * kLoadsPerStep + kScaleLoads>();
         if constexpr (ST == 2) lds_barrier(); else lds_barrier_in_flight();
         __builtin_amdgcn_sched_barrier(0);
         int baseA, baseB;
         load_base(kt + ST < nk ? kb + kt + ST : -1, baseA, baseB);
         voffs_of_step(kt + ST);
         const int fetch_step = kt + 3 < nk ? kt + 3 : nk - 1;        // kEdgeUnaligned: the loads run a step ahead of the LDS writes
-        mma_quadrant<FA, FB, Y0, HJ, true>(acc, aY, bH, [&](auto m) {
+        mma_quadrant<FA, FB, Y0, HJ, true>(acc, aY, bH, sc, [&](auto m) {
             readsB_of_slot(nxtB, IntTag<0>{}, bL, m);     // past the last slab this reads bytes that are never used
             loads_of_slot(curA, curB, baseA, baseB, fetch_step, m);
         });
-        mma_quadrant<FA, FB, X0, HJ, false>(acc, aX, bH, [&](auto m) {
+        mma_quadrant<FA, FB, X0, HJ, false>(acc, aX, bH, sc, [&](auto m) {
             readsA_of_slot(nxtA, IntTag<Y0>{}, aY, m);
             loads_of_slot(curA, curB, baseA, baseB, fetch_step, IntTag<kSlots + decltype(m)::value>{});
         });
@@ -744,9 +816,17 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
             touchB[parity] = __builtin_amdgcn_raw_buffer_load_b32(rsB, touch_voffB, on ? (kb + kp) * ksB : kOutOfRange, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (BS) {
+            request_scales(scales[parity], kt + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
     if constexpr (!fixup) {
+    if constexpr (BS) {
+        request_scales(scales[0], 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     // both stages are requested at once; only the first has to have landed before the first fragments
     if constexpr (UA) {
         static_for<kLoadsPerStep>([&](auto piece) { fetch(0, piece); });
@@ -769,7 +849,12 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         touchA[1] = __builtin_amdgcn_raw_buffer_load_b32(rsA, touch_voffA, on ? (kb + 2) * ksA : kOutOfRange, 0);
         touchB[1] = __builtin_amdgcn_raw_buffer_load_b32(rsB, touch_voffB, on ? (kb + 2) * ksB : kOutOfRange, 0);
     }
-    if constexpr (!UA) wait_vmcnt<(ST - 1) * kLoadsPerStep + (kTouch ? 2 : 0)>();
+    if constexpr (BS) {                           // the newest loads, as at the end of every step
+        __builtin_amdgcn_sched_barrier(0);
+        request_scales(scales[1], 1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (!UA) wait_vmcnt<(ST - 1) * kLoadsPerStep + (kTouch ? 2 : 0) + kScaleLoads>();
     if constexpr (ST == 2) lds_barrier(); else lds_barrier_in_flight();
     read_fragsA(ldsA0, IntTag<0>{}, aL);
     read_fragsB(ldsB0, IntTag<0>{}, bL);

@@ -170,6 +170,9 @@ int launch_gemm_tn(const uint8_t* A, int fmtA, const uint8_t* B, int fmtB, int64
                    int accumulate, float* d_amax_c, bool amax_is_zeroed, hipStream_t stream, int num_cus,
                    GemmScratch scratch, bool slabs_a = false, bool slabs_b = false);
 
+// Clears the absmax accumulator of a contraction.
+void launch_gemm_amax_reset(unsigned* amax, hipStream_t stream);
+
 // The 256 x 256 tile kernel with phase stamps: 16 words of 64 bits per workgroup id, gemm_phase_stamp_blocks() ids.
 int gemm_phase_stamp_blocks(int64_t R, int64_t C);
 int launch_gemm_phase_stamps(const uint8_t* A, const uint8_t* B, int64_t R, int64_t C, int64_t T, const float* sA,

@@ -35,6 +35,7 @@ EXPORTS = ["llmq_status_string", "llmq_version", "llmq_amax_workspace_bytes", "l
            "llmq_fp8_linear_fwd", "llmq_fp8_linear_dgrad", "llmq_fp8_linear_wgrad",
            "llmq_scale_from_amax", "llmq_swiglu_workspace_bytes", "llmq_swiglu_fwd", "llmq_swiglu_fwd_fp8", "llmq_swiglu_fwd_fp8_slabs",
            "llmq_swiglu_bwd", "llmq_rmsnorm_workspace_bytes", "llmq_rmsnorm_fwd", "llmq_rmsnorm_apply_fp8", "llmq_rmsnorm_apply_fp8_slabs",
+           "llmq_block_scales_bytes", "llmq_quantize_fp8_blocks", "llmq_fp8_gemm_blocks",
            "llmq_calibrate_mfma", "llmq_calibrate_copy", "llmq_calibrate_gemm_phases_bytes", "llmq_calibrate_gemm_phases"]
 
 
@@ -113,6 +114,12 @@ def lib() -> ctypes.CDLL:
     L.llmq_rmsnorm_apply_fp8.argtypes = [vp, vp, vp, i64, i64, vp, i32, vp, vp, vp, vp]
     L.llmq_rmsnorm_apply_fp8_slabs.restype = i32
     L.llmq_rmsnorm_apply_fp8_slabs.argtypes = [vp, vp, vp, i64, i64, vp, i32, vp, vp, vp, vp]
+    L.llmq_block_scales_bytes.restype = sz
+    L.llmq_block_scales_bytes.argtypes = [i64, i64]
+    L.llmq_quantize_fp8_blocks.restype = i32
+    L.llmq_quantize_fp8_blocks.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp, vp, vp]
+    L.llmq_fp8_gemm_blocks.restype = i32
+    L.llmq_fp8_gemm_blocks.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, vp]
     L.llmq_calibrate_mfma.restype = i32
     L.llmq_calibrate_mfma.argtypes = [i32, i32, i32, i32, vp, c.POINTER(c.c_double), vp]
     L.llmq_calibrate_gemm_phases_bytes.restype = sz
@@ -480,6 +487,54 @@ def llmq_rmsnorm_apply_fp8_slabs(res: torch.Tensor, w: torch.Tensor, rstd: torch
                                               _dev(d_scale_y, torch.float32, "d_scale_y"), fmt, _dev(q, torch.uint8, "q"),
                                               _dev(q_t, torch.uint8, "q_t"), _dev(y, torch.bfloat16, "y"), _stream()),
            "llmq_rmsnorm_apply_fp8_slabs")
+
+
+def _here(t: Optional[torch.Tensor], dtype=None, name="tensor", numel: Optional[int] = None) -> Optional[int]:
+    """_dev for calls that also want the current device, whose stream they run on, and a number of elements."""
+    p = _dev(t, dtype, name)
+    if t is not None:
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+        if numel is not None and t.numel() != numel:
+            raise ValueError("%s must have %d elements, got %s" % (name, numel, tuple(t.shape)))
+    return p
+
+
+def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int]:
+    if t.dim() != 2:
+        raise ValueError("%s must be 2-D, got %s" % (name, tuple(t.shape)))
+    return int(t.shape[0]), int(t.shape[1])
+
+
+def llmq_block_scales_bytes(rows: int, cols: int) -> int:
+    return int(lib().llmq_block_scales_bytes(rows, cols))
+
+
+def llmq_quantize_fp8_blocks(x: torch.Tensor, fmt: int, block_rows: int, q: Optional[torch.Tensor], s: Optional[torch.Tensor],
+                             q_t: Optional[torch.Tensor] = None, s_t: Optional[torch.Tensor] = None) -> None:
+    """s and s_t: uint8, llmq_block_scales_bytes(rows, cols) and llmq_block_scales_bytes(cols, rows) elements."""
+    status = _fast.quantize_fp8_blocks(x, fmt, block_rows, q, s, q_t, s_t)
+    if status is not None:
+        return _check(status, "llmq_quantize_fp8_blocks") if status else None
+    rows, cols = _matrix(x, "x")
+    n, n_s, n_st = rows * cols, llmq_block_scales_bytes(rows, cols), llmq_block_scales_bytes(cols, rows)
+    _check(lib().llmq_quantize_fp8_blocks(_here(x, torch.bfloat16, "x"), rows, cols, fmt, block_rows, _here(q, torch.uint8, "q", n), _here(s, torch.uint8, "s", n_s),
+                                          _here(q_t, torch.uint8, "q_t", n), _here(s_t, torch.uint8, "s_t", n_st), _stream()), "llmq_quantize_fp8_blocks")
+
+
+def llmq_fp8_gemm_blocks(A: torch.Tensor, sA: torch.Tensor, fmtA: int, B: torch.Tensor, sB: torch.Tensor, fmtB: int, c: torch.Tensor,
+                         accumulate: bool = False, d_amax_c: Optional[torch.Tensor] = None) -> None:
+    status = _fast.fp8_gemm_blocks(A, sA, fmtA, B, sB, fmtB, c, accumulate, d_amax_c)
+    if status is not None:
+        return _check(status, "llmq_fp8_gemm_blocks") if status else None
+    R, T = _matrix(A, "A")
+    C, T2 = _matrix(B, "B")
+    if T != T2 or tuple(c.shape) != (R, C):
+        raise ValueError("shape mismatch: A %s, B %s, c %s" % (tuple(A.shape), tuple(B.shape), tuple(c.shape)))
+    _check(lib().llmq_fp8_gemm_blocks(_here(A, torch.uint8, "A"), _here(sA, torch.uint8, "sA", llmq_block_scales_bytes(R, T)), fmtA,
+                                      _here(B, torch.uint8, "B"), _here(sB, torch.uint8, "sB", llmq_block_scales_bytes(C, T)), fmtB, R, C, T,
+                                      _here(c, torch.bfloat16, "c"), int(bool(accumulate)), _here(d_amax_c, torch.float32, "d_amax_c", 1), _stream()),
+           "llmq_fp8_gemm_blocks")
 
 
 def llmq_calibrate_mfma(fmtA: int, fmtB: int, random_bits: bool, iters: int, d_sink: torch.Tensor) -> float:
