@@ -422,6 +422,41 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
                                  void* y_bf16, void* stream);
 
 /*
+ * RMSNorm of every query and key head joined with the rotation by position, between the QKV projection and attention, and the gradient of both, which
+ * is the dY of the QKV projection.
+ *
+ *   qkv [M, (Hq + 2 Hkv) D] BF16: a row is Hq query heads, Hkv key heads and Hkv value heads of D values each.
+ *   n[i] = (x[i] rstd) w[i],   rstd = 1 / sqrt(mean of x^2 over the head + eps),   w = wq or wk, [D] BF16; both NULL: no norm, n = x
+ *   the first `rot` values of a head (even, 0 .. D) are turned in pairs, the others stay:  interleaved == 0: i with i + rot/2;  1: 2 i with 2 i + 1
+ *     y_a = n_a cos t - n_b sin t,   y_b = n_b cos t + n_a sin t,   t = d_positions[m] d_inv_freq[pair]
+ *   d_positions [M] int64 (any value; those of a cache go on where it ends), d_inv_freq [rot/2] double, radians per position, finite.  The angle is found in 64-bit
+ *   fractions of a turn: to 2^-52 of the frequency times the position, for any position.  Sums and everything else in binary32, one rounding to BF16.
+ *
+ * llmq_qk_norm_rope_fwd: q [M, Hq D] and k [M, Hkv D] BF16; rstd [M, Hq + Hkv] float, kept for the backward pass, or NULL (not with NULL weights: ignored).
+ *   The values V stay where they are.  q and k may be the query and key columns of qkv themselves (in place).
+ * llmq_qk_norm_rope_bwd: dq, dk of q and k, dv of V (or NULL: V's columns of dqkv already hold it, or dv points at them) -> dqkv, laid out as qkv, and
+ *     g = dy turned back;   dw[i] = sum over rows and heads of g[i] x[i] rstd;   dx[i] = rstd (g[i] w[i] - x[i] rstd mean(g w x rstd))
+ *   dwq, dwk [D] float, added to if accumulate != 0; NULL: not wanted.  The sums are taken in an order that depends on the sizes alone.  d_amax, d_scale [1] float or
+ *   NULL: absmax of all of dqkv and its scale for fmt, bit for bit as llmq_amax of dqkv has them.  qkv and rstd are not read without a norm (and may be NULL).
+ *   dq and dk may be the query and key columns of dqkv.  ws: llmq_qk_norm_rope_workspace_bytes bytes, 16-byte aligned, contents irrelevant; NULL if neither dw nor
+ *   d_amax is wanted.
+ * *_stride: elements from row to row, at least a row's width.  Rows may start at any element (2-byte aligned); D and rot multiples of 8 (D up to 512) with rows that
+ * start at multiples of 8 bytes are fast, others take a slow kernel.  M, Hq, Hkv >= 1, heads up to 65536, 1 <= D <= 1024.
+ */
+int llmq_qk_norm_rope_fwd(const void* qkv_bf16, int64_t qkv_stride, int64_t M, int Hq, int Hkv, int D,
+                          const void* wq_bf16, const void* wk_bf16, float eps, const int64_t* d_positions,
+                          const double* d_inv_freq, int rot, int interleaved, void* q_bf16, int64_t q_stride,
+                          void* k_bf16, int64_t k_stride, float* rstd, void* stream);
+size_t llmq_qk_norm_rope_workspace_bytes(int64_t M, int Hq, int Hkv, int D);
+int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk_bf16, int64_t dk_stride,
+                          const void* dv_bf16, int64_t dv_stride, const void* qkv_bf16, int64_t qkv_stride,
+                          int64_t M, int Hq, int Hkv, int D, const void* wq_bf16, const void* wk_bf16,
+                          const float* rstd, const int64_t* d_positions, const double* d_inv_freq, int rot,
+                          int interleaved, void* dqkv_bf16, int64_t dqkv_stride, float* dwq, float* dwk,
+                          int accumulate, int fmt, float* d_amax, float* d_scale, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/*
  * Peak calibration (the paper's appendix "A note on MFU" measures the attainable peak with a large-matmul
  * micro-benchmark instead of trusting the spec sheet).  Both calls only enqueue; the caller times them.
  *

@@ -316,6 +316,26 @@ struct HereArgs : Args {
         if (t && numel >= 0 && t->numel() != numel) { ok = false; return nullptr; }
         return t ? t->data_ptr() : nullptr;
     }
+    // A BF16 matrix [M, width] whose rows may lie apart
+    void* rows(int i, int64_t M, int64_t width, bool required, int64_t& stride) {
+        stride = 0;
+        if (a[i] == Py_None) { if (required) ok = false; return nullptr; }
+        if (!THPVariable_CheckExact(a[i])) { ok = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (!t.is_cuda() || t.device().index() != device || t.layout() != at::kStrided || t.scalar_type() != kBf16 || t.dim() != 2 || t.size(0) != M || t.size(1) != width ||
+            (width > 1 && t.stride(1) != 1) || (M > 1 && t.stride(0) < width)) { ok = false; return nullptr; }
+        stride = M > 1 ? t.stride(0) : width;
+        return t.data_ptr();
+    }
+    int64_t rows_of(int i) {
+        if (!THPVariable_CheckExact(a[i]) || THPVariable_Unpack(a[i]).dim() != 2) { ok = false; return 0; }
+        return THPVariable_Unpack(a[i]).size(0);
+    }
+    int64_t numel_of(int i) {
+        if (a[i] == Py_None) return 0;
+        if (!THPVariable_CheckExact(a[i])) { ok = false; return 0; }
+        return THPVariable_Unpack(a[i]).numel();
+    }
     uint8_t* codes(int i, int64_t numel, bool required) { return static_cast<uint8_t*>(pointer(i, kU8, numel, required)); }
 };
 
@@ -352,11 +372,59 @@ LLMQ_BINDING(fp8_gemm_blocks) {
     });
 }
 
+LLMQ_BINDING(qk_norm_rope_fwd) {
+    return run(args, n, 13, [](Args& args_) {
+        HereArgs a(args_);
+        const int64_t M = a.rows_of(0);
+        const int Hq = a.i32(1), Hkv = a.i32(2), D = a.i32(3), rot = (int)(2 * a.numel_of(8));
+        int64_t xs = 0, qs = 0, ks = 0;
+        void* x = a.rows(0, M, (int64_t)(Hq + 2 * (int64_t)Hkv) * D, true, xs);
+        void *wq = a.pointer(4, kBf16, D, false), *wk = a.pointer(5, kBf16, D, false);
+        if (!wq != !wk || !PyFloat_CheckExact(a.a[6])) a.ok = false;
+        const float eps = a.ok ? (float)PyFloat_AS_DOUBLE(a.a[6]) : 0.0f;
+        int64_t* positions = static_cast<int64_t*>(a.pointer(7, at::kLong, rot ? M : -1, false));
+        double* freq = static_cast<double*>(a.pointer(8, at::kDouble, -1, false));
+        const int interleaved = a.truth(9);
+        void *q = a.rows(10, M, (int64_t)Hq * D, true, qs), *k = a.rows(11, M, (int64_t)Hkv * D, true, ks);
+        float* rstd = static_cast<float*>(a.pointer(12, kF32, M * ((int64_t)Hq + Hkv), false));
+        args_.ok = a.ok;
+        return [=](void* s) { return llmq_qk_norm_rope_fwd(x, xs, M, Hq, Hkv, D, wq, wk, eps, positions, freq, rot, interleaved, q, qs, k, ks, rstd, s); };
+    });
+}
+
+LLMQ_BINDING(qk_norm_rope_bwd) {
+    return run(args, n, 21, [](Args& args_) {
+        HereArgs a(args_);
+        const int64_t M = a.rows_of(13);
+        const int Hq = a.i32(4), Hkv = a.i32(5), D = a.i32(6), rot = (int)(2 * a.numel_of(11));
+        const int64_t width = (int64_t)(Hq + 2 * (int64_t)Hkv) * D;
+        int64_t qs = 0, ks = 0, vs = 0, xs = 0, dxs = 0;
+        void *dq = a.rows(0, M, (int64_t)Hq * D, true, qs), *dk = a.rows(1, M, (int64_t)Hkv * D, true, ks), *dv = a.rows(2, M, (int64_t)Hkv * D, false, vs);
+        void *x = a.rows(3, M, width, false, xs), *dx = a.rows(13, M, width, true, dxs);
+        void *wq = a.pointer(7, kBf16, D, false), *wk = a.pointer(8, kBf16, D, false);
+        if (!wq != !wk) a.ok = false;
+        float* rstd = static_cast<float*>(a.pointer(9, kF32, M * ((int64_t)Hq + Hkv), false));
+        int64_t* positions = static_cast<int64_t*>(a.pointer(10, at::kLong, rot ? M : -1, false));
+        double* freq = static_cast<double*>(a.pointer(11, at::kDouble, -1, false));
+        const int interleaved = a.truth(12);
+        float *dwq = static_cast<float*>(a.pointer(14, kF32, D, false)), *dwk = static_cast<float*>(a.pointer(15, kF32, D, false));
+        const int accumulate = a.truth(16), fmt = a.i32(17);
+        float *amax = static_cast<float*>(a.pointer(18, kF32, 1, false)), *scale = static_cast<float*>(a.pointer(19, kF32, 1, false));
+        void* ws = a.pointer(20, kU8, -1, false);
+        const size_t bytes = ws ? (size_t)a.numel_of(20) : 0;
+        args_.ok = a.ok;
+        return [=](void* s) {
+            return llmq_qk_norm_rope_bwd(dq, qs, dk, ks, dv, vs, x, xs, M, Hq, Hkv, D, wq, wk, rstd, positions, freq, rot, interleaved, dx, dxs, dwq, dwk, accumulate, fmt, amax, scale, ws,
+                                         bytes, s);
+        };
+    });
+}
+
 #define LLMQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {LLMQ_METHOD(linear_fwd), LLMQ_METHOD(linear_dgrad), LLMQ_METHOD(linear_wgrad), LLMQ_METHOD(amax), LLMQ_METHOD(quantize_fp8),
                            LLMQ_METHOD(quantize_fp8_slabs), LLMQ_METHOD(bf16_gemm_tn), LLMQ_METHOD(swiglu_fwd), LLMQ_METHOD(swiglu_fwd_fp8),
                            LLMQ_METHOD(swiglu_fwd_fp8_slabs), LLMQ_METHOD(swiglu_bwd), LLMQ_METHOD(rmsnorm_fwd), LLMQ_METHOD(rmsnorm_apply_fp8),
-                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), {nullptr, nullptr, 0, nullptr}};
+                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

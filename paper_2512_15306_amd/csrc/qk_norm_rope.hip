@@ -1,0 +1,614 @@
+// Queries and keys of a QKV projection: RMSNorm of every head and the rotation by position in one pass, and the gradient of both.
+//
+//   n[i] = x[i] rstd w[i],  rstd = 1 / sqrt(mean x^2 + eps)  over the D values of a head (without weights: n = x)
+//   pairs (a, b) of the first `rot` values: i and i + rot/2, or neighbours;   y_a = n_a cos t - n_b sin t,  y_b = n_b cos t + n_a sin t
+//   backward: g = the same rotation by -t of dy;  dw += g x rstd;  dx = rstd (g w - x rstd mean(g w x rstd))
+//
+// HBM-bound: 2 bytes read and 2 written per value (backward 4 and 2).  What there is to compute is arranged around the angles: t = position f mod one turn is
+// a product of 64-bit whole numbers, with the frequency as a 64-bit fraction of a turn, exact for every position, so that far positions lose nothing and no table
+// is read; a sine and a cosine by their series then cost about 25 instructions, which a lane pays once per token for its four pairs and uses
+// for all heads.  For that a wave takes a token and walks over its heads, as many at a time as fit (four of 128 values), eight
+// values a lane in two pieces of 8 bytes that hold both halves of its pairs: no exchange between lanes but the sums of a head.
+// The sums of dw stay in a lane's registers over all tokens and heads of its wave; each workgroup leaves one row of them, which a second kernel adds
+// in the order of the workgroups (no atomics).
+#include "api_checks.h"
+#include "llmq_device.h"
+
+namespace llmq {
+
+typedef uint16_t u16;
+
+struct QkArgs {
+    int64_t M;
+    int Hq, Hkv, D, rot, interleaved;
+    const u16* x;                               // [M, Hq + 2 Hkv, D]
+    const u16 *wq, *wk;                         // NULL: no norm
+    const int64_t* positions;
+    const double* inv_freq;
+    float eps;
+    float* rstd;                                // [M, Hq + Hkv]; written by the forward pass if not NULL, read by the backward pass
+    u16 *q, *k;                                 // forward: outputs; backward: gradients of the outputs (not written)
+    const u16* dv;                              // backward: NULL: V's gradient is in its place already
+    u16* dx;                                    // backward: [M, Hq + 2 Hkv, D]
+    int64_t x_stride, q_stride, k_stride, dv_stride, dx_stride;        // elements from row to row
+    float* dw_partial;                          // backward: a row of 2 D sums for each workgroup, or NULL
+    unsigned* amax_partial;                     // backward: a word for each workgroup, or NULL
+    int split;                                  // waves that share a token
+};
+
+// A frequency in radians as a 64-bit fraction of a turn per position (whole turns do not matter)
+__device__ inline uint64_t turns_of(double inv_freq) {
+    double t = inv_freq * 0.15915494309189533577;            // 1 / (2 pi)
+    t -= __builtin_floor(t);                                 // [0, 1]
+    const double hi = __builtin_floor(t * 4294967296.0);
+    const double lo = (t * 4294967296.0 - hi) * 4294967296.0;
+    return ((uint64_t)hi << 32) + (uint64_t)lo;              // (a whole turn wraps to none)
+}
+
+// Cosine and sine of a fraction of a turn: to the nearest quarter, the rest (at most pi/4) by the Taylor series, whose first missing terms are
+// x^11/11! < 2e-9 and x^10/10! < 3e-8.
+__device__ inline void cos_sin(uint64_t turns, float& c, float& s) {
+    const unsigned top = (unsigned)(turns >> 32);
+    const unsigned quarter = (top + 0x20000000u) >> 30;
+    const float x = (float)(int)(top - (quarter << 30)) * 1.46291807926715968e-9f;         // 2 pi / 2^32
+    const float z = x * x;
+    const float sine = x * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
+    const float cosine = __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+    const bool odd = quarter & 1;
+    const float a = odd ? sine : cosine, b = odd ? cosine : sine;
+    c = ((quarter + 1) & 2) ? -a : a;
+    s = (quarter & 2) ? -b : b;
+}
+
+// Sum over groups of G neighbouring lanes, in all of them
+template <int G>
+__device__ inline float group_sum(float v) {
+    auto dpp = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, false)); };
+    v += dpp(std::integral_constant<int, 0xB1>{});           // quad_perm [1,0,3,2]
+    v += dpp(std::integral_constant<int, 0x4E>{});           // quad_perm [2,3,0,1]
+    v += dpp(std::integral_constant<int, 0x141>{});          // row_half_mirror
+    if constexpr (G >= 16) v += dpp(std::integral_constant<int, 0x140>{});      // row_mirror
+    if constexpr (G >= 32) { const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false); v = __uint_as_float(r[0]) + __uint_as_float(r[1]); }
+    if constexpr (G >= 64) { const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false); v = __uint_as_float(r[0]) + __uint_as_float(r[1]); }
+    return v;
+}
+
+// Eight values of a head: two pieces of four
+struct Eight { v2u lo, hi; };
+__device__ inline void unpack(const Eight& e, float (&f)[8]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        f[2 * j] = __uint_as_float(e.lo[j] << 16);
+        f[2 * j + 1] = __uint_as_float(e.lo[j] & 0xFFFF0000u);
+        f[4 + 2 * j] = __uint_as_float(e.hi[j] << 16);
+        f[5 + 2 * j] = __uint_as_float(e.hi[j] & 0xFFFF0000u);
+    }
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+__device__ inline unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(v2f{a, b}, bf16x2)); }
+__device__ inline Eight pack(const float (&f)[8]) {
+    return Eight{v2u{pack2(f[0], f[1]), pack2(f[2], f[3])}, v2u{pack2(f[4], f[5]), pack2(f[6], f[7])}};
+}
+
+// The lane's place among the G lanes of a head: its two pieces' columns and its angles' frequencies
+template <int G>
+struct Place {
+    int l, sub;                                  // lane of the head; head among those of a pass
+    bool there, turned;
+    int lo, hi;
+    uint64_t f[4];
+    __device__ Place(const QkArgs& a) {
+        const int lane = threadIdx.x & (kWave - 1);
+        l = lane % G, sub = lane / G;
+        there = 8 * l < a.D;
+        turned = 8 * l < a.rot;
+        lo = turned && !a.interleaved ? 4 * l : 8 * l;       // (the values behind the turned ones start at a multiple of 8 as well)
+        hi = turned && !a.interleaved ? 4 * l + a.rot / 2 : 8 * l + 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = turned ? turns_of(a.inv_freq[4 * l + j]) : 0;
+    }
+    __device__ Eight load(const u16* p) const { return Eight{*reinterpret_cast<const v2u*>(p + lo), *reinterpret_cast<const v2u*>(p + hi)}; }
+    __device__ void store(u16* p, const Eight& e) const {
+        *reinterpret_cast<v2u*>(p + lo) = e.lo;
+        *reinterpret_cast<v2u*>(p + hi) = e.hi;
+    }
+    // SIGN 1: by the angles, -1: back
+    template <int SIGN>
+    __device__ void turn(const float (&c)[4], const float (&s)[4], bool interleaved, float (&v)[8]) const {
+        auto pair = [&](float& a, float& b, float cc, float ss) {
+            const float x = a, y = b;
+            a = __builtin_fmaf(x, cc, SIGN > 0 ? -y * ss : y * ss);
+            b = __builtin_fmaf(y, cc, SIGN > 0 ? x * ss : -x * ss);
+        };
+        if (interleaved) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pair(v[2 * j], v[2 * j + 1], c[j], s[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pair(v[j], v[4 + j], c[j], s[j]);
+        }
+    }
+    __device__ void angles(int64_t position, float (&c)[4], float (&s)[4]) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) cos_sin((uint64_t)position * f[j], c[j], s[j]);
+    }
+};
+
+constexpr int kQkThreads = 256, kQkWaves = kQkThreads / kWave, kQkAtOnce = 4;
+
+template <int G, bool NORM>
+__global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
+    const int wave = blockIdx.x * kQkWaves + threadIdx.x / kWave, waves = gridDim.x * kQkWaves;
+    const Place<G> at(a);
+    constexpr int kHeads = kWave / G;            // of a pass
+    const int heads = a.Hq + a.Hkv, passes = (heads + kHeads - 1) / kHeads;
+    const int part = wave % a.split, per_part = (passes + a.split - 1) / a.split;
+    const int first = part * per_part, last = first + per_part < passes ? first + per_part : passes;
+    float wq[8], wk[8];
+    if constexpr (NORM) {
+        if (at.there) { unpack(at.load(a.wq), wq); unpack(at.load(a.wk), wk); }
+    }
+    for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
+        float c[4], s[4];
+        const int64_t position = a.rot ? a.positions[m] : 0;
+        const u16* x = a.x + m * a.x_stride;
+        for (int p0 = first; p0 < last; p0 += kQkAtOnce) {
+            Eight in[kQkAtOnce];
+#pragma unroll
+            for (int u = 0; u < kQkAtOnce; ++u) {
+                const int head = (p0 + u) * kHeads + at.sub;
+                if (p0 + u < last && head < heads && at.there) in[u] = at.load(x + (int64_t)head * a.D);
+                else in[u] = Eight{v2u{0, 0}, v2u{0, 0}};
+            }
+            if (p0 == first) at.angles(position, c, s);
+#pragma unroll
+            for (int u = 0; u < kQkAtOnce; ++u) {
+                const int head = (p0 + u) * kHeads + at.sub;
+                float v[8];
+                unpack(in[u], v);
+                if constexpr (NORM) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(v[j], v[j], sum);
+                    const float rstd = 1.0f / __builtin_sqrtf(group_sum<G>(sum) / (float)a.D + a.eps);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = v[j] * rstd * (head < a.Hq ? wq[j] : wk[j]);
+                    if (a.rstd && at.l == 0 && p0 + u < last && head < heads) a.rstd[m * heads + head] = rstd;
+                }
+                at.template turn<1>(c, s, a.interleaved, v);
+                if (p0 + u < last && head < heads && at.there)
+                    at.store(head < a.Hq ? a.q + m * a.q_stride + (int64_t)head * a.D : a.k + m * a.k_stride + (int64_t)(head - a.Hq) * a.D, pack(v));
+            }
+        }
+    }
+}
+
+__device__ inline void track(unsigned& mag, const Eight& e) { mag = pk_max_mag(pk_max_mag(pk_max_mag(pk_max_mag(mag, e.lo[0]), e.lo[1]), e.hi[0]), e.hi[1]); }
+
+// The gradient of V on its way to its place, V values a lane at once, `step` lanes side by side
+template <int V>
+__device__ inline void move_v(const QkArgs& a, int64_t m, int first, int step, unsigned& mag) {
+    const int64_t n = (int64_t)a.Hkv * a.D;
+    u16* to = a.dx + m * a.dx_stride + (int64_t)(a.Hq + a.Hkv) * a.D;
+    const u16* from = a.dv ? a.dv + m * a.dv_stride : to;
+    if (!a.dv && !a.amax_partial) return;
+    for (int64_t i = (int64_t)first * V; i < n; i += (int64_t)step * V) {
+        if constexpr (V == 4) {
+            const v2u v = *reinterpret_cast<const v2u*>(from + i);
+            mag = pk_max_mag(pk_max_mag(mag, v[0]), v[1]);
+            if (a.dv) *reinterpret_cast<v2u*>(to + i) = v;
+        } else {
+            const u16 v = from[i];
+            mag = pk_max_mag(mag, v);
+            if (a.dv) to[i] = v;
+        }
+    }
+}
+
+// A workgroup's sums and absmax.  dwq / dwk: a lane's sums for its eight columns.
+template <int G>
+__device__ inline void leave_partials(const QkArgs& a, const Place<G>& at, float (&dwq)[8], float (&dwk)[8], unsigned mag, float* s_dw, unsigned* s_part) {
+    if (a.dw_partial) {
+        // the heads of a pass first, then the waves one after the other, each adding to what the ones before it left
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int step = G; step < kWave; step *= 2) {
+                dwq[j] += __shfl_xor(dwq[j], step);
+                dwk[j] += __shfl_xor(dwk[j], step);
+            }
+        }
+        for (int w = 0; w < kQkWaves; ++w) {
+            if ((int)(threadIdx.x / kWave) == w && at.sub == 0 && at.there) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int col = j < 4 ? at.lo + j : at.hi + j - 4;
+                    s_dw[col] = (w ? s_dw[col] : 0.0f) + dwq[j];
+                    s_dw[a.D + col] = (w ? s_dw[a.D + col] : 0.0f) + dwk[j];
+                }
+            }
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) a.dw_partial[(int64_t)blockIdx.x * 2 * a.D + i] = s_dw[i];
+    }
+    if (a.amax_partial) {
+        mag = (mag & 0xFFFFu) > (mag >> 16) ? mag & 0xFFFFu : mag >> 16;
+        mag = block_max_u32<kQkThreads>(mag, s_part);
+        if (threadIdx.x == 0) a.amax_partial[blockIdx.x] = mag;
+    }
+}
+
+template <int G, bool NORM>
+__global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
+    __shared__ float s_dw[NORM ? 2 * 8 * G : 1];
+    __shared__ unsigned s_part[kQkWaves];
+    const int wave = blockIdx.x * kQkWaves + threadIdx.x / kWave, waves = gridDim.x * kQkWaves;
+    const Place<G> at(a);
+    constexpr int kHeads = kWave / G;
+    const int heads = a.Hq + a.Hkv, passes = (heads + kHeads - 1) / kHeads;
+    const int part = wave % a.split, per_part = (passes + a.split - 1) / a.split;
+    const int first = part * per_part, last = first + per_part < passes ? first + per_part : passes;
+    float wq[8], wk[8], dwq[8] = {}, dwk[8] = {};
+    unsigned mag = 0;
+    if constexpr (NORM) {
+        if (at.there) { unpack(at.load(a.wq), wq); unpack(at.load(a.wk), wk); }
+    }
+    for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
+        float c[4], s[4];
+        const int64_t position = a.rot ? a.positions[m] : 0;
+        for (int p0 = first; p0 < last; p0 += kQkAtOnce) {
+            Eight in[kQkAtOnce], dy[kQkAtOnce];
+            float rstd[kQkAtOnce];
+#pragma unroll
+            for (int u = 0; u < kQkAtOnce; ++u) {
+                const int head = (p0 + u) * kHeads + at.sub;
+                in[u] = dy[u] = Eight{v2u{0, 0}, v2u{0, 0}};
+                rstd[u] = 0.0f;
+                if (p0 + u < last && head < heads && at.there) {
+                    dy[u] = at.load(head < a.Hq ? a.q + m * a.q_stride + (int64_t)head * a.D : a.k + m * a.k_stride + (int64_t)(head - a.Hq) * a.D);
+                    if constexpr (NORM) {
+                        in[u] = at.load(a.x + m * a.x_stride + (int64_t)head * a.D);
+                        rstd[u] = a.rstd[m * heads + head];
+                    }
+                }
+            }
+            if (p0 == first) at.angles(position, c, s);
+#pragma unroll
+            for (int u = 0; u < kQkAtOnce; ++u) {
+                const int head = (p0 + u) * kHeads + at.sub;
+                float g[8];
+                unpack(dy[u], g);
+                at.template turn<-1>(c, s, a.interleaved, g);
+                if constexpr (NORM) {
+                    float n[8], sum = 0.0f;
+                    unpack(in[u], n);
+                    const bool query = head < a.Hq;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        n[j] *= rstd[u];
+                        const float gn = g[j] * n[j];
+                        dwq[j] += query ? gn : 0.0f;
+                        dwk[j] += query ? 0.0f : gn;
+                        g[j] *= query ? wq[j] : wk[j];
+                        sum = __builtin_fmaf(g[j], n[j], sum);
+                    }
+                    const float mean = group_sum<G>(at.there ? sum : 0.0f) / (float)a.D;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[j] = rstd[u] * __builtin_fmaf(-n[j], mean, g[j]);
+                }
+                if (p0 + u < last && head < heads && at.there) {
+                    const Eight out = pack(g);
+                    track(mag, out);
+                    at.store(a.dx + m * a.dx_stride + (int64_t)head * a.D, out);
+                }
+            }
+        }
+        move_v<4>(a, m, (threadIdx.x & (kWave - 1)) + part * kWave, a.split * kWave, mag);
+    }
+    leave_partials<G>(a, at, dwq, dwk, mag, s_dw, s_part);
+}
+
+// ---- Any head size, stride and alignment: a wave for each head of a token, value by value, twice over the head.  Pair p of the turned values, or the single value
+// behind them.
+struct PairCols { int a, b; };
+__device__ inline PairCols pair_cols(const QkArgs& a, int p) { return a.interleaved ? PairCols{2 * p, 2 * p + 1} : PairCols{p, p + a.rot / 2}; }
+__device__ inline float value(const u16* p, int i) { return __uint_as_float((unsigned)p[i] << 16); }
+__device__ inline u16 rounded(float f) { return __builtin_bit_cast(u16, (__bf16)f); }
+
+template <bool NORM>
+__global__ __launch_bounds__(kQkThreads) void qk_fwd_any_kernel(const QkArgs a) {
+    const int lane = threadIdx.x & (kWave - 1), heads = a.Hq + a.Hkv;
+    const int64_t waves = (int64_t)gridDim.x * kQkWaves;
+    for (int64_t at = (int64_t)blockIdx.x * kQkWaves + threadIdx.x / kWave; at < a.M * heads; at += waves) {
+        const int64_t m = at / heads;
+        const int head = (int)(at - m * heads);
+        const u16* x = a.x + m * a.x_stride + (int64_t)head * a.D;
+        u16* y = head < a.Hq ? a.q + m * a.q_stride + (int64_t)head * a.D : a.k + m * a.k_stride + (int64_t)(head - a.Hq) * a.D;
+        const u16* w = head < a.Hq ? a.wq : a.wk;
+        float rstd = 1.0f;
+        if constexpr (NORM) {
+            float sum = 0.0f;
+            for (int i = lane; i < a.D; i += kWave) { const float v = value(x, i); sum = __builtin_fmaf(v, v, sum); }
+            rstd = 1.0f / __builtin_sqrtf(group_sum<kWave>(sum) / (float)a.D + a.eps);
+            if (a.rstd && lane == 0) a.rstd[at] = rstd;
+        }
+        auto normed = [&](int i) { return NORM ? value(x, i) * rstd * value(w, i) : value(x, i); };
+        for (int p = lane; p < a.rot / 2; p += kWave) {
+            const PairCols col = pair_cols(a, p);
+            const float u = normed(col.a), v = normed(col.b);
+            float c, s;
+            cos_sin((uint64_t)a.positions[m] * turns_of(a.inv_freq[p]), c, s);
+            y[col.a] = rounded(__builtin_fmaf(u, c, -v * s));
+            y[col.b] = rounded(__builtin_fmaf(v, c, u * s));
+        }
+        for (int i = a.rot + lane; i < a.D; i += kWave) y[i] = rounded(normed(i));
+    }
+}
+
+// A workgroup's sums of dw lie in LDS, a row for each wave (heads of at most kQkAnyWidth values; wider ones have no norm here)
+constexpr int kQkAnyWidth = 1024;
+template <bool NORM>
+__global__ __launch_bounds__(kQkThreads) void qk_bwd_any_kernel(const QkArgs a) {
+    __shared__ float s_dw[NORM ? kQkWaves : 1][NORM ? 2 * kQkAnyWidth : 1];
+    __shared__ unsigned s_part[kQkWaves];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, heads = a.Hq + a.Hkv;
+    const int64_t waves = (int64_t)gridDim.x * kQkWaves;
+    unsigned mag = 0;
+    if constexpr (NORM) {
+        for (int i = lane; i < 2 * a.D; i += kWave) s_dw[wave][i] = 0.0f;      // (a lane's own columns: pairs and single values have one lane each)
+        __syncthreads();
+    }
+    for (int64_t at = (int64_t)blockIdx.x * kQkWaves + wave; at < a.M * heads; at += waves) {
+        const int64_t m = at / heads;
+        const int head = (int)(at - m * heads);
+        const u16* dy = head < a.Hq ? a.q + m * a.q_stride + (int64_t)head * a.D : a.k + m * a.k_stride + (int64_t)(head - a.Hq) * a.D;
+        const u16* x = a.x + m * a.x_stride + (int64_t)head * a.D;
+        const u16* w = head < a.Hq ? a.wq : a.wk;
+        u16* dx = a.dx + m * a.dx_stride + (int64_t)head * a.D;
+        const float rstd = NORM ? a.rstd[at] : 1.0f;
+        // f(column, gradient of the normed value) for the columns of this lane
+        auto each = [&](auto f) {
+            for (int p = lane; p < a.rot / 2; p += kWave) {
+                const PairCols col = pair_cols(a, p);
+                const float u = value(dy, col.a), v = value(dy, col.b);
+                float c, s;
+                cos_sin((uint64_t)a.positions[m] * turns_of(a.inv_freq[p]), c, s);
+                f(col.a, __builtin_fmaf(u, c, v * s));
+                f(col.b, __builtin_fmaf(v, c, -u * s));
+            }
+            for (int i = a.rot + lane; i < a.D; i += kWave) f(i, value(dy, i));
+        };
+        float mean = 0.0f;
+        if constexpr (NORM) {
+            float sum = 0.0f;
+            float* dw = s_dw[wave] + (head < a.Hq ? 0 : a.D);
+            each([&](int i, float g) {
+                const float n = value(x, i) * rstd;
+                dw[i] += g * n;
+                sum = __builtin_fmaf(g * value(w, i), n, sum);
+            });
+            mean = group_sum<kWave>(sum) / (float)a.D;
+        }
+        // (a pair's two gradients are read before either place is written, so dx may be dy)
+        auto out = [&](int i, float g) {
+            if constexpr (NORM) g = rstd * __builtin_fmaf(-value(x, i) * rstd, mean, g * value(w, i));
+            const u16 o = rounded(g);
+            mag = pk_max_mag(mag, o);
+            dx[i] = o;
+        };
+        each(out);
+        if (head == 0) move_v<1>(a, m, lane, kWave, mag);
+    }
+    if constexpr (NORM) {
+        __syncthreads();
+        if (a.dw_partial)
+            for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kQkWaves; ++w) sum += s_dw[w][i];
+                a.dw_partial[(int64_t)blockIdx.x * 2 * a.D + i] = sum;
+            }
+    }
+    if (a.amax_partial) {
+        mag = (mag & 0xFFFFu) > (mag >> 16) ? mag & 0xFFFFu : mag >> 16;
+        mag = block_max_u32<kQkThreads>(mag, s_part);
+        if (threadIdx.x == 0) a.amax_partial[blockIdx.x] = mag;
+    }
+}
+
+// The workgroups' sums in their order: a workgroup has 16 columns and 16 lanes to each, which take every 16th row and are added at the end; the
+// last workgroup finds the absmax.
+constexpr int kFinalCols = 16;
+__global__ __launch_bounds__(256) void qk_bwd_final_kernel(const float* dw_partial, const unsigned* amax_partial, int n, int D, float* dwq, float* dwk, int accumulate,
+                                                           float fmax, float* d_amax, float* d_scale) {
+    __shared__ float s_sum[16][kFinalCols + 1];
+    __shared__ unsigned s_part[4];
+    if (blockIdx.x == gridDim.x - 1) {
+        if (!amax_partial) return;
+        unsigned m = 0;
+        for (int i = threadIdx.x; i < n; i += 256) m = m > amax_partial[i] ? m : amax_partial[i];
+        m = block_max_u32<256>(m, s_part);
+        if (threadIdx.x == 0) {
+            const float amax = __uint_as_float(amax_bits_from_bf16_mag(m));
+            *d_amax = amax;
+            if (d_scale) *d_scale = scale_of_amax(amax, fmax);
+        }
+        return;
+    }
+    const int c = threadIdx.x % kFinalCols, r = threadIdx.x / kFinalCols, col = blockIdx.x * kFinalCols + c;
+    float sum = 0.0f;
+    if (col < 2 * D)
+        for (int i = r; i < n; i += 16) sum += dw_partial[(int64_t)i * 2 * D + col];
+    s_sum[r][c] = sum;
+    __syncthreads();
+    if (r == 0 && col < 2 * D) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) sum += s_sum[i][c];
+        float* out = col < D ? dwq : dwk;
+        if (out) {
+            const int i = col < D ? col : col - D;
+            out[i] = accumulate ? out[i] + sum : sum;
+        }
+    }
+}
+
+// ---- host side
+constexpr int kQkMaxBlocks = 1024;              // workgroups of the backward pass: rows of its workspace
+
+static bool aligned8(const void* p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0 && stride % 4 == 0; }
+
+// Lanes to a head of the vector kernels, or 0: pieces of four values have to be whole and to start at multiples of 8 bytes.
+static int lanes_of_head(int D, int rot) {
+    if (D % 8 != 0 || rot % 8 != 0 || D > 8 * kWave) return 0;
+    return D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64;
+}
+
+struct QkGrid { int blocks, split; };
+// A wave takes a token; where there are fewer than eight waves a CU that way, the heads of a token are shared out among 2, 4, ... of them, each of which finds the angles for itself.
+static QkGrid qk_grid(int64_t M, int passes, int cus, int most) {
+    int split = 1;
+    while (split < passes && M * split < 8 * (int64_t)cus) split *= 2;
+    const int64_t blocks = (M * split + kQkWaves - 1) / kQkWaves;
+    // (waves that share a token lie in one grid of a multiple of `split` waves)
+    int n = (int)(blocks < most ? blocks : most);
+    if (split > kQkWaves) { const int per = split / kQkWaves; n = (n + per - 1) / per * per; }
+    return {n, split};
+}
+
+static int launch_qk_fwd(QkArgs a, hipStream_t stream, int cus) {
+    const int G = lanes_of_head(a.D, a.rot);
+    const bool vec = G && aligned8(a.x, a.x_stride) && aligned8(a.q, a.q_stride) && aligned8(a.k, a.k_stride) && aligned8(a.wq, 0) && aligned8(a.wk, 0);
+    if (!vec) {
+        const int64_t blocks = (a.M * (a.Hq + a.Hkv) + kQkWaves - 1) / kQkWaves, most = (int64_t)cus * 32;
+        const dim3 grid((unsigned)(blocks < most ? blocks : most));
+        if (a.wq) hipLaunchKernelGGL(qk_fwd_any_kernel<true>, grid, dim3(kQkThreads), 0, stream, a);
+        else hipLaunchKernelGGL(qk_fwd_any_kernel<false>, grid, dim3(kQkThreads), 0, stream, a);
+    } else {
+        const QkGrid g = qk_grid(a.M, (a.Hq + a.Hkv + kWave / G - 1) / (kWave / G), cus, cus * 8);
+        a.split = g.split;
+        auto launch = [&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            if (a.wq) hipLaunchKernelGGL((qk_fwd_kernel<L, true>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
+            else hipLaunchKernelGGL((qk_fwd_kernel<L, false>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
+        };
+        if (G == 8) launch(std::integral_constant<int, 8>{});
+        else if (G == 16) launch(std::integral_constant<int, 16>{});
+        else if (G == 32) launch(std::integral_constant<int, 32>{});
+        else launch(std::integral_constant<int, 64>{});
+    }
+    return hipGetLastError() == hipSuccess ? LLMQ_OK : LLMQ_ERR_DEVICE;
+}
+
+struct QkFinal { float *dwq, *dwk; int accumulate, fmt; float *d_amax, *d_scale; };
+
+static int launch_qk_bwd(QkArgs a, const QkFinal& f, hipStream_t stream, int cus) {
+    const int G = lanes_of_head(a.D, a.rot);
+    const bool vec = G && aligned8(a.q, a.q_stride) && aligned8(a.k, a.k_stride) && aligned8(a.dx, a.dx_stride) && aligned8(a.dv, a.dv_stride) &&
+                     (!a.wq || (aligned8(a.x, a.x_stride) && aligned8(a.wq, 0) && aligned8(a.wk, 0)));
+    int blocks;
+    if (!vec) {
+        const int64_t wanted = (a.M * (a.Hq + a.Hkv) + kQkWaves - 1) / kQkWaves;
+        blocks = (int)(wanted < kQkMaxBlocks ? wanted : kQkMaxBlocks);
+        if (a.wq) hipLaunchKernelGGL(qk_bwd_any_kernel<true>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
+        else hipLaunchKernelGGL(qk_bwd_any_kernel<false>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
+    } else {
+        const QkGrid g = qk_grid(a.M, (a.Hq + a.Hkv + kWave / G - 1) / (kWave / G), cus, kQkMaxBlocks);
+        a.split = g.split;
+        blocks = g.blocks;
+        auto launch = [&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            if (a.wq) hipLaunchKernelGGL((qk_bwd_kernel<L, true>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
+            else hipLaunchKernelGGL((qk_bwd_kernel<L, false>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
+        };
+        if (G == 8) launch(std::integral_constant<int, 8>{});
+        else if (G == 16) launch(std::integral_constant<int, 16>{});
+        else if (G == 32) launch(std::integral_constant<int, 32>{});
+        else launch(std::integral_constant<int, 64>{});
+    }
+    if (a.dw_partial || a.amax_partial) {
+        const int cols = a.dw_partial ? (2 * a.D + kFinalCols - 1) / kFinalCols : 0;
+        hipLaunchKernelGGL(qk_bwd_final_kernel, dim3(cols + 1), dim3(256), 0, stream, a.dw_partial, a.amax_partial, blocks, a.D, f.dwq, f.dwk, f.accumulate, fp8_max(f.fmt), f.d_amax, f.d_scale);
+    }
+    return hipGetLastError() == hipSuccess ? LLMQ_OK : LLMQ_ERR_DEVICE;
+}
+
+}  // namespace llmq
+
+namespace {
+
+constexpr int64_t kMaxHeads = 1 << 16, kMaxHead = 1024;
+
+int check_qk(int64_t M, int64_t Hq, int64_t Hkv, int64_t D, int rot, int interleaved) {
+    if (!dim_ok(M) || Hq < 1 || Hq > kMaxHeads || Hkv < 1 || Hkv > kMaxHeads || D < 1 || D > kMaxHead || M * (Hq + 2 * Hkv) * D >= kMaxElems) return LLMQ_ERR_SHAPE;
+    if (rot < 0 || rot > D || rot % 2 != 0) return LLMQ_ERR_SHAPE;
+    if (interleaved != 0 && interleaved != 1) return LLMQ_ERR_FLAGS;
+    return LLMQ_OK;
+}
+// Rows of `width` elements, `stride` apart
+bool stride_ok(int64_t M, int64_t width, int64_t stride) { return (M == 1 || stride >= width) && stride >= 0 && stride < kMaxDim && M * stride < kMaxElems; }
+
+size_t qk_workspace(int64_t D) { return round256((size_t)llmq::kQkMaxBlocks * 2 * (size_t)D * sizeof(float)) + (size_t)llmq::kQkMaxBlocks * sizeof(unsigned); }
+
+}  // namespace
+
+extern "C" {
+
+int llmq_qk_norm_rope_fwd(const void* qkv_bf16, int64_t qkv_stride, int64_t M, int Hq, int Hkv, int D, const void* wq_bf16, const void* wk_bf16, float eps,
+                          const int64_t* d_positions, const double* d_inv_freq, int rot, int interleaved, void* q_bf16, int64_t q_stride, void* k_bf16,
+                          int64_t k_stride, float* rstd, void* stream) {
+    if (!qkv_bf16 || !q_bf16 || !k_bf16 || !wq_bf16 != !wk_bf16 || (rot > 0 && (!d_positions || !d_inv_freq))) return LLMQ_ERR_NULL;
+    const int st = check_qk(M, Hq, Hkv, D, rot, interleaved);
+    if (st != LLMQ_OK) return st;
+    if (!stride_ok(M, (int64_t)(Hq + 2 * Hkv) * D, qkv_stride) || !stride_ok(M, (int64_t)Hq * D, q_stride) || !stride_ok(M, (int64_t)Hkv * D, k_stride)) return LLMQ_ERR_SHAPE;
+    if (!aligned(qkv_bf16, 2) || !aligned(q_bf16, 2) || !aligned(k_bf16, 2) || !aligned(wq_bf16, 2) || !aligned(wk_bf16, 2) || !aligned(d_positions, 8) ||
+        !aligned(d_inv_freq, 8) || !aligned(rstd, 4))
+        return LLMQ_ERR_ALIGN;
+    typedef llmq::u16 u16;
+    llmq::QkArgs a{};
+    a.M = M, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.rot = rot, a.interleaved = interleaved;
+    a.x = static_cast<const u16*>(qkv_bf16), a.x_stride = qkv_stride;
+    a.wq = static_cast<const u16*>(wq_bf16), a.wk = static_cast<const u16*>(wk_bf16), a.eps = eps;
+    a.positions = d_positions, a.inv_freq = d_inv_freq, a.rstd = rstd;
+    a.q = static_cast<u16*>(q_bf16), a.q_stride = q_stride, a.k = static_cast<u16*>(k_bf16), a.k_stride = k_stride;
+    return llmq::launch_qk_fwd(a, static_cast<hipStream_t>(stream), num_cus());
+}
+
+size_t llmq_qk_norm_rope_workspace_bytes(int64_t M, int Hq, int Hkv, int D) {
+    return check_qk(M, Hq, Hkv, D, 0, 0) == LLMQ_OK ? qk_workspace(D) : 0;
+}
+
+int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk_bf16, int64_t dk_stride, const void* dv_bf16, int64_t dv_stride,
+                          const void* qkv_bf16, int64_t qkv_stride, int64_t M, int Hq, int Hkv, int D, const void* wq_bf16, const void* wk_bf16,
+                          const float* rstd, const int64_t* d_positions, const double* d_inv_freq, int rot, int interleaved, void* dqkv_bf16,
+                          int64_t dqkv_stride, float* dwq, float* dwk, int accumulate, int fmt, float* d_amax, float* d_scale, void* ws, size_t ws_bytes,
+                          void* stream) {
+    if (!dq_bf16 || !dk_bf16 || !dqkv_bf16 || !wq_bf16 != !wk_bf16 || (rot > 0 && (!d_positions || !d_inv_freq)) || (d_scale && !d_amax)) return LLMQ_ERR_NULL;
+    const bool norm = wq_bf16 != nullptr, sums = norm && (dwq || dwk);
+    if (norm && (!qkv_bf16 || !rstd)) return LLMQ_ERR_NULL;
+    if ((sums || d_amax) && !ws) return LLMQ_ERR_NULL;
+    const int st = check_qk(M, Hq, Hkv, D, rot, interleaved);
+    if (st != LLMQ_OK) return st;
+    if (!stride_ok(M, (int64_t)(Hq + 2 * Hkv) * D, dqkv_stride) || !stride_ok(M, (int64_t)Hq * D, dq_stride) || !stride_ok(M, (int64_t)Hkv * D, dk_stride) ||
+        (dv_bf16 && !stride_ok(M, (int64_t)Hkv * D, dv_stride)) || (norm && !stride_ok(M, (int64_t)(Hq + 2 * Hkv) * D, qkv_stride)))
+        return LLMQ_ERR_SHAPE;
+    if (d_amax && !fmt_ok(fmt)) return LLMQ_ERR_FORMAT;
+    if (!aligned(dq_bf16, 2) || !aligned(dk_bf16, 2) || !aligned(dv_bf16, 2) || !aligned(qkv_bf16, 2) || !aligned(wq_bf16, 2) || !aligned(wk_bf16, 2) || !aligned(rstd, 4) ||
+        !aligned(d_positions, 8) || !aligned(d_inv_freq, 8) || !aligned(dqkv_bf16, 2) || !aligned(dwq, 4) || !aligned(dwk, 4) || !aligned(d_amax, 4) || !aligned(d_scale, 4) || !aligned(ws, 16))
+        return LLMQ_ERR_ALIGN;
+    if ((sums || d_amax) && ws_bytes < qk_workspace(D)) return LLMQ_ERR_WORKSPACE;
+    typedef llmq::u16 u16;
+    llmq::QkArgs a{};
+    a.M = M, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.rot = rot, a.interleaved = interleaved;
+    a.x = static_cast<const u16*>(qkv_bf16), a.x_stride = qkv_stride;
+    a.wq = static_cast<const u16*>(wq_bf16), a.wk = static_cast<const u16*>(wk_bf16);
+    a.positions = d_positions, a.inv_freq = d_inv_freq, a.rstd = const_cast<float*>(rstd);
+    a.q = static_cast<u16*>(const_cast<void*>(dq_bf16)), a.q_stride = dq_stride, a.k = static_cast<u16*>(const_cast<void*>(dk_bf16)), a.k_stride = dk_stride;
+    a.dv = static_cast<const u16*>(dv_bf16), a.dv_stride = dv_stride;
+    a.dx = static_cast<u16*>(dqkv_bf16), a.dx_stride = dqkv_stride;
+    a.dw_partial = sums ? static_cast<float*>(ws) : nullptr;
+    a.amax_partial = d_amax ? reinterpret_cast<unsigned*>(static_cast<uint8_t*>(ws) + round256((size_t)llmq::kQkMaxBlocks * 2 * (size_t)D * sizeof(float))) : nullptr;
+    return llmq::launch_qk_bwd(a, llmq::QkFinal{dwq, dwk, accumulate != 0, d_amax ? fmt : 0, d_amax, d_scale}, static_cast<hipStream_t>(stream), num_cus());
+}
+
+}  // extern "C"

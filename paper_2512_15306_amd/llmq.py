@@ -36,6 +36,7 @@ EXPORTS = ["llmq_status_string", "llmq_version", "llmq_amax_workspace_bytes", "l
            "llmq_scale_from_amax", "llmq_swiglu_workspace_bytes", "llmq_swiglu_fwd", "llmq_swiglu_fwd_fp8", "llmq_swiglu_fwd_fp8_slabs",
            "llmq_swiglu_bwd", "llmq_rmsnorm_workspace_bytes", "llmq_rmsnorm_fwd", "llmq_rmsnorm_apply_fp8", "llmq_rmsnorm_apply_fp8_slabs",
            "llmq_block_scales_bytes", "llmq_quantize_fp8_blocks", "llmq_fp8_gemm_blocks",
+           "llmq_qk_norm_rope_fwd", "llmq_qk_norm_rope_workspace_bytes", "llmq_qk_norm_rope_bwd",
            "llmq_calibrate_mfma", "llmq_calibrate_copy", "llmq_calibrate_gemm_phases_bytes", "llmq_calibrate_gemm_phases"]
 
 
@@ -120,6 +121,12 @@ def lib() -> ctypes.CDLL:
     L.llmq_quantize_fp8_blocks.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp, vp, vp]
     L.llmq_fp8_gemm_blocks.restype = i32
     L.llmq_fp8_gemm_blocks.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, vp]
+    L.llmq_qk_norm_rope_fwd.restype = i32
+    L.llmq_qk_norm_rope_fwd.argtypes = [vp, i64, i64, i32, i32, i32, vp, vp, c.c_float, vp, vp, i32, i32, vp, i64, vp, i64, vp, vp]
+    L.llmq_qk_norm_rope_workspace_bytes.restype = sz
+    L.llmq_qk_norm_rope_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    L.llmq_qk_norm_rope_bwd.restype = i32
+    L.llmq_qk_norm_rope_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, vp, i64, vp, vp, i32, i32, vp, vp, vp, sz, vp]
     L.llmq_calibrate_mfma.restype = i32
     L.llmq_calibrate_mfma.argtypes = [i32, i32, i32, i32, vp, c.POINTER(c.c_double), vp]
     L.llmq_calibrate_gemm_phases_bytes.restype = sz
@@ -535,6 +542,68 @@ def llmq_fp8_gemm_blocks(A: torch.Tensor, sA: torch.Tensor, fmtA: int, B: torch.
                                       _here(B, torch.uint8, "B"), _here(sB, torch.uint8, "sB", llmq_block_scales_bytes(C, T)), fmtB, R, C, T,
                                       _here(c, torch.bfloat16, "c"), int(bool(accumulate)), _here(d_amax_c, torch.float32, "d_amax_c", 1), _stream()),
            "llmq_fp8_gemm_blocks")
+
+
+def _rows(t: Optional[torch.Tensor], M: int, width: int, name: str) -> Tuple[Optional[int], int]:
+    """Pointer and row stride of a BF16 matrix [M, width] on the current device, whose rows may lie apart."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+    if t.dtype != torch.bfloat16:
+        raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, t.dtype))
+    if tuple(t.shape) != (M, width):
+        raise ValueError("%s must be [%d, %d], got %s" % (name, M, width, tuple(t.shape)))
+    if (width > 1 and t.stride(1) != 1) or (M > 1 and t.stride(0) < width):
+        raise ValueError("%s must have rows of consecutive elements that do not overlap, got strides %s" % (name, t.stride()))
+    return t.data_ptr(), t.stride(0) if M > 1 else width
+
+
+def _qk_norm(wq, wk, D: int):
+    if (wq is None) != (wk is None):
+        raise ValueError("wq and wk go together")
+    return _here(wq, torch.bfloat16, "wq", D), _here(wk, torch.bfloat16, "wk", D)
+
+
+def llmq_qk_norm_rope_fwd(qkv: torch.Tensor, Hq: int, Hkv: int, D: int, wq: Optional[torch.Tensor], wk: Optional[torch.Tensor], eps: float,
+                          positions: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], interleaved: bool, q: torch.Tensor, k: torch.Tensor,
+                          rstd: Optional[torch.Tensor] = None) -> None:
+    """inv_freq: float64 [rot / 2], the pairs that are turned (None: none); positions: int64 [M]."""
+    status = _fast.qk_norm_rope_fwd(qkv, Hq, Hkv, D, wq, wk, eps, positions, inv_freq, interleaved, q, k, rstd)
+    if status is not None:
+        return _check(status, "llmq_qk_norm_rope_fwd") if status else None
+    M = _matrix(qkv, "qkv")[0]
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    (x, xs), (qp, qs), (kp, ks) = _rows(qkv, M, (Hq + 2 * Hkv) * D, "qkv"), _rows(q, M, Hq * D, "q"), _rows(k, M, Hkv * D, "k")
+    pq, pk = _qk_norm(wq, wk, D)
+    _check(lib().llmq_qk_norm_rope_fwd(x, xs, M, Hq, Hkv, D, pq, pk, float(eps), _here(positions, torch.int64, "positions", M if rot else None), _here(inv_freq, torch.float64, "inv_freq"),
+                                       rot, int(bool(interleaved)), qp, qs, kp, ks, _here(rstd, torch.float32, "rstd", M * (Hq + Hkv)), _stream()), "llmq_qk_norm_rope_fwd")
+
+
+def llmq_qk_norm_rope_workspace_bytes(M: int, Hq: int, Hkv: int, D: int) -> int:
+    return int(lib().llmq_qk_norm_rope_workspace_bytes(M, Hq, Hkv, D))
+
+
+def llmq_qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, dv: Optional[torch.Tensor], qkv: Optional[torch.Tensor], Hq: int, Hkv: int, D: int,
+                          wq: Optional[torch.Tensor], wk: Optional[torch.Tensor], rstd: Optional[torch.Tensor], positions: Optional[torch.Tensor],
+                          inv_freq: Optional[torch.Tensor], interleaved: bool, dqkv: torch.Tensor, dwq: Optional[torch.Tensor], dwk: Optional[torch.Tensor],
+                          accumulate: bool, fmt: int, d_amax: Optional[torch.Tensor], d_scale: Optional[torch.Tensor], ws: Optional[torch.Tensor]) -> None:
+    """dv None: the V columns of dqkv already hold its gradient."""
+    status = _fast.qk_norm_rope_bwd(dq, dk, dv, qkv, Hq, Hkv, D, wq, wk, rstd, positions, inv_freq, interleaved, dqkv, dwq, dwk, accumulate, fmt, d_amax, d_scale, ws)
+    if status is not None:
+        return _check(status, "llmq_qk_norm_rope_bwd") if status else None
+    M = _matrix(dqkv, "dqkv")[0]
+    rot, width = 0 if inv_freq is None else 2 * inv_freq.numel(), (Hq + 2 * Hkv) * D
+    (qp, qs), (kp, ks), (vp, vs) = _rows(dq, M, Hq * D, "dq"), _rows(dk, M, Hkv * D, "dk"), _rows(dv, M, Hkv * D, "dv")
+    (x, xs), (dx, dxs) = _rows(qkv, M, width, "qkv"), _rows(dqkv, M, width, "dqkv")
+    pq, pk = _qk_norm(wq, wk, D)
+    _check(lib().llmq_qk_norm_rope_bwd(qp, qs, kp, ks, vp, vs, x, xs, M, Hq, Hkv, D, pq, pk, _here(rstd, torch.float32, "rstd", M * (Hq + Hkv)),
+                                       _here(positions, torch.int64, "positions", M if rot else None), _here(inv_freq, torch.float64, "inv_freq"), rot, int(bool(interleaved)), dx, dxs,
+                                       _here(dwq, torch.float32, "dwq", D), _here(dwk, torch.float32, "dwk", D), int(bool(accumulate)), fmt, _here(d_amax, torch.float32, "d_amax", 1),
+                                       _here(d_scale, torch.float32, "d_scale", 1), _here(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(), _stream()),
+           "llmq_qk_norm_rope_bwd")
 
 
 def llmq_calibrate_mfma(fmtA: int, fmtB: int, random_bits: bool, iters: int, d_sink: torch.Tensor) -> float:
