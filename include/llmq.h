@@ -49,7 +49,8 @@ typedef enum {
     LLMQ_ERR_FORMAT = -4,     /* not an llmq_fp8_format */
     LLMQ_ERR_WORKSPACE = -5,  /* workspace missing or smaller than llmq_fp8_linear_workspace_bytes() */
     LLMQ_ERR_DEVICE = -6,     /* the HIP runtime reported an error at launch */
-    LLMQ_ERR_FLAGS = -7       /* unknown bits in `flags` */
+    LLMQ_ERR_FLAGS = -7,      /* unknown bits in `flags` */
+    LLMQ_ERR_VALUE = -8       /* a number is out of range */
 } llmq_status;
 
 /* OCP 8-bit floating point formats (Section 2): E4M3 has bias 7 and max 448 (no Inf, NaN = S.1111.111),
@@ -455,6 +456,58 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
                           int interleaved, void* dqkv_bf16, int64_t dqkv_stride, float* dwq, float* dwk,
                           int accumulate, int fmt, float* d_amax, float* d_scale, void* ws, size_t ws_bytes,
                           void* stream);
+
+/*
+ * One AdamW step over any number of tensors in one launch, from the gradients the calls above leave (BF16 weight gradients, binary32 gradients of norm weights) to the
+ * weights they read.
+ *
+ *   g' = g s                        s = *d_grad_scale (a clipping factor, say), 1 if it is NULL; where it is not finite the whole step is skipped and nothing is written
+ *   m' = m b1 + g' (1 - b1)         v' = v b2 + g'^2 (1 - b2)
+ *   w' = (w - w lr weight_decay) - (m' / (sqrt(v') / sqrt(1 - b2^step) + eps)) (lr / (1 - b1^step))        LLMQ_ADAMW_NO_DECAY: without the decay
+ *   in binary32, each operation rounded by itself; the factors made of b1, b2, lr and step in binary64 and rounded once.
+ *
+ * llmq_adamw_tensor, all pointers device memory, each array of n elements, 16-byte aligned (the scales: any):
+ *   w_bf16, w_f32   the weights: BF16 alone;  binary32 alone;  or both: w_f32 is the master copy, which is stepped, and w_bf16 receives it rounded to nearest
+ *                   even.  BF16 alone is rounded to nearest even, or with LLMQ_ADAMW_STOCHASTIC up or down with the probability that keeps the mean.
+ *   grad            BF16, or binary32 with LLMQ_ADAMW_GRAD_F32.
+ *   m, v            binary32, zeros before the first step.  LLMQ_ADAMW_STATES_8BIT: one byte each, E4M3 codes of m and of sqrt(v) with m_scale and v_scale [ceil(n / 128)], a
+ *                   power-of-two scale for each 128 elements as llmq_quantize_fp8_blocks has them; codes 0 and scales 127 before the first step.  Codes are rounded up or
+ *                   down with the probability that keeps the mean (below 2^-6 to the nearest; a root above 0 stays above 0), for beta2 > 31/32 the mean of the root's square, without
+ *                   which v would grow by its rounding; up to 31/32 that growth is at most 4 % of v.  A gradient that is not finite makes
+ *                   its whole block NaN.
+ *   d_amax          [1] float or NULL: absmax of the new w_bf16 (canonical NaN as llmq_amax), of all tensors that name the same word: the next quantization of these
+ *                   weights then needs no pass of its own (llmq_scale_from_amax).
+ *   first_counter   number of the tensor's first element among all that are rounded at random (>= 0): element i takes its bits from first_counter + i, the seed and the step.
+ *                   Tensors should not share numbers.  Same inputs, same bytes.
+ *
+ * llmq_adamw_plan (host code): checks `count` tensors and writes the table that a step reads into `plan`, llmq_adamw_plan_bytes bytes of HOST memory, which the caller copies to
+ *   device memory (16-byte aligned) once; info [4]: host words that llmq_adamw_step takes back.  The plan holds as long as the pointers do.
+ * llmq_adamw_hyper (host code): the numbers of a step (1, 2, ...) as LLMQ_ADAMW_HYPER_WORDS 32-bit words.  0 <= beta < 1, lr and weight_decay >= 0, eps > 0 in binary32, else
+ *   LLMQ_ERR_VALUE.
+ * llmq_adamw_step: exactly one of hyper (HOST words, read during the call) and d_hyper (the same words in device memory, read when the step runs: a captured step takes new ones with
+ *   every replay) is given.
+ */
+#define LLMQ_ADAMW_GRAD_F32    1
+#define LLMQ_ADAMW_STATES_8BIT 2
+#define LLMQ_ADAMW_NO_DECAY    4
+#define LLMQ_ADAMW_STOCHASTIC  8
+#define LLMQ_ADAMW_HYPER_WORDS 10
+typedef struct llmq_adamw_tensor {
+    void* w_bf16;
+    float* w_f32;
+    const void* grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    float* d_amax;
+    int64_t n, first_counter;
+    int flags;
+} llmq_adamw_tensor;
+size_t llmq_adamw_plan_bytes(const llmq_adamw_tensor* tensors, int64_t count);
+int llmq_adamw_plan(const llmq_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes, int64_t info[4]);
+int llmq_adamw_hyper(int64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
+                     uint64_t seed, uint32_t hyper[LLMQ_ADAMW_HYPER_WORDS]);
+int llmq_adamw_step(const void* d_plan, const int64_t info[4], const uint32_t* hyper, const void* d_hyper,
+                    const float* d_grad_scale, void* stream);
 
 /*
  * Peak calibration (the paper's appendix "A note on MFU" measures the attainable peak with a large-matmul

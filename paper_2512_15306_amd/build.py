@@ -26,7 +26,7 @@ TILE_SOURCES += ["gemm_edge_%s.hip" % kind for kind in
                   "e4m3_e4m3_bt", "e5m2_e4m3_bt", "e4m3_e4m3_abt", "e5m2_e4m3_abt")]
 # and for operands with block scales
 TILE_SOURCES += ["gemm_blocks_%s.hip" % kind for kind in ("e4m3_e4m3", "e5m2_e4m3", "e4m3_e5m2", "e5m2_e5m2")]
-SOURCES = TILE_SOURCES + ["gemm.hip", "gemm_blocks.hip", "gemm_tmajor.hip", "quantize_blocks.hip", "api.hip", "amax.hip", "quantize.hip", "swiglu.hip", "rmsnorm.hip", "qk_norm_rope.hip", "calibrate.hip"]
+SOURCES = TILE_SOURCES + ["gemm.hip", "gemm_blocks.hip", "gemm_tmajor.hip", "quantize_blocks.hip", "api.hip", "amax.hip", "quantize.hip", "swiglu.hip", "rmsnorm.hip", "qk_norm_rope.hip", "adamw.hip", "calibrate.hip"]
 # Sources that hold tile kernels (see check_accumulator_reads).
 CHECKED_SOURCES = set(TILE_SOURCES) | {"gemm.hip"}
 # packed-fp32 VALU ops are disabled on purpose (they have produced silent wrong results on this

@@ -420,11 +420,34 @@ LLMQ_BINDING(qk_norm_rope_bwd) {
     });
 }
 
+LLMQ_BINDING(adamw_step) {
+    return run(args, n, 4, [](Args& args_) {
+        HereArgs a(args_);
+        // (the plan's words and the numbers of the step, unless those are on the device, are read during the call)
+        auto words = [&](int i, at::ScalarType type, int64_t numel) -> const at::Tensor* {
+            if (!THPVariable_CheckExact(a.a[i])) { a.ok = false; return nullptr; }
+            const at::Tensor& t = THPVariable_Unpack(a.a[i]);
+            if (t.layout() != at::kStrided || t.scalar_type() != type || t.numel() != numel || !t.is_contiguous() || !(t.is_cpu() || t.is_cuda())) { a.ok = false; return nullptr; }
+            return &t;
+        };
+        void* table = a.pointer(0, kU8, -1, true);
+        const at::Tensor *info = words(1, at::kLong, 4), *hyper = words(2, at::kInt, LLMQ_ADAMW_HYPER_WORDS);
+        if (info && !info->is_cpu()) a.ok = false;
+        if (hyper && hyper->is_cuda() && hyper->device().index() != a.device) a.ok = false;
+        const bool on_device = hyper && hyper->is_cuda();
+        const int64_t* i = a.ok ? static_cast<const int64_t*>(info->data_ptr()) : nullptr;
+        const void* h = a.ok ? hyper->data_ptr() : nullptr;
+        float* scale = static_cast<float*>(a.pointer(3, kF32, 1, false));
+        args_.ok = a.ok;
+        return [=](void* s) { return llmq_adamw_step(table, i, on_device ? nullptr : static_cast<const uint32_t*>(h), on_device ? h : nullptr, scale, s); };
+    });
+}
+
 #define LLMQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {LLMQ_METHOD(linear_fwd), LLMQ_METHOD(linear_dgrad), LLMQ_METHOD(linear_wgrad), LLMQ_METHOD(amax), LLMQ_METHOD(quantize_fp8),
                            LLMQ_METHOD(quantize_fp8_slabs), LLMQ_METHOD(bf16_gemm_tn), LLMQ_METHOD(swiglu_fwd), LLMQ_METHOD(swiglu_fwd_fp8),
                            LLMQ_METHOD(swiglu_fwd_fp8_slabs), LLMQ_METHOD(swiglu_bwd), LLMQ_METHOD(rmsnorm_fwd), LLMQ_METHOD(rmsnorm_apply_fp8),
-                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), {nullptr, nullptr, 0, nullptr}};
+                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), LLMQ_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -8,7 +8,7 @@ from __future__ import annotations
 import ctypes
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch  # imported first on purpose: the library then binds to the HIP runtime PyTorch loaded
 
@@ -23,6 +23,7 @@ JIT_DY = 32
 NO_TRANSPOSE = 64
 SHARE_TILES = 128
 SLAB_COPIES = 256
+ADAMW_GRAD_F32, ADAMW_STATES_8BIT, ADAMW_NO_DECAY, ADAMW_STOCHASTIC, ADAMW_HYPER_WORDS = 1, 2, 4, 8, 10
 LAYOUT_ROWS, LAYOUT_T_MAJOR, LAYOUT_SLABS = 0, 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -37,6 +38,7 @@ EXPORTS = ["llmq_status_string", "llmq_version", "llmq_amax_workspace_bytes", "l
            "llmq_swiglu_bwd", "llmq_rmsnorm_workspace_bytes", "llmq_rmsnorm_fwd", "llmq_rmsnorm_apply_fp8", "llmq_rmsnorm_apply_fp8_slabs",
            "llmq_block_scales_bytes", "llmq_quantize_fp8_blocks", "llmq_fp8_gemm_blocks",
            "llmq_qk_norm_rope_fwd", "llmq_qk_norm_rope_workspace_bytes", "llmq_qk_norm_rope_bwd",
+           "llmq_adamw_plan_bytes", "llmq_adamw_plan", "llmq_adamw_hyper", "llmq_adamw_step",
            "llmq_calibrate_mfma", "llmq_calibrate_copy", "llmq_calibrate_gemm_phases_bytes", "llmq_calibrate_gemm_phases"]
 
 
@@ -44,6 +46,12 @@ class LlmqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
         super().__init__("%s failed: %d (%s)" % (where, status, status_string(status)))
+
+
+class _AdamWTensor(ctypes.Structure):
+    """llmq_adamw_tensor"""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("w_bf16", "w_f32", "grad", "m", "v", "m_scale", "v_scale", "d_amax")] + \
+               [("n", ctypes.c_int64), ("first_counter", ctypes.c_int64), ("flags", ctypes.c_int)]
 
 
 def lib() -> ctypes.CDLL:
@@ -127,6 +135,15 @@ def lib() -> ctypes.CDLL:
     L.llmq_qk_norm_rope_workspace_bytes.argtypes = [i64, i32, i32, i32]
     L.llmq_qk_norm_rope_bwd.restype = i32
     L.llmq_qk_norm_rope_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, vp, i64, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+    f64 = c.c_double
+    L.llmq_adamw_plan_bytes.restype = sz
+    L.llmq_adamw_plan_bytes.argtypes = [c.POINTER(_AdamWTensor), i64]
+    L.llmq_adamw_plan.restype = i32
+    L.llmq_adamw_plan.argtypes = [c.POINTER(_AdamWTensor), i64, vp, sz, vp]
+    L.llmq_adamw_hyper.restype = i32
+    L.llmq_adamw_hyper.argtypes = [i64, f64, f64, f64, f64, f64, c.c_uint64, vp]
+    L.llmq_adamw_step.restype = i32
+    L.llmq_adamw_step.argtypes = [vp, vp, vp, vp, vp, vp]
     L.llmq_calibrate_mfma.restype = i32
     L.llmq_calibrate_mfma.argtypes = [i32, i32, i32, i32, vp, c.POINTER(c.c_double), vp]
     L.llmq_calibrate_gemm_phases_bytes.restype = sz
@@ -604,6 +621,73 @@ def llmq_qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, dv: Optional[torch
                                        _here(dwq, torch.float32, "dwq", D), _here(dwk, torch.float32, "dwk", D), int(bool(accumulate)), fmt, _here(d_amax, torch.float32, "d_amax", 1),
                                        _here(d_scale, torch.float32, "d_scale", 1), _here(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(), _stream()),
            "llmq_qk_norm_rope_bwd")
+
+
+class AdamWTensor(NamedTuple):
+    """One tensor of an AdamW step.  w: BF16, master: float32, one of them or both; grad BF16 or float32; m and v float32, or uint8 with m_scale and v_scale
+    (uint8, one for each 128 elements); decay: whether the weight decay applies; stochastic: how BF16 weights without a master copy are rounded; amax: float32 [1]."""
+    w: Optional[torch.Tensor]
+    master: Optional[torch.Tensor]
+    grad: torch.Tensor
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    first_counter: int = 0
+    decay: bool = True
+    stochastic: bool = False
+    amax: Optional[torch.Tensor] = None
+
+
+class AdamWPlan(NamedTuple):
+    """What llmq_adamw_step reads: the table on the device, the words that belong to it, and the tensors it points at."""
+    table: torch.Tensor
+    info: torch.Tensor
+    tensors: Tuple[AdamWTensor, ...]
+
+
+def llmq_adamw_plan(tensors: Sequence[AdamWTensor]) -> AdamWPlan:
+    """The plan of a step over `tensors`, in memory of its own on the current device."""
+    entries = (_AdamWTensor * max(len(tensors), 1))()
+    for e, t in zip(entries, tensors):
+        first = t.w if t.w is not None else t.master
+        if first is None:
+            raise ValueError("a tensor needs w or master")
+        n, codes = first.numel(), t.m.dtype == torch.uint8
+        state, scales = torch.uint8 if codes else torch.float32, (n + 127) // 128
+        if t.grad.dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError("grad must be bfloat16 or float32, got %s" % t.grad.dtype)
+        if not codes and (t.m_scale is not None or t.v_scale is not None):
+            raise ValueError("m_scale and v_scale belong to 8-bit moments")
+        e.w_bf16, e.w_f32 = _here(t.w, torch.bfloat16, "w", n), _here(t.master, torch.float32, "master", n)
+        e.grad, e.m, e.v = _here(t.grad, None, "grad", n), _here(t.m, state, "m", n), _here(t.v, state, "v", n)
+        e.m_scale, e.v_scale = _here(t.m_scale, torch.uint8, "m_scale", scales), _here(t.v_scale, torch.uint8, "v_scale", scales)
+        e.d_amax, e.n, e.first_counter = _here(t.amax, torch.float32, "amax", 1), n, t.first_counter
+        e.flags = (ADAMW_GRAD_F32 if t.grad.dtype == torch.float32 else 0) | (ADAMW_STATES_8BIT if codes else 0) | (0 if t.decay else ADAMW_NO_DECAY) | (ADAMW_STOCHASTIC if t.stochastic else 0)
+    nbytes = int(lib().llmq_adamw_plan_bytes(entries, len(tensors)))
+    table, info = torch.empty(max(nbytes, 1), dtype=torch.uint8), torch.zeros(4, dtype=torch.int64)
+    _check(lib().llmq_adamw_plan(entries, len(tensors), table.data_ptr(), nbytes, info.data_ptr()), "llmq_adamw_plan")
+    return AdamWPlan(table.to("cuda:%d" % torch.cuda.current_device()), info, tuple(tensors))
+
+
+def llmq_adamw_hyper(step: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, seed: int = 0) -> torch.Tensor:
+    """The numbers of a step as an int32 tensor in host memory; copied to the device it serves captured steps."""
+    words = torch.empty(ADAMW_HYPER_WORDS, dtype=torch.int32)
+    _check(lib().llmq_adamw_hyper(step, lr, beta1, beta2, eps, weight_decay, seed, words.data_ptr()), "llmq_adamw_hyper")
+    return words
+
+
+def llmq_adamw_step(plan: AdamWPlan, hyper: torch.Tensor, grad_scale: Optional[torch.Tensor] = None) -> None:
+    """hyper: what llmq_adamw_hyper returned, on the host (read now) or on the device (read when the step runs)."""
+    status = _fast.adamw_step(plan.table, plan.info, hyper, grad_scale)
+    if status is not None:
+        return _check(status, "llmq_adamw_step") if status else None
+    if hyper.dtype != torch.int32 or hyper.numel() != ADAMW_HYPER_WORDS or not hyper.is_contiguous():
+        raise ValueError("hyper must be %d int32 words" % ADAMW_HYPER_WORDS)
+    on_device = hyper.is_cuda
+    words = _here(hyper, torch.int32, "hyper") if on_device else hyper.data_ptr()
+    _check(lib().llmq_adamw_step(_here(plan.table, torch.uint8, "plan"), plan.info.data_ptr(), None if on_device else words, words if on_device else None,
+                                 _here(grad_scale, torch.float32, "grad_scale", 1), _stream()), "llmq_adamw_step")
 
 
 def llmq_calibrate_mfma(fmtA: int, fmtB: int, random_bits: bool, iters: int, d_sink: torch.Tensor) -> float:
