@@ -39,10 +39,10 @@ struct QkArgs {
 // A frequency in radians as a 64-bit fraction of a turn per position (whole turns do not matter)
 __device__ inline uint64_t turns_of(double inv_freq) {
     double t = inv_freq * 0.15915494309189533577;            // 1 / (2 pi)
-    t -= __builtin_floor(t);                                 // [0, 1]
-    const double hi = __builtin_floor(t * 4294967296.0);
-    const double lo = (t * 4294967296.0 - hi) * 4294967296.0;
-    return ((uint64_t)hi << 32) + (uint64_t)lo;              // (a whole turn wraps to none)
+    t -= __builtin_floor(t);
+    t = t < 1.0 ? t * 4294967296.0 : 0.0;                    // (the difference may round to a whole turn)
+    const unsigned hi = (unsigned)t, lo = (unsigned)((t - (double)hi) * 4294967296.0);
+    return ((uint64_t)hi << 32) | lo;
 }
 
 // Cosine and sine of a fraction of a turn: to the nearest quarter, the rest (at most pi/4) by the Taylor series, whose first missing terms are
@@ -73,6 +73,13 @@ __device__ inline float group_sum(float v) {
     return v;
 }
 
+// 1 / sqrt(x): the hardware's, to within a unit in the last place, and a Newton step
+__device__ inline float inverse_root(float x) {
+    const float y = __builtin_amdgcn_rsqf(x);
+    const float e = __builtin_fmaf(-x * y, y, 1.0f);
+    return e == e ? __builtin_fmaf(0.5f * y, e, y) : y;      // (0 and infinity: y is infinity and 0)
+}
+
 // Eight values of a head: two pieces of four
 struct Eight { v2u lo, hi; };
 __device__ inline void unpack(const Eight& e, float (&f)[8]) {
@@ -92,41 +99,43 @@ __device__ inline Eight pack(const float (&f)[8]) {
 }
 
 // The lane's place among the G lanes of a head: its two pieces' columns and its angles' frequencies
-template <int G>
+template <int G, bool NEIGHBOURS>
 struct Place {
     int l, sub;                                  // lane of the head; head among those of a pass
     bool there, turned;
-    int lo, hi;
+    int lo, hi;                                  // first columns of the pieces
+    unsigned off_lo, off_hi;                     // their places behind the first head of a pass
     uint64_t f[4];
     __device__ Place(const QkArgs& a) {
         const int lane = threadIdx.x & (kWave - 1);
         l = lane % G, sub = lane / G;
         there = 8 * l < a.D;
         turned = 8 * l < a.rot;
-        lo = turned && !a.interleaved ? 4 * l : 8 * l;       // (the values behind the turned ones start at a multiple of 8 as well)
-        hi = turned && !a.interleaved ? 4 * l + a.rot / 2 : 8 * l + 4;
+        lo = turned && !NEIGHBOURS ? 4 * l : 8 * l;       // (the values behind the turned ones start at a multiple of 8 as well)
+        hi = turned && !NEIGHBOURS ? 4 * l + a.rot / 2 : 8 * l + 4;
+        off_lo = (unsigned)(sub * a.D + lo), off_hi = (unsigned)(sub * a.D + hi);
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[j] = turned ? turns_of(a.inv_freq[4 * l + j]) : 0;
     }
-    __device__ Eight load(const u16* p) const { return Eight{*reinterpret_cast<const v2u*>(p + lo), *reinterpret_cast<const v2u*>(p + hi)}; }
+    __device__ Eight weights(const u16* p) const { return Eight{*reinterpret_cast<const v2u*>(p + lo), *reinterpret_cast<const v2u*>(p + hi)}; }
+    // p: the first head of the pass (the same for the whole wave)
+    __device__ Eight load(const u16* p) const {
+        return Eight{__builtin_nontemporal_load(reinterpret_cast<const v2u*>(p + off_lo)), __builtin_nontemporal_load(reinterpret_cast<const v2u*>(p + off_hi))};
+    }
     __device__ void store(u16* p, const Eight& e) const {
-        *reinterpret_cast<v2u*>(p + lo) = e.lo;
-        *reinterpret_cast<v2u*>(p + hi) = e.hi;
+        *reinterpret_cast<v2u*>(p + off_lo) = e.lo;
+        *reinterpret_cast<v2u*>(p + off_hi) = e.hi;
     }
     // SIGN 1: by the angles, -1: back
     template <int SIGN>
-    __device__ void turn(const float (&c)[4], const float (&s)[4], bool interleaved, float (&v)[8]) const {
-        auto pair = [&](float& a, float& b, float cc, float ss) {
-            const float x = a, y = b;
-            a = __builtin_fmaf(x, cc, SIGN > 0 ? -y * ss : y * ss);
-            b = __builtin_fmaf(y, cc, SIGN > 0 ? x * ss : -x * ss);
-        };
-        if (interleaved) {
+    __device__ void turn(const float (&c)[4], const float (&s)[4], float (&v)[8]) const {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) pair(v[2 * j], v[2 * j + 1], c[j], s[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) pair(v[j], v[4 + j], c[j], s[j]);
+        for (int j = 0; j < 4; ++j) {
+            constexpr int kStep = NEIGHBOURS ? 1 : 4;
+            const int i = NEIGHBOURS ? 2 * j : j;
+            const float x = v[i], y = v[i + kStep];
+            v[i] = __builtin_fmaf(x, c[j], SIGN > 0 ? -y * s[j] : y * s[j]);
+            v[i + kStep] = __builtin_fmaf(y, c[j], SIGN > 0 ? x * s[j] : -x * s[j]);
         }
     }
     __device__ void angles(int64_t position, float (&c)[4], float (&s)[4]) const {
@@ -137,50 +146,87 @@ struct Place {
 
 constexpr int kQkThreads = 256, kQkWaves = kQkThreads / kWave, kQkAtOnce = 4;
 
-template <int G, bool NORM>
+// The passes of a wave over the heads of a token: first all of the queries, then all of the keys, so that a pass has one weight and one base address.
+// each(f): f(tag, first, last, head0) for the wave's share of the queries' passes, then of the keys'; tag::value: whether they are queries.
+template <int G>
+struct Passes {
+    static constexpr int kHeads = kWave / G;
+    int queries, first, last;
+    __device__ Passes(const QkArgs& a, int part) {
+        queries = (a.Hq + kHeads - 1) / kHeads;
+        const int all = queries + (a.Hkv + kHeads - 1) / kHeads, per_part = (all + a.split - 1) / a.split;
+        first = part * per_part;
+        last = first + per_part < all ? first + per_part : all;
+    }
+    template <class F>
+    __device__ __attribute__((always_inline)) void each(F&& f) const {
+        if (first < queries) f(std::true_type{}, first, last < queries ? last : queries);
+        if (last > queries) f(std::false_type{}, (first > queries ? first : queries) - queries, last - queries);
+    }
+};
+// Batches of kQkAtOnce passes [first, last): while one is computed the next is on its way.
+template <class Batch, class Request, class Compute>
+__device__ __attribute__((always_inline)) inline void pipelined(int first, int last, Request&& request, Compute&& compute) {
+    Batch in[2][kQkAtOnce];
+    request(first, in[0]);
+    for (int p = first; p < last; p += 2 * kQkAtOnce) {
+        request(p + kQkAtOnce, in[1]);
+        compute(p, in[0]);
+        request(p + 2 * kQkAtOnce, in[0]);
+        compute(p + kQkAtOnce, in[1]);
+    }
+}
+
+template <int G, bool NORM, bool NEIGHBOURS>
 __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
-    const int wave = blockIdx.x * kQkWaves + threadIdx.x / kWave, waves = gridDim.x * kQkWaves;
-    const Place<G> at(a);
-    constexpr int kHeads = kWave / G;            // of a pass
-    const int heads = a.Hq + a.Hkv, passes = (heads + kHeads - 1) / kHeads;
-    const int part = wave % a.split, per_part = (passes + a.split - 1) / a.split;
-    const int first = part * per_part, last = first + per_part < passes ? first + per_part : passes;
+    const int wave = blockIdx.x * kQkWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = gridDim.x * kQkWaves;
+    const Place<G, NEIGHBOURS> at(a);
+    const Passes<G> ps(a, wave % a.split);
+    const int heads = a.Hq + a.Hkv;
+    const float per_d = 1.0f / (float)a.D;
     float wq[8], wk[8];
     if constexpr (NORM) {
-        if (at.there) { unpack(at.load(a.wq), wq); unpack(at.load(a.wk), wk); }
+        if (at.there) { unpack(at.weights(a.wq), wq); unpack(at.weights(a.wk), wk); }
     }
     for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
         float c[4], s[4];
-        const int64_t position = a.rot ? a.positions[m] : 0;
-        const u16* x = a.x + m * a.x_stride;
-        for (int p0 = first; p0 < last; p0 += kQkAtOnce) {
-            Eight in[kQkAtOnce];
+        at.angles(a.rot ? a.positions[m] : 0, c, s);
+        ps.each([&](auto tag, int first, int last) __attribute__((always_inline)) {
+            constexpr bool query = decltype(tag)::value;
+            const int count = query ? a.Hq : a.Hkv, head0 = query ? 0 : a.Hq;
+            const u16* x = a.x + m * a.x_stride + (int64_t)head0 * a.D;
+            u16* y = query ? a.q + m * a.q_stride : a.k + m * a.k_stride;
+            auto request = [&](int p0, Eight (&in)[kQkAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < kQkAtOnce; ++u) {
-                const int head = (p0 + u) * kHeads + at.sub;
-                if (p0 + u < last && head < heads && at.there) in[u] = at.load(x + (int64_t)head * a.D);
-                else in[u] = Eight{v2u{0, 0}, v2u{0, 0}};
-            }
-            if (p0 == first) at.angles(position, c, s);
-#pragma unroll
-            for (int u = 0; u < kQkAtOnce; ++u) {
-                const int head = (p0 + u) * kHeads + at.sub;
-                float v[8];
-                unpack(in[u], v);
-                if constexpr (NORM) {
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(v[j], v[j], sum);
-                    const float rstd = 1.0f / __builtin_sqrtf(group_sum<G>(sum) / (float)a.D + a.eps);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = v[j] * rstd * (head < a.Hq ? wq[j] : wk[j]);
-                    if (a.rstd && at.l == 0 && p0 + u < last && head < heads) a.rstd[m * heads + head] = rstd;
+                for (int u = 0; u < kQkAtOnce; ++u) {
+                    const int head = (p0 + u) * ps.kHeads;
+                    if (p0 + u < last && at.there && head + at.sub < count) in[u] = at.load(x + (int64_t)head * a.D);
                 }
-                at.template turn<1>(c, s, a.interleaved, v);
-                if (p0 + u < last && head < heads && at.there)
-                    at.store(head < a.Hq ? a.q + m * a.q_stride + (int64_t)head * a.D : a.k + m * a.k_stride + (int64_t)(head - a.Hq) * a.D, pack(v));
-            }
-        }
+            };
+            auto compute = [&](int p0, const Eight (&in)[kQkAtOnce]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int u = 0; u < kQkAtOnce; ++u) {
+                    const int head = (p0 + u) * ps.kHeads;
+                    if (p0 + u < last) {
+                        const bool mine = at.there && head + at.sub < count;
+                        float v[8];
+                        unpack(in[u], v);
+                        if constexpr (NORM) {
+                            float sum = 0.0f;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(v[j], v[j], sum);
+                            const float rstd = inverse_root(__builtin_fmaf(group_sum<G>(mine ? sum : 0.0f), per_d, a.eps));
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = v[j] * rstd * (query ? wq[j] : wk[j]);
+                            if (a.rstd && at.l == 0 && mine) a.rstd[m * heads + head0 + head + at.sub] = rstd;
+                        }
+                        at.template turn<1>(c, s, v);
+                        if (mine) at.store(y + (int64_t)head * a.D, pack(v));
+                    }
+                }
+            };
+            pipelined<Eight>(first, last, request, compute);
+        });
     }
 }
 
@@ -207,8 +253,8 @@ __device__ inline void move_v(const QkArgs& a, int64_t m, int first, int step, u
 }
 
 // A workgroup's sums and absmax.  dwq / dwk: a lane's sums for its eight columns.
-template <int G>
-__device__ inline void leave_partials(const QkArgs& a, const Place<G>& at, float (&dwq)[8], float (&dwk)[8], unsigned mag, float* s_dw, unsigned* s_part) {
+template <int G, bool NEIGHBOURS>
+__device__ inline void leave_partials(const QkArgs& a, const Place<G, NEIGHBOURS>& at, float (&dwq)[8], float (&dwk)[8], unsigned mag, float* s_dw, unsigned* s_part) {
     if (a.dw_partial) {
         // the heads of a pass first, then the waves one after the other, each adding to what the ones before it left
 #pragma unroll
@@ -239,74 +285,84 @@ __device__ inline void leave_partials(const QkArgs& a, const Place<G>& at, float
     }
 }
 
-template <int G, bool NORM>
+template <int G, bool NORM, bool NEIGHBOURS>
 __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
     __shared__ float s_dw[NORM ? 2 * 8 * G : 1];
     __shared__ unsigned s_part[kQkWaves];
-    const int wave = blockIdx.x * kQkWaves + threadIdx.x / kWave, waves = gridDim.x * kQkWaves;
-    const Place<G> at(a);
-    constexpr int kHeads = kWave / G;
-    const int heads = a.Hq + a.Hkv, passes = (heads + kHeads - 1) / kHeads;
-    const int part = wave % a.split, per_part = (passes + a.split - 1) / a.split;
-    const int first = part * per_part, last = first + per_part < passes ? first + per_part : passes;
+    const int wave = blockIdx.x * kQkWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = gridDim.x * kQkWaves, part = wave % a.split;
+    const Place<G, NEIGHBOURS> at(a);
+    const Passes<G> ps(a, part);
+    const int heads = a.Hq + a.Hkv;
+    const float per_d = 1.0f / (float)a.D;
     float wq[8], wk[8], dwq[8] = {}, dwk[8] = {};
     unsigned mag = 0;
     if constexpr (NORM) {
-        if (at.there) { unpack(at.load(a.wq), wq); unpack(at.load(a.wk), wk); }
+        if (at.there) { unpack(at.weights(a.wq), wq); unpack(at.weights(a.wk), wk); }
     }
+    struct In { Eight x, dy; float rstd; };
     for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
         float c[4], s[4];
-        const int64_t position = a.rot ? a.positions[m] : 0;
-        for (int p0 = first; p0 < last; p0 += kQkAtOnce) {
-            Eight in[kQkAtOnce], dy[kQkAtOnce];
-            float rstd[kQkAtOnce];
+        at.angles(a.rot ? a.positions[m] : 0, c, s);
+        ps.each([&](auto tag, int first, int last) __attribute__((always_inline)) {
+            constexpr bool query = decltype(tag)::value;
+            const int count = query ? a.Hq : a.Hkv, head0 = query ? 0 : a.Hq;
+            const u16* dy = query ? a.q + m * a.q_stride : a.k + m * a.k_stride;
+            const u16* x = NORM ? a.x + m * a.x_stride + (int64_t)head0 * a.D : nullptr;
+            const float* rstd = NORM ? a.rstd + m * heads + head0 : nullptr;
+            u16* dx = a.dx + m * a.dx_stride + (int64_t)head0 * a.D;
+            auto request = [&](int p0, In (&in)[kQkAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < kQkAtOnce; ++u) {
-                const int head = (p0 + u) * kHeads + at.sub;
-                in[u] = dy[u] = Eight{v2u{0, 0}, v2u{0, 0}};
-                rstd[u] = 0.0f;
-                if (p0 + u < last && head < heads && at.there) {
-                    dy[u] = at.load(head < a.Hq ? a.q + m * a.q_stride + (int64_t)head * a.D : a.k + m * a.k_stride + (int64_t)(head - a.Hq) * a.D);
-                    if constexpr (NORM) {
-                        in[u] = at.load(a.x + m * a.x_stride + (int64_t)head * a.D);
-                        rstd[u] = a.rstd[m * heads + head];
+                for (int u = 0; u < kQkAtOnce; ++u) {
+                    const int head = (p0 + u) * ps.kHeads;
+                    if (p0 + u < last) {
+                        in[u] = In{};                        // (what is not there adds nothing to the sums)
+                        if (at.there && head + at.sub < count) {
+                            in[u].dy = at.load(dy + (int64_t)head * a.D);
+                            if constexpr (NORM) {
+                                in[u].x = at.load(x + (int64_t)head * a.D);
+                                in[u].rstd = rstd[head + at.sub];
+                            }
+                        }
                     }
                 }
-            }
-            if (p0 == first) at.angles(position, c, s);
+            };
+            auto compute = [&](int p0, const In (&in)[kQkAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < kQkAtOnce; ++u) {
-                const int head = (p0 + u) * kHeads + at.sub;
-                float g[8];
-                unpack(dy[u], g);
-                at.template turn<-1>(c, s, a.interleaved, g);
-                if constexpr (NORM) {
-                    float n[8], sum = 0.0f;
-                    unpack(in[u], n);
-                    const bool query = head < a.Hq;
+                for (int u = 0; u < kQkAtOnce; ++u) {
+                    const int head = (p0 + u) * ps.kHeads;
+                    if (p0 + u < last) {
+                        float g[8];
+                        unpack(in[u].dy, g);
+                        at.template turn<-1>(c, s, g);
+                        if constexpr (NORM) {
+                            float n[8], sum = 0.0f;
+                            unpack(in[u].x, n);
+                            const float r = in[u].rstd;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        n[j] *= rstd[u];
-                        const float gn = g[j] * n[j];
-                        dwq[j] += query ? gn : 0.0f;
-                        dwk[j] += query ? 0.0f : gn;
-                        g[j] *= query ? wq[j] : wk[j];
-                        sum = __builtin_fmaf(g[j], n[j], sum);
+                            for (int j = 0; j < 8; ++j) {
+                                n[j] *= r;
+                                if constexpr (query) dwq[j] = __builtin_fmaf(g[j], n[j], dwq[j]);
+                                else dwk[j] = __builtin_fmaf(g[j], n[j], dwk[j]);
+                                g[j] *= query ? wq[j] : wk[j];
+                                sum = __builtin_fmaf(g[j], n[j], sum);
+                            }
+                            const float mean = group_sum<G>(at.there ? sum : 0.0f) * per_d;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) g[j] = r * __builtin_fmaf(-n[j], mean, g[j]);
+                        }
+                        if (at.there && head + at.sub < count) {
+                            const Eight out = pack(g);
+                            track(mag, out);
+                            at.store(dx + (int64_t)head * a.D, out);
+                        }
                     }
-                    const float mean = group_sum<G>(at.there ? sum : 0.0f) / (float)a.D;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] = rstd[u] * __builtin_fmaf(-n[j], mean, g[j]);
                 }
-                if (p0 + u < last && head < heads && at.there) {
-                    const Eight out = pack(g);
-                    track(mag, out);
-                    at.store(a.dx + m * a.dx_stride + (int64_t)head * a.D, out);
-                }
-            }
-        }
+            };
+            pipelined<In>(first, last, request, compute);
+        });
         move_v<4>(a, m, (threadIdx.x & (kWave - 1)) + part * kWave, a.split * kWave, mag);
     }
-    leave_partials<G>(a, at, dwq, dwk, mag, s_dw, s_part);
+    leave_partials(a, at, dwq, dwk, mag, s_dw, s_part);
 }
 
 // ---- Any head size, stride and alignment: a wave for each head of a token, value by value, twice over the head.  Pair p of the turned values, or the single value
@@ -330,7 +386,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_any_kernel(const QkArgs a) 
         if constexpr (NORM) {
             float sum = 0.0f;
             for (int i = lane; i < a.D; i += kWave) { const float v = value(x, i); sum = __builtin_fmaf(v, v, sum); }
-            rstd = 1.0f / __builtin_sqrtf(group_sum<kWave>(sum) / (float)a.D + a.eps);
+            rstd = inverse_root(group_sum<kWave>(sum) / (float)a.D + a.eps);
             if (a.rstd && lane == 0) a.rstd[at] = rstd;
         }
         auto normed = [&](int i) { return NORM ? value(x, i) * rstd * value(w, i) : value(x, i); };
@@ -438,8 +494,16 @@ __global__ __launch_bounds__(256) void qk_bwd_final_kernel(const float* dw_parti
     }
     const int c = threadIdx.x % kFinalCols, r = threadIdx.x / kFinalCols, col = blockIdx.x * kFinalCols + c;
     float sum = 0.0f;
-    if (col < 2 * D)
-        for (int i = r; i < n; i += 16) sum += dw_partial[(int64_t)i * 2 * D + col];
+    if (col < 2 * D) {
+        constexpr int kAtOnce = 16;                          // loads on their way together
+        for (int i0 = r; i0 < n; i0 += 16 * kAtOnce) {
+            float v[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) v[k] = i0 + 16 * k < n ? dw_partial[(int64_t)(i0 + 16 * k) * 2 * D + col] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) sum += v[k];
+        }
+    }
     s_sum[r][c] = sum;
     __syncthreads();
     if (r == 0 && col < 2 * D) {
@@ -485,12 +549,13 @@ static int launch_qk_fwd(QkArgs a, hipStream_t stream, int cus) {
         if (a.wq) hipLaunchKernelGGL(qk_fwd_any_kernel<true>, grid, dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_fwd_any_kernel<false>, grid, dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + a.Hkv + kWave / G - 1) / (kWave / G), cus, cus * 8);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), cus, cus * 8);
         a.split = g.split;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            if (a.wq) hipLaunchKernelGGL((qk_fwd_kernel<L, true>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
-            else hipLaunchKernelGGL((qk_fwd_kernel<L, false>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
+            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(g.blocks), dim3(kQkThreads), 0, stream, a); };
+            if (a.wq) a.interleaved ? with(qk_fwd_kernel<L, true, true>) : with(qk_fwd_kernel<L, true, false>);
+            else a.interleaved ? with(qk_fwd_kernel<L, false, true>) : with(qk_fwd_kernel<L, false, false>);
         };
         if (G == 8) launch(std::integral_constant<int, 8>{});
         else if (G == 16) launch(std::integral_constant<int, 16>{});
@@ -513,13 +578,14 @@ static int launch_qk_bwd(QkArgs a, const QkFinal& f, hipStream_t stream, int cus
         if (a.wq) hipLaunchKernelGGL(qk_bwd_any_kernel<true>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_bwd_any_kernel<false>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + a.Hkv + kWave / G - 1) / (kWave / G), cus, kQkMaxBlocks);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), cus, kQkMaxBlocks);
         a.split = g.split;
         blocks = g.blocks;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            if (a.wq) hipLaunchKernelGGL((qk_bwd_kernel<L, true>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
-            else hipLaunchKernelGGL((qk_bwd_kernel<L, false>), dim3(g.blocks), dim3(kQkThreads), 0, stream, a);
+            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(g.blocks), dim3(kQkThreads), 0, stream, a); };
+            if (a.wq) a.interleaved ? with(qk_bwd_kernel<L, true, true>) : with(qk_bwd_kernel<L, true, false>);
+            else a.interleaved ? with(qk_bwd_kernel<L, false, true>) : with(qk_bwd_kernel<L, false, false>);
         };
         if (G == 8) launch(std::integral_constant<int, 8>{});
         else if (G == 16) launch(std::integral_constant<int, 16>{});
