@@ -144,7 +144,9 @@ struct Place {
     }
 };
 
-constexpr int kQkThreads = 256, kQkWaves = kQkThreads / kWave, kQkAtOnce = 4;
+constexpr int kQkThreads = 256, kQkWaves = kQkThreads / kWave;
+// The vector kernel of the backward pass: workgroups of eight waves, so that there are fewer rows of sums to add
+constexpr int kQkBwdThreads = 512, kQkBwdWaves = kQkBwdThreads / kWave;
 
 // The passes of a wave over the heads of a token: first all of the queries, then all of the keys, so that a pass has one weight and one base address.
 // each(f): f(tag, first, last, head0) for the wave's share of the queries' passes, then of the keys'; tag::value: whether they are queries.
@@ -164,16 +166,16 @@ struct Passes {
         if (last > queries) f(std::false_type{}, (first > queries ? first : queries) - queries, last - queries);
     }
 };
-// Batches of kQkAtOnce passes [first, last): while one is computed the next is on its way.
-template <class Batch, class Request, class Compute>
+// Batches of N passes [first, last): while one is computed the next is on its way.
+template <class Batch, int N, class Request, class Compute>
 __device__ __attribute__((always_inline)) inline void pipelined(int first, int last, Request&& request, Compute&& compute) {
-    Batch in[2][kQkAtOnce];
+    Batch in[2][N];
     request(first, in[0]);
-    for (int p = first; p < last; p += 2 * kQkAtOnce) {
-        request(p + kQkAtOnce, in[1]);
+    for (int p = first; p < last; p += 2 * N) {
+        request(p + N, in[1]);
         compute(p, in[0]);
-        request(p + 2 * kQkAtOnce, in[0]);
-        compute(p + kQkAtOnce, in[1]);
+        request(p + 2 * N, in[0]);
+        compute(p + N, in[1]);
     }
 }
 
@@ -188,6 +190,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
     if constexpr (NORM) {
         if (at.there) { unpack(at.weights(a.wq), wq); unpack(at.weights(a.wk), wk); }
     }
+    constexpr int kAtOnce = 4;
     for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
         float c[4], s[4];
         at.angles(a.rot ? a.positions[m] : 0, c, s);
@@ -196,16 +199,16 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
             const int count = query ? a.Hq : a.Hkv, head0 = query ? 0 : a.Hq;
             const u16* x = a.x + m * a.x_stride + (int64_t)head0 * a.D;
             u16* y = query ? a.q + m * a.q_stride : a.k + m * a.k_stride;
-            auto request = [&](int p0, Eight (&in)[kQkAtOnce]) __attribute__((always_inline)) {
+            auto request = [&](int p0, Eight (&in)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int u = 0; u < kQkAtOnce; ++u) {
+                for (int u = 0; u < kAtOnce; ++u) {
                     const int head = (p0 + u) * ps.kHeads;
                     if (p0 + u < last && at.there && head + at.sub < count) in[u] = at.load(x + (int64_t)head * a.D);
                 }
             };
-            auto compute = [&](int p0, const Eight (&in)[kQkAtOnce]) __attribute__((always_inline)) {
+            auto compute = [&](int p0, const Eight (&in)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int u = 0; u < kQkAtOnce; ++u) {
+                for (int u = 0; u < kAtOnce; ++u) {
                     const int head = (p0 + u) * ps.kHeads;
                     if (p0 + u < last) {
                         const bool mine = at.there && head + at.sub < count;
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
                     }
                 }
             };
-            pipelined<Eight>(first, last, request, compute);
+            pipelined<Eight, kAtOnce>(first, last, request, compute);
         });
     }
 }
@@ -252,44 +255,19 @@ __device__ inline void move_v(const QkArgs& a, int64_t m, int first, int step, u
     }
 }
 
-// A workgroup's sums and absmax.  dwq / dwk: a lane's sums for its eight columns.
-template <int G, bool NEIGHBOURS>
-__device__ inline void leave_partials(const QkArgs& a, const Place<G, NEIGHBOURS>& at, float (&dwq)[8], float (&dwk)[8], unsigned mag, float* s_dw, unsigned* s_part) {
-    if (a.dw_partial) {
-        // the heads of a pass first, then the waves one after the other, each adding to what the ones before it left
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-#pragma unroll
-            for (int step = G; step < kWave; step *= 2) {
-                dwq[j] += __shfl_xor(dwq[j], step);
-                dwk[j] += __shfl_xor(dwk[j], step);
-            }
-        }
-        for (int w = 0; w < kQkWaves; ++w) {
-            if ((int)(threadIdx.x / kWave) == w && at.sub == 0 && at.there) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int col = j < 4 ? at.lo + j : at.hi + j - 4;
-                    s_dw[col] = (w ? s_dw[col] : 0.0f) + dwq[j];
-                    s_dw[a.D + col] = (w ? s_dw[a.D + col] : 0.0f) + dwk[j];
-                }
-            }
-            __syncthreads();
-        }
-        for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) a.dw_partial[(int64_t)blockIdx.x * 2 * a.D + i] = s_dw[i];
-    }
-    if (a.amax_partial) {
-        mag = (mag & 0xFFFFu) > (mag >> 16) ? mag & 0xFFFFu : mag >> 16;
-        mag = block_max_u32<kQkThreads>(mag, s_part);
-        if (threadIdx.x == 0) a.amax_partial[blockIdx.x] = mag;
-    }
+template <int THREADS>
+__device__ inline void leave_absmax(const QkArgs& a, unsigned mag, unsigned* s_part) {
+    if (!a.amax_partial) return;
+    mag = (mag & 0xFFFFu) > (mag >> 16) ? mag & 0xFFFFu : mag >> 16;
+    mag = block_max_u32<THREADS>(mag, s_part);
+    if (threadIdx.x == 0) a.amax_partial[blockIdx.x] = mag;
 }
 
 template <int G, bool NORM, bool NEIGHBOURS>
-__global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
-    __shared__ float s_dw[NORM ? 2 * 8 * G : 1];
-    __shared__ unsigned s_part[kQkWaves];
-    const int wave = blockIdx.x * kQkWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = gridDim.x * kQkWaves, part = wave % a.split;
+__global__ __launch_bounds__(kQkBwdThreads) void qk_bwd_kernel(const QkArgs a) {
+    __shared__ float s_dw[NORM ? kQkBwdWaves : 1][NORM ? 2 * 8 * G : 1];
+    __shared__ unsigned s_part[kQkBwdWaves];
+    const int wave = blockIdx.x * kQkBwdWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = gridDim.x * kQkBwdWaves, part = wave % a.split;
     const Place<G, NEIGHBOURS> at(a);
     const Passes<G> ps(a, part);
     const int heads = a.Hq + a.Hkv;
@@ -300,6 +278,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
         if (at.there) { unpack(at.weights(a.wq), wq); unpack(at.weights(a.wk), wk); }
     }
     struct In { Eight x, dy; float rstd; };
+    constexpr int kAtOnce = 2;
     for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
         float c[4], s[4];
         at.angles(a.rot ? a.positions[m] : 0, c, s);
@@ -310,9 +289,9 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
             const u16* x = NORM ? a.x + m * a.x_stride + (int64_t)head0 * a.D : nullptr;
             const float* rstd = NORM ? a.rstd + m * heads + head0 : nullptr;
             u16* dx = a.dx + m * a.dx_stride + (int64_t)head0 * a.D;
-            auto request = [&](int p0, In (&in)[kQkAtOnce]) __attribute__((always_inline)) {
+            auto request = [&](int p0, In (&in)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int u = 0; u < kQkAtOnce; ++u) {
+                for (int u = 0; u < kAtOnce; ++u) {
                     const int head = (p0 + u) * ps.kHeads;
                     if (p0 + u < last) {
                         in[u] = In{};                        // (what is not there adds nothing to the sums)
@@ -326,9 +305,9 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
                     }
                 }
             };
-            auto compute = [&](int p0, const In (&in)[kQkAtOnce]) __attribute__((always_inline)) {
+            auto compute = [&](int p0, const In (&in)[kAtOnce]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int u = 0; u < kQkAtOnce; ++u) {
+                for (int u = 0; u < kAtOnce; ++u) {
                     const int head = (p0 + u) * ps.kHeads;
                     if (p0 + u < last) {
                         float g[8];
@@ -358,11 +337,36 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_kernel(const QkArgs a) {
                     }
                 }
             };
-            pipelined<In>(first, last, request, compute);
+            pipelined<In, kAtOnce>(first, last, request, compute);
         });
         move_v<4>(a, m, (threadIdx.x & (kWave - 1)) + part * kWave, a.split * kWave, mag);
     }
-    leave_partials(a, at, dwq, dwk, mag, s_dw, s_part);
+    if constexpr (NORM) {
+        if (a.dw_partial) {
+            // the heads of a pass first, then the waves
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                for (int step = G; step < kWave; step *= 2) {
+                    dwq[j] += __shfl_xor(dwq[j], step);
+                    dwk[j] += __shfl_xor(dwk[j], step);
+                }
+                const int col = j < 4 ? at.lo + j : at.hi + j - 4;
+                if (at.sub == 0 && at.there) {
+                    s_dw[threadIdx.x / kWave][col] = dwq[j];
+                    s_dw[threadIdx.x / kWave][a.D + col] = dwk[j];
+                }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < 2 * a.D; i += kQkBwdThreads) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kQkBwdWaves; ++w) sum += s_dw[w][i];
+                a.dw_partial[(int64_t)blockIdx.x * 2 * a.D + i] = sum;
+            }
+        }
+    }
+    leave_absmax<kQkBwdThreads>(a, mag, s_part);
 }
 
 // ---- Any head size, stride and alignment: a wave for each head of a token, value by value, twice over the head.  Pair p of the turned values, or the single value
@@ -466,11 +470,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_bwd_any_kernel(const QkArgs a) 
                 a.dw_partial[(int64_t)blockIdx.x * 2 * a.D + i] = sum;
             }
     }
-    if (a.amax_partial) {
-        mag = (mag & 0xFFFFu) > (mag >> 16) ? mag & 0xFFFFu : mag >> 16;
-        mag = block_max_u32<kQkThreads>(mag, s_part);
-        if (threadIdx.x == 0) a.amax_partial[blockIdx.x] = mag;
-    }
+    leave_absmax<kQkThreads>(a, mag, s_part);
 }
 
 // The workgroups' sums in their order: a workgroup has 16 columns and 16 lanes to each, which take every 16th row and are added at the end; the
@@ -529,14 +529,14 @@ static int lanes_of_head(int D, int rot) {
 }
 
 struct QkGrid { int blocks, split; };
-// A wave takes a token; where there are fewer than eight waves a CU that way, the heads of a token are shared out among 2, 4, ... of them, each of which finds the angles for itself.
-static QkGrid qk_grid(int64_t M, int passes, int cus, int most) {
+// A wave takes a token; where there are fewer than `wanted` waves that way, the heads of a token are shared out among 2, 4, ... of them, each of which finds the angles for itself.
+// most: workgroups
+static QkGrid qk_grid(int64_t M, int passes, int64_t wanted, int wg_waves, int most) {
     int split = 1;
-    while (split < passes && M * split < 8 * (int64_t)cus) split *= 2;
-    const int64_t blocks = (M * split + kQkWaves - 1) / kQkWaves;
-    // (waves that share a token lie in one grid of a multiple of `split` waves)
+    while (split < passes && M * split < wanted) split *= 2;
+    const int64_t blocks = (M * split + wg_waves - 1) / wg_waves;
     int n = (int)(blocks < most ? blocks : most);
-    if (split > kQkWaves) { const int per = split / kQkWaves; n = (n + per - 1) / per * per; }
+    if (split > wg_waves) { const int per = split / wg_waves; n = (n + per - 1) / per * per; }      // (a multiple of `split` waves)
     return {n, split};
 }
 
@@ -549,7 +549,7 @@ static int launch_qk_fwd(QkArgs a, hipStream_t stream, int cus) {
         if (a.wq) hipLaunchKernelGGL(qk_fwd_any_kernel<true>, grid, dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_fwd_any_kernel<false>, grid, dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), cus, cus * 8);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 8 * cus, kQkWaves, cus * 8);
         a.split = g.split;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
@@ -578,12 +578,12 @@ static int launch_qk_bwd(QkArgs a, const QkFinal& f, hipStream_t stream, int cus
         if (a.wq) hipLaunchKernelGGL(qk_bwd_any_kernel<true>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_bwd_any_kernel<false>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), cus, kQkMaxBlocks);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 4 * cus, kQkBwdWaves, kQkMaxBlocks / 2);
         a.split = g.split;
         blocks = g.blocks;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(g.blocks), dim3(kQkThreads), 0, stream, a); };
+            auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(g.blocks), dim3(kQkBwdThreads), 0, stream, a); };
             if (a.wq) a.interleaved ? with(qk_bwd_kernel<L, true, true>) : with(qk_bwd_kernel<L, true, false>);
             else a.interleaved ? with(qk_bwd_kernel<L, false, true>) : with(qk_bwd_kernel<L, false, false>);
         };
