@@ -122,9 +122,10 @@ struct Place {
     __device__ Eight load(const u16* p) const {
         return Eight{__builtin_nontemporal_load(reinterpret_cast<const v2u*>(p + off_lo)), __builtin_nontemporal_load(reinterpret_cast<const v2u*>(p + off_hi))};
     }
+    template <bool STREAM>
     __device__ void store(u16* p, const Eight& e) const {
-        *reinterpret_cast<v2u*>(p + off_lo) = e.lo;
-        *reinterpret_cast<v2u*>(p + off_hi) = e.hi;
+        store_hinted<STREAM>(e.lo, reinterpret_cast<v2u*>(p + off_lo));
+        store_hinted<STREAM>(e.hi, reinterpret_cast<v2u*>(p + off_hi));
     }
     // SIGN 1: by the angles, -1: back
     template <int SIGN>
@@ -145,8 +146,7 @@ struct Place {
 };
 
 constexpr int kQkThreads = 256, kQkWaves = kQkThreads / kWave;
-// The vector kernel of the backward pass: workgroups of eight waves, so that there are fewer rows of sums to add
-constexpr int kQkBwdThreads = 512, kQkBwdWaves = kQkBwdThreads / kWave;
+constexpr int kQkBwdThreads = 256, kQkBwdWaves = kQkBwdThreads / kWave;
 
 // The passes of a wave over the heads of a token: first all of the queries, then all of the keys, so that a pass has one weight and one base address.
 // each(f): f(tag, first, last, head0) for the wave's share of the queries' passes, then of the keys'; tag::value: whether they are queries.
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
                             if (a.rstd && at.l == 0 && mine) a.rstd[m * heads + head0 + head + at.sub] = rstd;
                         }
                         at.template turn<1>(c, s, v);
-                        if (mine) at.store(y + (int64_t)head * a.D, pack(v));
+                        if (mine) at.template store<false>(y + (int64_t)head * a.D, pack(v));
                     }
                 }
             };
@@ -263,7 +263,7 @@ __device__ inline void leave_absmax(const QkArgs& a, unsigned mag, unsigned* s_p
     if (threadIdx.x == 0) a.amax_partial[blockIdx.x] = mag;
 }
 
-template <int G, bool NORM, bool NEIGHBOURS>
+template <int G, bool NORM, bool NEIGHBOURS, bool STREAM>
 __global__ __launch_bounds__(kQkBwdThreads) void qk_bwd_kernel(const QkArgs a) {
     __shared__ float s_dw[NORM ? kQkBwdWaves : 1][NORM ? 2 * 8 * G : 1];
     __shared__ unsigned s_part[kQkBwdWaves];
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kQkBwdThreads) void qk_bwd_kernel(const QkArgs a) {
                         if (at.there && head + at.sub < count) {
                             const Eight out = pack(g);
                             track(mag, out);
-                            at.store(dx + (int64_t)head * a.D, out);
+                            at.template store<STREAM>(dx + (int64_t)head * a.D, out);
                         }
                     }
                 }
@@ -549,7 +549,7 @@ static int launch_qk_fwd(QkArgs a, hipStream_t stream, int cus) {
         if (a.wq) hipLaunchKernelGGL(qk_fwd_any_kernel<true>, grid, dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_fwd_any_kernel<false>, grid, dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 8 * cus, kQkWaves, cus * 8);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 8 * cus, kQkWaves, cus * 5);
         a.split = g.split;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
@@ -578,14 +578,21 @@ static int launch_qk_bwd(QkArgs a, const QkFinal& f, hipStream_t stream, int cus
         if (a.wq) hipLaunchKernelGGL(qk_bwd_any_kernel<true>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_bwd_any_kernel<false>, dim3(blocks), dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 4 * cus, kQkBwdWaves, kQkMaxBlocks / 2);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 4 * cus, kQkBwdWaves, 3 * cus < kQkMaxBlocks ? 3 * cus : kQkMaxBlocks);
         a.split = g.split;
         blocks = g.blocks;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
             auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(g.blocks), dim3(kQkBwdThreads), 0, stream, a); };
-            if (a.wq) a.interleaved ? with(qk_bwd_kernel<L, true, true>) : with(qk_bwd_kernel<L, true, false>);
-            else a.interleaved ? with(qk_bwd_kernel<L, false, true>) : with(qk_bwd_kernel<L, false, false>);
+            auto of = [&](auto stream) {
+                constexpr bool ST = decltype(stream)::value;
+                if (a.wq) a.interleaved ? with(qk_bwd_kernel<L, true, true, ST>) : with(qk_bwd_kernel<L, true, false, ST>);
+                else a.interleaved ? with(qk_bwd_kernel<L, false, true, ST>) : with(qk_bwd_kernel<L, false, false, ST>);
+            };
+            // (of the pass and the quantizer of its result behind it, 112 MiB of query and key gradients take 105 us with plain stores and 110 streamed, 140 129 and 132,
+            // 192 224 and 210; alone, with nothing to read them, 77 and 69, 92 and 83, 138 and 124)
+            if (streams_out(a.M * (a.Hq + a.Hkv) * (int64_t)a.D * 2, a.D, 64)) of(std::true_type{});
+            else of(std::false_type{});
         };
         if (G == 8) launch(std::integral_constant<int, 8>{});
         else if (G == 16) launch(std::integral_constant<int, 16>{});
