@@ -38,7 +38,9 @@ struct AdamWHyper { float b1, b2, c1, c2, lr_decay, lr_m, root_scale, eps; unsig
 static_assert(sizeof(AdamWHyper) == 4 * LLMQ_ADAMW_HYPER_WORDS, "");
 
 constexpr float kRootMeanBeta = 0.96875f;
-constexpr int kAdamThreads = 256, kAdamLane = 8, kAdamTrips = 2, kAdamPiece = kAdamThreads * kAdamLane * kAdamTrips;
+// A lane has four elements of a group, a wave 256 that follow each other, so that every load and store of a wave is one piece of memory; a workgroup's piece of a
+// tensor is several groups one after the other, the next one's loads on their way while one is computed.
+constexpr int kAdamThreads = 256, kAdamLane = 4, kAdamGroup = kAdamThreads * kAdamLane, kAdamTrips = 4, kAdamPiece = kAdamGroup * kAdamTrips;
 
 // 32 well mixed bits for a counter under a key.  The multipliers are odd numbers from the golden ratio and the square roots of 2 and 3.
 __host__ __device__ inline unsigned mixed_bits(uint64_t counter, unsigned key) {
@@ -51,109 +53,130 @@ __host__ __device__ inline unsigned mixed_bits(uint64_t counter, unsigned key) {
 // 2^(code - 127); NaN for 255
 __device__ inline float power_of(unsigned code) { return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7FC00000u : code << 23); }
 
-// Largest of 16 lanes (a block of 128 values, eight a lane), in all of them
-__device__ inline unsigned max_of_16(unsigned v) {
+// Largest of 32 lanes (a block of 128 values, four a lane), in all of them
+__device__ inline unsigned max_of_32(unsigned v) {
     auto with = [&](unsigned t) { v = v > t ? v : t; };
     with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
     with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
     with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));
     with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false));
-    return v;
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return r[0] > r[1] ? r[0] : r[1];
 }
 
-// E4M3 code of a magnitude of at most 448, by 16 random bits; square: the mean of the code's square is kept instead of its own
-__device__ inline unsigned code_of(float a, unsigned rnd, bool square) {
-    const unsigned bits = __float_as_uint(a);
-    unsigned normal = ((bits + (rnd << 4)) >> 20) - 960u;
-    if (square) {
+// E4M3 code (its low 8 bits) of a magnitude x with x 2^(127 - scale) <= 448, by 16 random bits.  x is brought to 2^8 times that: the low byte of the exponent
+// and the first three bits of the mantissa is then the code of a normal value, and below 2^-6 the last bits of x + 2^22, which rounds to nearest even at the spacing of those codes.
+// SQUARE: the mean of the code's square is kept instead of its own.
+template <bool SQUARE>
+__device__ inline unsigned code_of(float x, int scale, unsigned rnd) {
+    const float a = __builtin_amdgcn_ldexpf(x, 135 - scale);
+    const unsigned bits = __float_as_uint(a), small = __float_as_uint(a + 4194304.0f);
+    unsigned normal = (bits + (rnd << 4)) >> 20;
+    if constexpr (SQUARE) {
         const float f = (float)(bits & 0xFFFFFu) * 0x1p-20f, n2 = (float)(16u + 2u * ((bits >> 20) & 7u));
-        normal = (bits >> 20) - 960u + (((float)rnd + 0.5f) * (n2 + 1.0f) < f * (n2 + f) * 65536.0f ? 1u : 0u);
+        normal = (bits >> 20) + (((float)rnd + 0.5f) * (n2 + 1.0f) < f * (n2 + f) * 65536.0f ? 1u : 0u);
     }
-    const unsigned small = (unsigned)(int)__builtin_rintf(a * 512.0f);
-    const unsigned c = a >= 0.015625f ? normal : small;
-    return c < 127u ? c : 127u;                              // (a NaN's)
+    return a >= 4.0f ? normal : small;
+}
+__device__ inline unsigned pack_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
-// Eight values of a lane, of which `valid` exist; zeros behind them
-template <class T>
-__device__ inline void load8(const T* p, int valid, T (&v)[8]) {
-    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T) < 8 ? 16 / sizeof(T) : 8)));
-    constexpr int kVec = sizeof(vec) / sizeof(T);
-    if (valid >= 8) {
-#pragma unroll
-        for (int i = 0; i < 8; i += kVec) {
-            const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p + i));
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) v[i + j] = x[j];
-        }
+// What a tensor holds, fixed for its workgroups: moments in codes; gradients in binary32; a master copy (or binary32 weights); BF16 weights.  GUARD: the piece reaches over the
+// tensor's end.
+template <bool CODES_, bool G32_, bool MASTER_, bool HALF_, bool GUARD_>
+struct Kind { static constexpr bool CODES = CODES_, G32 = G32_, MASTER = MASTER_, HALF = HALF_, GUARD = GUARD_; };
+
+// Four elements at p, of which `valid` exist; zeros behind them
+template <bool GUARD, class V, class T>
+__device__ inline V load4(const T* p, int valid) {
+    static_assert(sizeof(V) == 4 * sizeof(T), "");
+    if constexpr (!GUARD) {
+        return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
     } else {
+        T e[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : T(0);
+        for (int i = 0; i < 4; ++i) e[i] = i < valid ? p[i] : T(0);
+        return __builtin_bit_cast(V, e);
     }
 }
-template <class T>
-__device__ inline void store8(T* p, int valid, const T (&v)[8]) {
-    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T) < 8 ? 16 / sizeof(T) : 8)));
-    constexpr int kVec = sizeof(vec) / sizeof(T);
-    if (valid >= 8) {
-#pragma unroll
-        for (int i = 0; i < 8; i += kVec) {
-            vec x;
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) x[j] = v[i + j];
-            __builtin_nontemporal_store(x, reinterpret_cast<vec*>(p + i));
-        }
+template <bool GUARD, class V, class T>
+__device__ inline void store4(T* p, int valid, const V& v) {
+    static_assert(sizeof(V) == 4 * sizeof(T), "");
+    if constexpr (!GUARD) {
+        __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
     } else {
+        T e[4];
+        __builtin_memcpy(e, &v, sizeof(v));
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) p[i] = v[i];
+        for (int i = 0; i < 4; ++i)
+            if (i < valid) p[i] = e[i];
     }
-}
-__device__ inline void bf16_values(const uint16_t (&b)[8], float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float((unsigned)b[i] << 16);
 }
 
-// The step for eight elements of a lane.  Every operation is rounded by itself (no fused multiply-add), so that the values, and the codes with them, are
-// the same wherever the formulas are evaluated in binary32.
-template <bool CODES>
-__device__ inline unsigned adamw_eight(const AdamWTensor& t, const AdamWHyper& h, float grad_scale, int64_t at) {
-#pragma clang fp contract(off)
+// A lane's four elements as they lie in memory
+template <class K>
+struct Group {
+    std::conditional_t<K::G32, v4f, v2u> g;
+    std::conditional_t<K::MASTER, v4f, v2u> w;
+    std::conditional_t<K::CODES, unsigned, v4f> m, v;
+    unsigned ms, vs;
+};
+__device__ inline v4f bf16_values(const v2u& b) {
+    return v4f{__uint_as_float(b[0] << 16), __uint_as_float(b[0] & 0xFFFF0000u), __uint_as_float(b[1] << 16), __uint_as_float(b[1] & 0xFFFF0000u)};
+}
+template <class K>
+__device__ inline int valid_of(const AdamWTensor& t, int64_t at) {
     const int64_t left = t.n - at;
-    const int valid = left >= 8 ? 8 : left > 0 ? (int)left : 0;
-    float g[8], w[8], m[8], v[8];
-    uint16_t half[8];
-    if (t.flags & LLMQ_ADAMW_GRAD_F32) {
-        load8(static_cast<const float*>(t.g) + at, valid, g);
+    return !K::GUARD || left >= 4 ? 4 : left > 0 ? (int)left : 0;
+}
+template <class K>
+__device__ inline void request(const AdamWTensor& t, int64_t at, Group<K>& r) {
+    const int valid = valid_of<K>(t, at);
+    if constexpr (K::G32) r.g = load4<K::GUARD, v4f>(static_cast<const float*>(t.g) + at, valid);
+    else r.g = load4<K::GUARD, v2u>(static_cast<const uint16_t*>(t.g) + at, valid);
+    if constexpr (K::MASTER) r.w = load4<K::GUARD, v4f>(t.master + at, valid);
+    else r.w = load4<K::GUARD, v2u>(t.w + at, valid);
+    if constexpr (K::CODES) {
+        r.m = load4<K::GUARD, unsigned>(static_cast<const uint8_t*>(t.m) + at, valid);
+        r.v = load4<K::GUARD, unsigned>(static_cast<const uint8_t*>(t.v) + at, valid);
+        r.ms = valid ? t.m_scale[at / kBlock] : 127u;
+        r.vs = valid ? t.v_scale[at / kBlock] : 127u;
     } else {
-        load8(static_cast<const uint16_t*>(t.g) + at, valid, half);
-        bf16_values(half, g);
+        r.m = load4<K::GUARD, v4f>(static_cast<const float*>(t.m) + at, valid);
+        r.v = load4<K::GUARD, v4f>(static_cast<const float*>(t.v) + at, valid);
     }
-    if (t.master) {
-        load8(t.master + at, valid, w);
-    } else {
-        load8(t.w + at, valid, half);
-        bf16_values(half, w);
-    }
-    if constexpr (CODES) {
-        uint8_t mc[8], vc[8];
-        load8(static_cast<const uint8_t*>(t.m) + at, valid, mc);
-        load8(static_cast<const uint8_t*>(t.v) + at, valid, vc);
-        const float ms = valid ? power_of(t.m_scale[at / kBlock]) : 1.0f, vs = valid ? power_of(t.v_scale[at / kBlock]) : 1.0f;
+}
+__device__ inline v4f decoded(unsigned codes) {
+    return v4f{__builtin_amdgcn_cvt_f32_fp8((int)codes, 0), __builtin_amdgcn_cvt_f32_fp8((int)codes, 1), __builtin_amdgcn_cvt_f32_fp8((int)codes, 2), __builtin_amdgcn_cvt_f32_fp8((int)codes, 3)};
+}
+
+// The step for a lane's four elements; returns the largest magnitude of its new BF16 weights.  Every operation is rounded by itself (no fused multiply-add), so that
+// the values, and the codes with them, are the same wherever the formulas are evaluated in binary32.
+template <class K>
+__device__ inline unsigned step_of(const AdamWTensor& t, const AdamWHyper& h, float grad_scale, int64_t at, const Group<K>& r) {
+#pragma clang fp contract(off)
+    const int valid = valid_of<K>(t, at);
+    v4f g, w, m, v, root;
+    if constexpr (K::G32) g = r.g; else g = bf16_values(r.g);
+    if constexpr (K::MASTER) w = r.w; else w = bf16_values(r.w);
+    if constexpr (K::CODES) {
+        const float ms = power_of(r.ms), vs = power_of(r.vs);
+        m = decoded(r.m);
+        v = decoded(r.v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i] = __builtin_amdgcn_cvt_f32_fp8(mc[i], 0) * ms;
-            v[i] = __builtin_amdgcn_cvt_f32_fp8(vc[i], 0) * vs;
+        for (int i = 0; i < 4; ++i) {
+            m[i] = m[i] * ms;
+            v[i] = v[i] * vs;
             v[i] = v[i] * v[i];
         }
     } else {
-        load8(static_cast<const float*>(t.m) + at, valid, m);
-        load8(static_cast<const float*>(t.v) + at, valid, v);
+        m = r.m;
+        v = r.v;
     }
     const float lr_decay = t.flags & LLMQ_ADAMW_NO_DECAY ? 0.0f : h.lr_decay;
-    float root[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
         g[i] = g[i] * grad_scale;
         m[i] = m[i] * h.b1 + g[i] * h.c1;
         v[i] = v[i] * h.b2 + (g[i] * g[i]) * h.c2;
@@ -162,48 +185,71 @@ __device__ inline unsigned adamw_eight(const AdamWTensor& t, const AdamWHyper& h
         w[i] = decayed - (m[i] / (root[i] * h.root_scale + h.eps)) * h.lr_m;
     }
     const uint64_t counter = (uint64_t)(t.counter + at);
-    if constexpr (CODES) {
+    if constexpr (K::CODES) {
         unsigned m_mag = 0, v_mag = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const unsigned a = __float_as_uint(m[i]) & 0x7FFFFFFFu, b = __float_as_uint(root[i]) & 0x7FFFFFFFu;
             m_mag = m_mag > a ? m_mag : a;
             v_mag = v_mag > b ? v_mag : b;
         }
-        const unsigned ms = scale_code<0>(max_of_16(m_mag)), vs = scale_code<0>(max_of_16(v_mag));
-        const float m_up = power_of(254u - ms), v_up = power_of(254u - vs);
-        uint8_t mc[8], vc[8];
+        const unsigned ms = scale_code<0>(max_of_32(m_mag)), vs = scale_code<0>(max_of_32(v_mag));
+        auto codes = [&](auto square) __attribute__((always_inline)) {
+            unsigned mc[4], vc[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned rnd = mixed_bits(counter + i, h.key);
-            mc[i] = (uint8_t)(code_of(__builtin_fabsf(m[i]) * m_up, rnd & 0xFFFFu, false) | (m[i] < 0.0f ? 0x80u : 0u));
-            const unsigned c = code_of(root[i] * v_up, rnd >> 16, h.b2 > kRootMeanBeta);
-            vc[i] = (uint8_t)(c == 0 && root[i] > 0.0f ? 1u : c);
-        }
-        store8(static_cast<uint8_t*>(t.m) + at, valid, mc);
-        store8(static_cast<uint8_t*>(t.v) + at, valid, vc);
+            for (int i = 0; i < 4; ++i) {
+                const unsigned rnd = mixed_bits(counter + i, h.key);
+                mc[i] = (code_of<false>(__builtin_fabsf(m[i]), (int)ms, rnd & 0xFFFFu) & 0x7Fu) | (__float_as_uint(m[i]) >> 24 & 0x80u);
+                vc[i] = code_of<decltype(square)::value>(root[i], (int)vs, rnd >> 16) & 0x7Fu;
+                vc[i] = vc[i] == 0 && root[i] > 0.0f ? 1u : vc[i];
+            }
+            store4<K::GUARD>(static_cast<uint8_t*>(t.m) + at, valid, pack_bytes(mc[0], mc[1], mc[2], mc[3]));
+            store4<K::GUARD>(static_cast<uint8_t*>(t.v) + at, valid, pack_bytes(vc[0], vc[1], vc[2], vc[3]));
+        };
+        if (h.b2 > kRootMeanBeta) codes(std::true_type{});
+        else codes(std::false_type{});
         if (valid && at % kBlock == 0) {
             t.m_scale[at / kBlock] = (uint8_t)ms;
             t.v_scale[at / kBlock] = (uint8_t)vs;
         }
     } else {
-        store8(static_cast<float*>(t.m) + at, valid, m);
-        store8(static_cast<float*>(t.v) + at, valid, v);
+        store4<K::GUARD>(static_cast<float*>(t.m) + at, valid, m);
+        store4<K::GUARD>(static_cast<float*>(t.v) + at, valid, v);
     }
-    if (t.master) store8(t.master + at, valid, w);
+    if constexpr (K::MASTER) store4<K::GUARD>(t.master + at, valid, w);
     unsigned mag = 0;
-    if (t.w) {
+    if constexpr (K::HALF) {
+        unsigned half[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             half[i] = __builtin_bit_cast(uint16_t, (__bf16)w[i]);
-            if (!t.master && (t.flags & LLMQ_ADAMW_STOCHASTIC)) {
+            if constexpr (!K::MASTER) {
                 const unsigned bits = __float_as_uint(w[i]);
-                if ((bits & 0x7F800000u) != 0x7F800000u) half[i] = (uint16_t)((bits + (mixed_bits(counter + i, ~h.key) & 0xFFFFu)) >> 16);
+                if ((t.flags & LLMQ_ADAMW_STOCHASTIC) && (bits & 0x7F800000u) != 0x7F800000u) half[i] = (bits + (mixed_bits(counter + i, ~h.key) & 0xFFFFu)) >> 16;
             }
-            const unsigned a = half[i] & 0x7FFFu;
-            if (i < valid) mag = mag > a ? mag : a;
         }
-        store8(t.w + at, valid, half);
+        const v2u packed = {half[0] | half[1] << 16, half[2] | half[3] << 16};
+        store4<K::GUARD>(t.w + at, valid, packed);
+        if (t.amax) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < valid) mag = mag > (half[i] & 0x7FFFu) ? mag : half[i] & 0x7FFFu;
+        }
+    }
+    return mag;
+}
+
+template <class K>
+__device__ inline unsigned step_of_piece(const AdamWTensor& t, const AdamWHyper& h, float grad_scale, int64_t at) {
+    Group<K> r[2];
+    unsigned mag = 0;
+    request(t, at, r[0]);
+#pragma unroll
+    for (int k = 0; k < kAdamTrips; ++k) {
+        if (k + 1 < kAdamTrips) request(t, at + kAdamGroup, r[(k + 1) % 2]);
+        const unsigned a = step_of(t, h, grad_scale, at, r[k % 2]);
+        mag = mag > a ? mag : a;
+        at += kAdamGroup;
     }
     return mag;
 }
@@ -216,13 +262,21 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamWTensor* 
     const AdamWHyper h = d_hyper ? *d_hyper : by_value;
     const AdamWPiece p = pieces[blockIdx.x + first];
     const AdamWTensor t = tensors[p.tensor];
-    int64_t at = (int64_t)p.piece * kAdamPiece + threadIdx.x * kAdamLane;
+    const int64_t at = (int64_t)p.piece * kAdamPiece + threadIdx.x * kAdamLane;
     unsigned mag = 0;
-#pragma unroll 1
-    for (int k = 0; k < kAdamTrips; ++k, at += kAdamThreads * kAdamLane) {
-        const unsigned a = t.flags & LLMQ_ADAMW_STATES_8BIT ? adamw_eight<true>(t, h, grad_scale, at) : adamw_eight<false>(t, h, grad_scale, at);
-        mag = mag > a ? mag : a;
-    }
+    auto with = [&](auto codes, auto g32, auto master, auto half) __attribute__((always_inline)) {
+        constexpr bool C = decltype(codes)::value, G = decltype(g32)::value, M = decltype(master)::value, H = decltype(half)::value;
+        if (t.n - (int64_t)p.piece * kAdamPiece >= kAdamPiece) mag = step_of_piece<Kind<C, G, M, H, false>>(t, h, grad_scale, at);
+        else mag = step_of_piece<Kind<C, G, M, H, true>>(t, h, grad_scale, at);
+    };
+    auto with_weights = [&](auto codes, auto g32) __attribute__((always_inline)) {
+        if (t.master && t.w) with(codes, g32, std::true_type{}, std::true_type{});
+        else if (t.master) with(codes, g32, std::true_type{}, std::false_type{});
+        else with(codes, g32, std::false_type{}, std::true_type{});
+    };
+    const bool g32 = t.flags & LLMQ_ADAMW_GRAD_F32;
+    if (t.flags & LLMQ_ADAMW_STATES_8BIT) g32 ? with_weights(std::true_type{}, std::true_type{}) : with_weights(std::true_type{}, std::false_type{});
+    else g32 ? with_weights(std::false_type{}, std::true_type{}) : with_weights(std::false_type{}, std::false_type{});
     if (t.amax) {
         mag = block_max_u32<kAdamThreads>(mag, s_part);
         if (threadIdx.x == 0) {
