@@ -8,8 +8,7 @@ namespace llmq {
 
 
 // The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
-// times by a few percent.  Tiles with sides of 192 and 320 are not built: a wave's rows would not start at a multiple of 64, where a register holds the
-// scales of whole groups of four blocks.
+// times by a few percent.  Tiles with sides of 320 are not built: they have no registers left for the scales.
 static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, bool with_amax, int num_cus) {
     BlocksPlan plan{0, {0, 0, kNoEdge}};
     const int64_t steps = (T + BK - 1) / BK, rounded = ((R > C ? R : C) + 127) / 128 * 128;
@@ -20,13 +19,15 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
         const bool whole = R % (64 * ni) == 0 && C % (64 * nj) == 0 && T % BK == 0;
         return TilePlan{ni, nj, whole ? kNoEdge : aligned_rows ? kEdge : kEdgeUnaligned};
     };
-    // (256 x 256 tiles whose chunks go through registers would spill accumulators)
-    auto built = [&](const TilePlan& p) { return p.edge != kEdgeUnaligned || p.ni * p.nj < 16; };
+    // guarded tiles: those whose accumulators stay where they are (192 x 128 with two workgroups to a CU, and 256 x 256 whose chunks go through registers, would move some)
+    auto built = [&](const TilePlan& p) {
+        if (p.edge == kNoEdge) return true;
+        return p.nj != 3 && (p.edge == kEdge ? p.ni != 3 || p.nj == 4 : p.ni != 3 && p.ni * p.nj < 16);
+    };
     if (const char* e = tuning_env("LLMQ_GEMM_ANY_TILE")) {
-        if ((e[0] == '2' || e[0] == '4') && e[1] == 'x' && (e[2] == '2' || e[2] == '4')) {
-            plan.tile = form(e[0] - '0', e[2] - '0');
-            if (built(plan.tile)) return plan;
-            plan.tile = {0, 0, kNoEdge};
+        if (e[0] >= '2' && e[0] <= '4' && e[1] == 'x' && e[2] >= '2' && e[2] <= '4') {
+            const TilePlan p = form(e[0] - '0', e[2] - '0');
+            if (built(p)) { plan.tile = p; return plan; }
         }
         if (e[0] == '0') return plan;
     }
@@ -36,8 +37,8 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
     if (ragged && generic_is_faster(R, C, T, false, false, accumulate, with_amax, false, num_cus)) return plan;
     if (((R + 127) / 128) * ((C + 127) / 128) <= resident_slots(num_cus, 2, 2) / 2) { plan.tile = form(2, 2); return plan; }
     double best_us = 0.0;
-    for (int ni = 4; ni >= 2; ni -= 2)
-        for (int nj = 4; nj >= 2; nj -= 2) {
+    for (int ni = 4; ni >= 2; --ni)
+        for (int nj = 4; nj >= 2; --nj) {
             const int64_t tiles = ((R + 64 * ni - 1) / (64 * ni)) * ((C + 64 * nj - 1) / (64 * nj));
             if (tiles > kMaxWorkgroups) continue;
             const TilePlan p = form(ni, nj);

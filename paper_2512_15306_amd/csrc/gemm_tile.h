@@ -273,10 +273,13 @@ __device__ inline void mma_block_scaled(v4f& c, const v8i& a, const v8i& b, int 
     }
 }
 
-// Scales of a K step, four block rows or columns of the wave tile to a register; NoScales: operands without.
+// Scales of a K step, PA block rows and PB block columns of the wave tile to a register; NoScales: operands without.
 struct NoScales {};
-template <int WA, int WB>
-struct BlockScales { int a[WA], b[WB]; };
+template <int WA, int WB, int PA, int PB>
+struct BlockScales {
+    static constexpr int kPerA = PA, kPerB = PB;
+    int a[WA], b[WB];
+};
 
 // One quarter of a wave tile's MFMAs of a K step: the 16 x 16 blocks (I0 + i, J0 + j) of the accumulators from HI
 // fragments of A and HJ fragments of B (32 bytes per lane each: the 128-byte K step of 16 operand rows), i running
@@ -291,7 +294,7 @@ __device__ inline void mma_quadrant(BlockAcc<MI, MJ>& acc, const v8i (&a)[HI], c
         constexpr int i = J_OUTER ? m % HI : m / HJ, j = J_OUTER ? m / HI : m % HJ;
         constexpr bool in_v = I0 + i >= kBlocksInFile || J0 + j >= kBlocksInFile;
         if constexpr (std::is_same_v<Scales, NoScales>) mma_block<FA, FB, in_v>(acc.t[I0 + i][J0 + j], a[i], b[j]);
-        else mma_block_scaled<FA, FB, in_v, (I0 + i) % 4, (J0 + j) % 4>(acc.t[I0 + i][J0 + j], a[i], b[j], sc.a[(I0 + i) / 4], sc.b[(J0 + j) / 4]);
+        else mma_block_scaled<FA, FB, in_v, (I0 + i) % Scales::kPerA, (J0 + j) % Scales::kPerB>(acc.t[I0 + i][J0 + j], a[i], b[j], sc.a[(I0 + i) / Scales::kPerA], sc.b[(J0 + j) / Scales::kPerB]);
         side(tag);
         __builtin_amdgcn_sched_barrier(0);
     });
@@ -671,36 +674,36 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
             for (int e = 0; e < 4; ++e) acc.t[i][j][e] = zero;
 
     // Block scales: d_sA / d_sB point at the codes, a 128-row group's K step one contiguous piece in which byte 8 (row % 16) + row / 16 is the row's, so
-    // that a lane's row of four neighbouring blocks of 16 rows is one register.  A step's registers are requested two steps ahead, into those of
-    // the step that has just ended; two instructions, a step's newest loads.
-    static_assert(!BS || ((NI == 2 || NI == 4) && (NJ == 2 || NJ == 4) && MODE == kWholeTiles && FA != kFmtBf16), "a wave's rows start at a multiple of 64");
-    constexpr int WA = (MI + 3) / 4, WB = (MJ + 3) / 4, kScaleLoads = BS ? 2 : 0;
-    typedef std::conditional_t<BS, BlockScales<WA, WB>, NoScales> Scales;
+    // that a lane's row of four neighbouring blocks of 16 rows is one register.  A side of 192 starts a wave's rows at a multiple of 32: there two blocks
+    // share a register.  A step's registers are requested two steps ahead, into those of the step that has just ended, as its newest loads.
+    static_assert(!BS || (NI <= 4 && NJ <= 4 && MODE == kWholeTiles && FA != kFmtBf16), "sides of 320 have no registers left for scales");
+    constexpr int PA = NI == 3 ? 2 : 4, PB = NJ == 3 ? 2 : 4, WA = (MI + PA - 1) / PA, WB = (MJ + PB - 1) / PB;
+    constexpr int kScaleLoads = BS ? (NI == 3 ? WA : 1) + (NJ == 3 ? WB : 1) : 0;
+    typedef std::conditional_t<BS, BlockScales<WA, WB, PA, PB>, NoScales> Scales;
     Scales scales[2];
     const int pitchA = (Rn + 127) & ~127, pitchB = (Cn + 127) & ~127;
-    auto rsrc_of_scales = [&](const float* d, int pitch, int first) {
-        const int all = ((T + BK - 1) / BK) * pitch;
-        return make_rsrc(reinterpret_cast<const uint8_t*>(d) + first, (unsigned)(all - first));
+    const __amdgpu_buffer_rsrc_t rsSA = BS ? make_rsrc(d_sA, (unsigned)(((T + BK - 1) / BK) * pitchA)) : rsA, rsSB = BS ? make_rsrc(d_sB, (unsigned)(((T + BK - 1) / BK) * pitchB)) : rsB;
+    // first block of 16 rows of the wave (with eight waves of the two that share a register)
+    const int blockA = tr * (BM / 16) + wr * MI, blockB = tc * (BN / 16) + (MJ == 2 ? (wc & ~1) * MJ : wc * MJ);
+    const int sc_voff = 8 * (lane & 15);
+    // offset of a block's codes in a K step (a tile may reach over the last group of 128 rows: what is read there, codes of another step or zeros, goes to rows that do not exist)
+    auto code_offset = [](int block) { return (block >> 3) * 128 + (block & 7); };
+    auto request_operand = [&](auto three, auto& words, __amdgpu_buffer_rsrc_t rs, int block, int at) __attribute__((always_inline)) {
+        constexpr int W = sizeof(words) / sizeof(int);
+        if constexpr (decltype(three)::value) {
+#pragma unroll
+            for (int p = 0; p < W; ++p) words[p] = (int)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, sc_voff, at + code_offset(block + 2 * p), 0);
+        } else if constexpr (W == 2) {
+            const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rs, sc_voff, at + code_offset(block), 0));
+            words[0] = v[0], words[1] = v[1];
+        } else {
+            words[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rs, sc_voff, at + code_offset(block), 0);
+        }
     };
-    // (a tile's second group of 128 rows may lie behind the last one: those rows' products go nowhere, whatever bytes are found there)
-    const int firstA = tr * BM + (NI == 4 ? wr * 128 : 0), firstB = tc * BN + (NJ == 4 ? wc * 128 : 0);
-    const __amdgpu_buffer_rsrc_t rsSA = BS ? rsrc_of_scales(d_sA, pitchA, firstA < pitchA ? firstA : 0) : rsA, rsSB = BS ? rsrc_of_scales(d_sB, pitchB, firstB < pitchB ? firstB : 0) : rsB;
-    const int sc_voffA = 8 * (lane & 15) + (NI == 2 ? 4 * wr : 0), sc_voffB = 8 * (lane & 15) + (NJ == 2 ? 4 * (MJ == 4 ? wc : wc >> 1) : 0);
-    auto request_scales = [&](auto& sc, int step) {
+    auto request_scales = [&](auto& sc, int step) __attribute__((always_inline)) {
         if constexpr (BS) {
-            const int stepA = step < nk ? step * pitchA : kOutOfRange, stepB = step < nk ? step * pitchB : kOutOfRange;
-            if constexpr (WA == 2) {
-                const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rsSA, sc_voffA, stepA, 0));
-                sc.a[0] = v[0], sc.a[1] = v[1];
-            } else {
-                sc.a[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rsSA, sc_voffA, stepA, 0);
-            }
-            if constexpr (WB == 2) {
-                const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rsSB, sc_voffB, stepB, 0));
-                sc.b[0] = v[0], sc.b[1] = v[1];
-            } else {
-                sc.b[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rsSB, sc_voffB, stepB, 0);
-            }
+            request_operand(BoolTag<NI == 3>{}, sc.a, rsSA, blockA, step < nk ? step * pitchA : kOutOfRange);
+            request_operand(BoolTag<NJ == 3>{}, sc.b, rsSB, blockB, step < nk ? step * pitchB : kOutOfRange);
         }
     };
 

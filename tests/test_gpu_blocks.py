@@ -159,12 +159,12 @@ def test_contraction(R, C, T, fa, fb):
     assert torch.equal(c, c3)                              # same inputs, same bytes
 
 
-TILES = ["4x4", "4x2", "2x4", "2x2"]
+TILES = ["4x4", "4x3", "4x2", "3x4", "3x3", "3x2", "2x4", "2x3", "2x2"]
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("tile", TILES + ["mini 32", "mini 64", "0x0"])
-@pytest.mark.parametrize("R,C,T", [(256, 512, 128), (512, 256, 640), (512, 768, 1152), (300, 700, 272), (450, 333, 400), (300, 268, 1001), (129, 257, 17), (600, 520, 1664)])
+@pytest.mark.parametrize("R,C,T", [(256, 512, 128), (512, 256, 640), (512, 768, 1152), (384, 576, 256), (768, 384, 640), (300, 700, 272), (450, 333, 400), (300, 268, 1001), (129, 257, 17), (600, 520, 1664)])
 def test_every_kernel(R, C, T, tile, accumulate, monkeypatch):
     if tile.startswith("mini"):
         monkeypatch.setenv("LLMQ_GEMM_MINI", tile[5:])
