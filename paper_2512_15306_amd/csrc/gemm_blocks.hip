@@ -9,8 +9,20 @@ namespace llmq {
 
 // The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
 // times by a few percent.  Tiles with sides of 320 are not built: they have no registers left for the scales.
+// Whether a contraction of few rows takes the kernel for those: more than one K step, and where its workgroups come in several rounds, enough of them.  The kernels below /
+// it, R x C x T, microseconds: 1 x 4608 x 3584 8.2 / 5.8, 16 x 1024 x 8192 13.8 / 7.3, 16 x 18944 x 3584 23.8 / 19.9, 5 x 39782 x 6960 80.5 / 50.6, 32 x 512 x 512 4.2 / 3.1,
+// 5 x 700 x 333 9.9 / 3.2, 9 x 5305 x 4643 40.2 / 17.0, 2 x 11141 x 12797 122 / 81;  and where they are faster 3 x 26124 x 1632 12.6 / 15.2, 28 x 20369 x 1120 10.9 / 12.8,
+// 3 x 9669 x 480 4.8 / 5.0, 2 x 6136 x 128 2.9 / 3.4, 2 x 25206 x 2203 26.4 / 31.8.
+// LLMQ_FEW=0 / 1 (tests): never, or for up to 32 rows always.
+static bool takes_few(int64_t R, int64_t C, int64_t T) {
+    if (R > 32) return false;
+    if (const char* e = tuning_env("LLMQ_FEW")) return atoi(e) != 0;
+    const int64_t steps = (T + BK - 1) / BK;
+    return steps > 1 && (C <= 8192 || steps >= (T % 16 == 0 ? 20 : 40));
+}
+
 static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, bool with_amax, int num_cus) {
-    BlocksPlan plan{0, {0, 0, kNoEdge}};
+    BlocksPlan plan{false, 0, {0, 0, kNoEdge}};
     const int64_t steps = (T + BK - 1) / BK, rounded = ((R > C ? R : C) + 127) / 128 * 128;
     // 32-bit offsets from the first row of a tile, of operands, scales and output; sixteen bytes in every row of an operand
     if (T < 16 || T >= (1ll << 22) || C >= (1ll << 22) || steps * rounded >= 0x7FFFF000ll) return plan;
@@ -31,6 +43,8 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
         }
         if (e[0] == '0') return plan;
     }
+    plan.few = takes_few(R, C, T);
+    if (plan.few) return plan;
     plan.side = aligned_rows ? takes_mini(R, C, T, false, false, accumulate, with_amax, false, num_cus) : 0;
     if (plan.side) return plan;
     const bool ragged = R % 128 != 0 || C % 128 != 0 || T % BK != 0;

@@ -171,6 +171,7 @@ def test_every_kernel(R, C, T, tile, accumulate, monkeypatch):
     else:
         monkeypatch.setenv("LLMQ_GEMM_ANY_TILE", tile)
         monkeypatch.setenv("LLMQ_GEMM_MINI", "0")
+    monkeypatch.setenv("LLMQ_FEW", "0")
     for deep in ("0", "1") if tile == "2x2" else ("0",):
         monkeypatch.setenv("LLMQ_GEMM_DEEP", deep)
         qa, sa, qb, sb, va, vb = operands(R, C, T, 1, 0, R + T, 1)
@@ -201,6 +202,22 @@ def test_scales_of_rows_alone_give_the_bytes_of_the_contraction_without_them(R, 
     llmq.llmq_fp8_gemm_blocks(a, sa, fa, b, sb, fb, got)
     power = torch.ldexp(torch.ones(()).double(), (ea - 127) + (eb - 127).t()).to(DEV)
     assert torch.equal(got.double(), want.double() * power)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("R,C,T", [(1, 16, 16), (1, 5, 200), (3, 50, 131), (16, 64, 2048), (9, 4200, 640), (16, 100, 1999), (17, 33, 4112), (32, 4099, 512), (25, 4096, 272), (31, 1000, 777), (2, 40, 20000)])
+def test_few_rows(R, C, T, accumulate, monkeypatch):
+    """The kernel for few rows, one and two blocks of columns to a workgroup, whole chunks and any, fewer steps than waves and many more."""
+    monkeypatch.setenv("LLMQ_FEW", "1")
+    for fa, fb in ((0, 0), (1, 0), (0, 1), (1, 1)):
+        qa, sa, qb, sb, va, vb = operands(R, C, T, fa, fb, R + T, 1 if C % 2 else 128)
+        old = torch.randn(R, C, device=DEV).to(torch.bfloat16)
+        guard = torch.full((R * C + 64,), 3.0, device=DEV, dtype=torch.bfloat16)
+        c, amax = guard[: R * C].view(R, C), torch.zeros(1, device=DEV)
+        c.copy_(old)
+        llmq.llmq_fp8_gemm_blocks(qa, sa, fa, qb, sb, fb, c, accumulate, amax)
+        assert_close(c, va, vb, T, old if accumulate else None)
+        assert amax.item() == c.abs().max().item() and (guard[R * C :] == 3.0).all()
 
 
 def test_many_steps_and_tiles():
