@@ -263,7 +263,7 @@ void launch_blocks(const BlocksOperands& p, const BlocksPlan& plan, hipStream_t 
         LLMQ_BLOCKS_CASE(4, 4, kNoEdge) LLMQ_BLOCKS_CASE(4, 3, kNoEdge) LLMQ_BLOCKS_CASE(4, 2, kNoEdge)
         LLMQ_BLOCKS_CASE(3, 4, kNoEdge) LLMQ_BLOCKS_CASE(3, 3, kNoEdge) LLMQ_BLOCKS_CASE(3, 2, kNoEdge)
         LLMQ_BLOCKS_CASE(2, 4, kNoEdge) LLMQ_BLOCKS_CASE(2, 3, kNoEdge) LLMQ_BLOCKS_CASE(2, 2, kNoEdge)
-        LLMQ_BLOCKS_CASE(4, 4, kEdge) LLMQ_BLOCKS_CASE(4, 2, kEdge) LLMQ_BLOCKS_CASE(3, 4, kEdge) LLMQ_BLOCKS_CASE(2, 4, kEdge) LLMQ_BLOCKS_CASE(2, 2, kEdge)
+        LLMQ_BLOCKS_CASE(4, 4, kEdge) LLMQ_BLOCKS_CASE(4, 2, kEdge) LLMQ_BLOCKS_CASE(3, 4, kEdge) LLMQ_BLOCKS_CASE(3, 2, kEdge) LLMQ_BLOCKS_CASE(2, 4, kEdge) LLMQ_BLOCKS_CASE(2, 2, kEdge)
         LLMQ_BLOCKS_CASE(4, 2, kEdgeUnaligned) LLMQ_BLOCKS_CASE(2, 4, kEdgeUnaligned) LLMQ_BLOCKS_CASE(2, 2, kEdgeUnaligned)
         default: break;
     }

@@ -5,10 +5,6 @@
 
 namespace llmq {
 
-
-
-// The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
-// times by a few percent.  Tiles with sides of 320 are not built: they have no registers left for the scales.
 // Whether a contraction of few rows takes the kernel for those: more than one K step, and where its workgroups come in several rounds, enough of them.  The kernels below /
 // it, R x C x T, microseconds: 1 x 4608 x 3584 8.2 / 5.8, 16 x 1024 x 8192 13.8 / 7.3, 16 x 18944 x 3584 23.8 / 19.9, 5 x 39782 x 6960 80.5 / 50.6, 32 x 512 x 512 4.2 / 3.1,
 // 5 x 700 x 333 9.9 / 3.2, 9 x 5305 x 4643 40.2 / 17.0, 2 x 11141 x 12797 122 / 81;  and where they are faster 3 x 26124 x 1632 12.6 / 15.2, 28 x 20369 x 1120 10.9 / 12.8,
@@ -21,6 +17,8 @@ static bool takes_few(int64_t R, int64_t C, int64_t T) {
     return steps > 1 && (C <= 8192 || steps >= (T % 16 == 0 ? 20 : 40));
 }
 
+// The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
+// times by a few percent.  Tiles with sides of 320 are not built: they have no registers left for the scales.
 static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, bool with_amax, int num_cus) {
     BlocksPlan plan{false, 0, {0, 0, kNoEdge}};
     const int64_t steps = (T + BK - 1) / BK, rounded = ((R > C ? R : C) + 127) / 128 * 128;
@@ -31,11 +29,8 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
         const bool whole = R % (64 * ni) == 0 && C % (64 * nj) == 0 && T % BK == 0;
         return TilePlan{ni, nj, whole ? kNoEdge : aligned_rows ? kEdge : kEdgeUnaligned};
     };
-    // guarded tiles: those whose accumulators stay where they are (192 x 128 with two workgroups to a CU, and 256 x 256 whose chunks go through registers, would move some)
-    auto built = [&](const TilePlan& p) {
-        if (p.edge == kNoEdge) return true;
-        return p.nj != 3 && (p.edge == kEdge ? p.ni != 3 || p.nj == 4 : p.ni != 3 && p.ni * p.nj < 16);
-    };
+    // guarded tiles are not built 192 columns wide, nor 192 rows high or 256 x 256 with chunks that go through registers (those would spill accumulators)
+    auto built = [&](const TilePlan& p) { return p.edge == kNoEdge || (p.nj != 3 && (p.edge == kEdge || (p.ni != 3 && p.ni * p.nj < 16))); };
     if (const char* e = tuning_env("LLMQ_GEMM_ANY_TILE")) {
         if (e[0] >= '2' && e[0] <= '4' && e[1] == 'x' && e[2] >= '2' && e[2] <= '4') {
             const TilePlan p = form(e[0] - '0', e[2] - '0');

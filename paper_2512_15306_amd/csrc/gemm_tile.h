@@ -384,8 +384,9 @@ __device__ inline v4u load16_upto(const uint8_t* p, int64_t valid) {
 
 // FP8 tiles of up to 6 units (2 x 2 to 3 x 2 and 2 x 3) fit twice into the LDS of a CU, and the launch bound keeps their kernels to the half of the registers that lets them.
 // Without it the accumulating ones take 276 (3 x 2) and 324 (2 x 3): 14016 x 3200 x 256 51.0 us without, 39.0 with it.  (In BF16 they fit by themselves.)
+// (A guarded tile of six units with block scales would move accumulators out of their registers to keep to it; it has its CU to itself.)
 template <int FA, int FB, int NI, int NJ, bool ACCUM, class V = GemmTuning, bool TA = false, bool TB = false, int MODE = kWholeTiles, int EDGE = kNoEdge>
-__global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 && V::kStages == 2 && EDGE != kEdgeUnaligned && FA != kFmtBf16) ? 2 : 1) void gemm_tile_kernel(
+__global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 && V::kStages == 2 && EDGE != kEdgeUnaligned && FA != kFmtBf16 && !(V::kBlockScales && EDGE == kEdge && NI * NJ == 6)) ? 2 : 1) void gemm_tile_kernel(
     const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, uint16_t* __restrict__ C,
     int Cn, int T, const float* __restrict__ d_sA, const float* __restrict__ d_sB,
     unsigned* __restrict__ amax_bits, int tiles_r, int tiles_c, int touch_ahead, int band_rows, int next_stride,

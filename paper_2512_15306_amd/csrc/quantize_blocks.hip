@@ -17,7 +17,7 @@ struct QuantBlocks {
     const uint16_t* x;
     int64_t rows, cols;
     uint8_t *q, *s, *qt, *st;
-    unsigned grid_cols, first;                  // tile columns; first tile of this launch
+    SmallGrid grid;                             // of 128 x 128 tiles
 };
 
 // Two BF16 values divided by 2^(code - 127) as two codes in the low or high half of old.  The instruction reads the exponent of its scale, rounds to
@@ -63,12 +63,14 @@ __device__ inline void tile_write_transposed_upto(const uint8_t* s_t, uint8_t* d
 }
 
 // SQUARE: blocks of 128 x 128 (both copies have the same codes), else 1 x 128 of each copy's rows.  ROWS / COLS: which copies are wanted.
-template <int FMT, bool SQUARE, bool ROWS, bool COLS, bool GUARD>
+// STREAM: the row-wise copy is stored with the streaming hint.
+template <int FMT, bool SQUARE, bool ROWS, bool COLS, bool GUARD, bool STREAM>
 __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const QuantBlocks t) {
     __shared__ __attribute__((aligned(16))) uint8_t s_t[COLS ? kTileLdsBytes : 16];
     __shared__ __attribute__((aligned(16))) unsigned s_mag[4][64];           // column pairs of each wave
     __shared__ __attribute__((aligned(16))) uint8_t s_code[2][kBlock];       // codes of the tile's rows and columns, in the order they are kept in
-    const unsigned tile = blockIdx.x + t.first, brow = tile / t.grid_cols, bcol = tile - brow * t.grid_cols;
+    unsigned brow, bcol;
+    if (!small_tile(t.grid, blockIdx.x + t.grid.first, brow, bcol)) return;
     const int wave = threadIdx.x / kWave;
     int stacked, beside;
     wave_patch(stacked, beside);
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Qua
             store_codes_upto(w, dst, cols, t.rows - r0, cols - c0);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPatchRows; ++i) *reinterpret_cast<v2u*>(dst + (int64_t)i * cols) = v2u{w[i][0], w[i][1]};
+            for (int i = 0; i < kPatchRows; ++i) store_hinted<STREAM>(v2u{w[i][0], w[i][1]}, reinterpret_cast<v2u*>(dst + (int64_t)i * cols));
         }
     }
     if constexpr (COLS) {
@@ -194,15 +196,22 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Qua
 template <int FMT, bool SQUARE, bool ROWS, bool COLS>
 static int launch_quantize_blocks(QuantBlocks t, hipStream_t stream) {
     const bool whole = t.rows % kTileRows == 0 && t.cols % kTileCols == 0;
-    t.grid_cols = (unsigned)((t.cols + kTileCols - 1) / kTileCols);
-    const int64_t tiles = (t.rows + kTileRows - 1) / kTileRows * t.grid_cols;
-    const unsigned most = max_workgroups();
-    for (int64_t first = 0; first < tiles; first += most) {
-        const unsigned blocks = (unsigned)(tiles - first < most ? tiles - first : most);
-        t.first = (unsigned)first;
-        if (whole) hipLaunchKernelGGL((quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false>), dim3(blocks), dim3(kTileThreads), 0, stream, t);
-        else hipLaunchKernelGGL((quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, true>), dim3(blocks), dim3(kTileThreads), 0, stream, t);
-    }
+    SmallGrid g{};
+    g.rows = (unsigned)((t.rows + kTileRows - 1) / kTileRows);
+    g.cols = (unsigned)((t.cols + kTileCols - 1) / kTileCols);
+    g.blocks = (g.rows * g.cols + kSmallXcds - 1) / kSmallXcds * kSmallXcds;
+    // Rows of either copy that do not start at cache lines share lines with the tiles beside them, which then belong on one XCD (launch order / XCD ranges: 1777 x 4601 13.6 / 11.2 us,
+    // 1777 x 4608 10.8 / 10.5, 8191 x 3583 38.2 / 38.1;  rows of lines 8192 x 3584 21.5 / 22.6).
+    g.xcd_ranges = t.rows % 64 != 0 || t.cols % 64 != 0;
+    // (plain / streamed: 8192 x 18944 130.2 / 124.6 us, 8192 x 3584 23.7 / 24.5)
+    const bool stream_q = whole && ROWS && streams_out((ROWS + COLS) * t.rows * t.cols, t.cols, 128, 96);
+    small_launches(g, [&](const SmallGrid& part, unsigned blocks) {
+        t.grid = part;
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kTileThreads), 0, stream, t); };
+        if (!whole) launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, true, false>);
+        else if (stream_q) launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false, ROWS>);
+        else launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false, false>);
+    });
     return hipGetLastError() == hipSuccess ? LLMQ_OK : LLMQ_ERR_DEVICE;
 }
 
@@ -229,7 +238,7 @@ int llmq_quantize_fp8_blocks(const void* x_bf16, int64_t rows, int64_t cols, int
     if (!fmt_ok(fmt)) return LLMQ_ERR_FORMAT;
     if (block_rows != 1 && block_rows != 128) return LLMQ_ERR_FLAGS;
     if (!aligned(x_bf16, 16) || !aligned(q, 16) || !aligned(s, 16) || !aligned(q_t, 16) || !aligned(s_t, 16)) return LLMQ_ERR_ALIGN;
-    const llmq::QuantBlocks t{static_cast<const uint16_t*>(x_bf16), rows, cols, q, s, q_t, s_t, 0, 0};
+    const llmq::QuantBlocks t{static_cast<const uint16_t*>(x_bf16), rows, cols, q, s, q_t, s_t, {}};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (fmt == LLMQ_E4M3) return block_rows == 128 ? llmq::launch_copies<0, true>(t, st) : llmq::launch_copies<0, false>(t, st);
     return block_rows == 128 ? llmq::launch_copies<1, true>(t, st) : llmq::launch_copies<1, false>(t, st);

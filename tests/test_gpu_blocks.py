@@ -59,6 +59,16 @@ def test_one_copy_alone_is_the_same(rows, cols, copies, block_rows):
         assert b is None or torch.equal(a, b)
 
 
+@pytest.mark.parametrize("rows,cols", [(384, 512), (300, 400)])
+def test_streamed_stores_and_pieces_of_a_launch(rows, cols, monkeypatch):
+    x = tensor(rows, cols, 3)
+    plain = run_quantize(x, 0, 1)
+    monkeypatch.setenv("LLMQ_STREAM", "1")
+    monkeypatch.setenv("LLMQ_MAX_WORKGROUPS", "8")
+    for a, b in zip(plain, run_quantize(x, 0, 1)):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_every_magnitude(fmt, block_rows):
