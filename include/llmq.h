@@ -439,8 +439,8 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
  *     g = dy turned back;   dw[i] = sum over rows and heads of g[i] x[i] rstd;   dx[i] = rstd (g[i] w[i] - x[i] rstd mean(g w x rstd))
  *   dwq, dwk [D] float, added to if accumulate != 0; NULL: not wanted.  The sums are taken in an order that depends on the sizes alone.  d_amax, d_scale [1] float or
  *   NULL: absmax of all of dqkv and its scale for fmt, bit for bit as llmq_amax of dqkv has them.  qkv and rstd are not read without a norm (and may be NULL).
- *   dq and dk may be the query and key columns of dqkv.  ws: llmq_qk_norm_rope_workspace_bytes bytes, 16-byte aligned, contents irrelevant; NULL if neither dw nor
- *   d_amax is wanted.
+ *   dq and dk may be the query and key columns of dqkv.  ws: llmq_qk_norm_rope_workspace_bytes bytes, 16-byte aligned, contents irrelevant (calls that may overlap on
+ *   the device, graphs among them, need different ones); NULL if neither dw nor d_amax is wanted.
  * *_stride: elements from row to row, at least a row's width.  Rows may start at any element (2-byte aligned); D and rot multiples of 8 (D up to 512) with rows that
  * start at multiples of 8 bytes are fast, others take a slow kernel.  M, Hq, Hkv >= 1, heads up to 65536, 1 <= D <= 1024.
  */

@@ -94,6 +94,25 @@ def check_accumulator_reads(src: str, asm: str) -> None:
         raise RuntimeError("%s: accumulator registers touched inside the MFMA stretch:\n  %s" % (src, "\n  ".join(bad)))
 
 
+def check_scale_operands(src: str, asm: str) -> None:
+    """The scaled MFMAs of the tile kernels are written out too, so the compiler keeps no distance between an ordinary vector instruction and the MFMA that reads
+    what it wrote.  Their operands come from loads, which are waited for by counter, or from statements that end with wait states of their own; a copy or shift that the
+    compiler adds on its own within the three instructions in front of such an MFMA is a build error."""
+    bad = []
+    for m in re.finditer(r"^(_ZN4llmq16gemm_tile_kernel\w*):[^\n]*\n(.*?)^\.Lfunc_end", asm, re.S | re.M):
+        code = [l.split(";")[0].strip() for l in m.group(2).splitlines()]
+        code = [l for l in code if l and (not l.startswith(".") or l.startswith(".LBB"))]
+        for i, l in enumerate(code):
+            if not l.startswith("v_mfma_scale_"):
+                continue
+            operands = _registers(l.split("op_sel")[0]) - _registers(l.split()[1])
+            for before in code[max(0, i - 3):i]:
+                if before.startswith("v_") and not before.startswith("v_mfma_") and _registers(before.split(",")[0]) & operands:
+                    bad.append("%s: %s in front of %s" % (m.group(1), before, l))
+    if bad:
+        raise RuntimeError("%s: an operand of a scaled MFMA is written right in front of it:\n  %s" % (src, "\n  ".join(bad[:20])))
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     work = tempfile.mkdtemp(prefix="llmq_build_")
@@ -166,7 +185,9 @@ def _build_in(work: str, hipcc: str, verbose: bool) -> str:
         raise RuntimeError("hipcc failed")
     for src in sorted(CHECKED_SOURCES):
         with open(os.path.join(work, src.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))) as f:
-            check_accumulator_reads(src, f.read())
+            asm = f.read()
+        check_accumulator_reads(src, asm)
+        check_scale_operands(src, asm)
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", new_lib])
     binding_built = binding_built and _finish_binding(_run_binding(link_binding))
     # Both are there (or the module is not going to be): now they replace the old ones.  A module of another build must not stay
