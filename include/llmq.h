@@ -50,7 +50,7 @@ typedef enum {
     LLMQ_ERR_WORKSPACE = -5,  /* workspace missing or smaller than llmq_fp8_linear_workspace_bytes() */
     LLMQ_ERR_DEVICE = -6,     /* the HIP runtime reported an error at launch */
     LLMQ_ERR_FLAGS = -7,      /* unknown bits in `flags` */
-    LLMQ_ERR_VALUE = -8       /* a number is out of range */
+    LLMQ_ERR_VALUE = -8       /* a number is out of range, or arrays overlap that must not */
 } llmq_status;
 
 /* OCP 8-bit floating point formats (Section 2): E4M3 has bias 7 and max 448 (no Inf, NaN = S.1111.111),
@@ -437,7 +437,7 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
  *   The values V stay where they are.  q and k may be the query and key columns of qkv themselves (in place).
  * llmq_qk_norm_rope_bwd: dq, dk of q and k, dv of V (or NULL: V's columns of dqkv already hold it, or dv points at them) -> dqkv, laid out as qkv, and
  *     g = dy turned back;   dw[i] = sum over rows and heads of g[i] x[i] rstd;   dx[i] = rstd (g[i] w[i] - x[i] rstd mean(g w x rstd))
- *   dwq, dwk [D] float, added to if accumulate != 0; NULL: not wanted.  The sums are taken in an order that depends on the sizes alone.  d_amax, d_scale [1] float or
+ *   dwq, dwk [D] float, added to if accumulate != 0; NULL: not wanted (and there are none without a norm: LLMQ_ERR_NULL).  The sums are taken in an order that depends on the sizes alone.  d_amax, d_scale [1] float or
  *   NULL: absmax of all of dqkv and its scale for fmt, bit for bit as llmq_amax of dqkv has them.  qkv and rstd are not read without a norm (and may be NULL).
  *   dq and dk may be the query and key columns of dqkv.  ws: llmq_qk_norm_rope_workspace_bytes bytes, 16-byte aligned, contents irrelevant (calls that may overlap on
  *   the device, graphs among them, need different ones); NULL if neither dw nor d_amax is wanted.
@@ -466,7 +466,8 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
  *   w' = (w - w lr weight_decay) - (m' / (sqrt(v') / sqrt(1 - b2^step) + eps)) (lr / (1 - b1^step))        LLMQ_ADAMW_NO_DECAY: without the decay
  *   in binary32, each operation rounded by itself; the factors made of b1, b2, lr and step in binary64 and rounded once.
  *
- * llmq_adamw_tensor, all pointers device memory, each array of n elements, 16-byte aligned (the scales: any):
+ * llmq_adamw_tensor, all pointers device memory, each array of n >= 1 elements, 16-byte aligned (the scales: any).  No array that is written shares memory with
+ * another of the call (LLMQ_ERR_VALUE from llmq_adamw_plan: a tensor that is named twice, say):
  *   w_bf16, w_f32   the weights: BF16 alone;  binary32 alone;  or both: w_f32 is the master copy, which is stepped, and w_bf16 receives it rounded to nearest
  *                   even.  BF16 alone is rounded to nearest even, or with LLMQ_ADAMW_STOCHASTIC up or down with the probability that keeps the mean.
  *   grad            BF16, or binary32 with LLMQ_ADAMW_GRAD_F32.

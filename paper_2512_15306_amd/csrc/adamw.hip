@@ -18,6 +18,9 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+#include <new>
+
 #include "api_checks.h"
 #include "blocks.h"
 
@@ -317,6 +320,39 @@ int check_adamw(const llmq_adamw_tensor* t, int64_t count, int64_t& pieces) {
     return LLMQ_OK;
 }
 
+// Whether an array that a step writes shares memory with another one of the plan: its workgroups run in any order.  (Absmax words may be shared; gradients are only read.)
+int check_apart(const llmq_adamw_tensor* t, int64_t count) {
+    struct Range { uintptr_t first, end; bool written; };
+    Range* const r = new (std::nothrow) Range[(size_t)count * 7];
+    if (!r) return LLMQ_ERR_WORKSPACE;
+    Range* last = r;
+    auto add = [&](const void* p, int64_t bytes, bool written) {
+        if (p) *last++ = Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written};
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const llmq_adamw_tensor& x = t[i];
+        const bool codes = (x.flags & LLMQ_ADAMW_STATES_8BIT) != 0;
+        const int64_t moment = codes ? x.n : 4 * x.n, scales = (x.n + 127) / 128;
+        add(x.w_bf16, 2 * x.n, true);
+        add(x.w_f32, 4 * x.n, true);
+        add(x.grad, x.flags & LLMQ_ADAMW_GRAD_F32 ? 4 * x.n : 2 * x.n, false);
+        add(x.m, moment, true);
+        add(x.v, moment, true);
+        add(codes ? x.m_scale : nullptr, scales, true);
+        add(codes ? x.v_scale : nullptr, scales, true);
+    }
+    std::sort(r, last, [](const Range& a, const Range& b) { return a.first < b.first; });
+    uintptr_t end = 0, written_end = 0;                      // of all ranges so far, of the written ones
+    int st = LLMQ_OK;
+    for (const Range* p = r; p < last; ++p) {
+        if (p->first < (p->written ? end : written_end)) st = LLMQ_ERR_VALUE;
+        end = std::max(end, p->end);
+        if (p->written) written_end = std::max(written_end, p->end);
+    }
+    delete[] r;
+    return st;
+}
+
 size_t adamw_table(int64_t count) { return round256((size_t)count * sizeof(llmq::AdamWTensor)); }
 
 }  // namespace
@@ -331,7 +367,8 @@ size_t llmq_adamw_plan_bytes(const llmq_adamw_tensor* tensors, int64_t count) {
 int llmq_adamw_plan(const llmq_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes, int64_t info[4]) {
     if (!plan || !info) return LLMQ_ERR_NULL;
     int64_t pieces = 0;
-    const int st = check_adamw(tensors, count, pieces);
+    int st = check_adamw(tensors, count, pieces);
+    if (st == LLMQ_OK) st = check_apart(tensors, count);
     if (st != LLMQ_OK) return st;
     if (plan_bytes < adamw_table(count) + (size_t)pieces * sizeof(llmq::AdamWPiece)) return LLMQ_ERR_WORKSPACE;
     memset(plan, 0, adamw_table(count));

@@ -147,7 +147,7 @@ const char* llmq_status_string(int status) {
         case LLMQ_ERR_WORKSPACE: return "workspace too small";
         case LLMQ_ERR_DEVICE: return "HIP launch failed";
         case LLMQ_ERR_FLAGS: return "unknown flag bits";
-        case LLMQ_ERR_VALUE: return "a number is out of range";
+        case LLMQ_ERR_VALUE: return "a number is out of range, or arrays overlap that must not";
         default: return "unknown status";
     }
 }

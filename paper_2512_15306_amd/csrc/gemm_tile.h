@@ -689,16 +689,16 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     const int sc_voff = 8 * (lane & 15);
     // offset of a block's codes in a K step (a tile may reach over the last group of 128 rows: what is read there, codes of another step or zeros, goes to rows that do not exist)
     auto code_offset = [](int block) { return (block >> 3) * 128 + (block & 7); };
-    auto request_operand = [&](auto three, auto& words, __amdgpu_buffer_rsrc_t rs, int block, int at) __attribute__((always_inline)) {
+    auto request_operand = [&](auto three, auto& words, __amdgpu_buffer_rsrc_t rs, int block, unsigned at) __attribute__((always_inline)) {
         constexpr int W = sizeof(words) / sizeof(int);
         if constexpr (decltype(three)::value) {
 #pragma unroll
-            for (int p = 0; p < W; ++p) words[p] = (int)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, sc_voff, at + code_offset(block + 2 * p), 0);
+            for (int p = 0; p < W; ++p) words[p] = (int)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, sc_voff, (int)(at + code_offset(block + 2 * p)), 0);
         } else if constexpr (W == 2) {
-            const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rs, sc_voff, at + code_offset(block), 0));
+            const v2i v = __builtin_bit_cast(v2i, __builtin_amdgcn_raw_buffer_load_b64(rs, sc_voff, (int)(at + code_offset(block)), 0));
             words[0] = v[0], words[1] = v[1];
         } else {
-            words[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rs, sc_voff, at + code_offset(block), 0);
+            words[0] = (int)__builtin_amdgcn_raw_buffer_load_b32(rs, sc_voff, (int)(at + code_offset(block)), 0);
         }
     };
     auto request_scales = [&](auto& sc, int step) __attribute__((always_inline)) {

@@ -659,8 +659,8 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
                           int64_t dqkv_stride, float* dwq, float* dwk, int accumulate, int fmt, float* d_amax, float* d_scale, void* ws, size_t ws_bytes,
                           void* stream) {
     if (!dq_bf16 || !dk_bf16 || !dqkv_bf16 || !wq_bf16 != !wk_bf16 || (rot > 0 && (!d_positions || !d_inv_freq)) || (d_scale && !d_amax)) return LLMQ_ERR_NULL;
-    const bool norm = wq_bf16 != nullptr, sums = norm && (dwq || dwk);
-    if (norm && (!qkv_bf16 || !rstd)) return LLMQ_ERR_NULL;
+    const bool norm = wq_bf16 != nullptr, sums = dwq || dwk;
+    if (norm ? !qkv_bf16 || !rstd : sums) return LLMQ_ERR_NULL;
     if ((sums || d_amax) && !ws) return LLMQ_ERR_NULL;
     const int st = check_qk(M, Hq, Hkv, D, rot, interleaved);
     if (st != LLMQ_OK) return st;

@@ -61,6 +61,7 @@ def test_query_and_key_calls_refuse():
                                        a["rot"], a["inter"], a["dx"], a["dxs"], a["dwq"], a["dwk"], 0, a["fmt"], a["amax"], a["scale"], a["ws"], ctypes.c_size_t(a["bytes"]), None)
 
     assert bwd(dq=None) == bwd(dk=None) == bwd(dx=None) == bwd(wk=None) == bwd(x=None) == bwd(rstd=None) == bwd(pos=None) == bwd(ws=None) == bwd(amax=None) == -1      # (a scale without absmax)
+    assert bwd(wq=None, wk=None) == bwd(wq=None, wk=None, dwq=None) == bwd(wq=None, wk=None, dwk=None) == -1 and bwd(wq=None, wk=None, dwq=None, dwk=None, bytes=0) == -5      # sums without a norm
     assert bwd(M=0) == bwd(dqs=255) == bwd(dks=127) == bwd(dvs=127) == bwd(xs=511) == bwd(dxs=511) == bwd(rot=66) == -2
     assert bwd(fmt=2) == -4 and bwd(bytes=b["bytes"] - 1) == -5 and bwd(inter=-1) == -7
     assert bwd(ws=P + 8) == bwd(dwq=P + 2) == bwd(dx=ODD) == bwd(dv=ODD) == bwd(amax=P + 2) == -3
@@ -68,7 +69,9 @@ def test_query_and_key_calls_refuse():
 
 
 def entry(**o):
-    e = llmq._AdamWTensor(w_bf16=P, w_f32=P, grad=P, m=P, v=P, n=10)
+    """Arrays that lie apart, those of one entry from those of another too"""
+    entry.at = getattr(entry, "at", P) + (1 << 24)
+    e = llmq._AdamWTensor(n=10, **{name: entry.at + (k << 20) for k, name in enumerate(("w_bf16", "w_f32", "grad", "m", "v"))})
     for k, v in o.items():
         setattr(e, k, v)
     return e
@@ -82,7 +85,7 @@ def plan_of(*entries):
 
 
 def test_plans():
-    status, table, info = plan_of(entry(n=4096), entry(n=4097, first_counter=9, flags=llmq.ADAMW_STATES_8BIT, m_scale=P, v_scale=P), entry(n=1, d_amax=P))
+    status, table, info = plan_of(entry(n=4096), entry(n=4097, first_counter=9, flags=llmq.ADAMW_STATES_8BIT, m_scale=P, v_scale=2 * P), entry(n=1, d_amax=P))
     assert status == 0 and info == [3, 4, 1, 0] and len(table) == 512 + 4 * 8
     assert [struct.unpack_from("ii", table, 512 + 8 * k) for k in range(4)] == [(0, 0), (1, 0), (1, 1), (2, 0)]
     assert plan_of(entry())[2][2] == 0
@@ -101,6 +104,24 @@ def test_plans():
     assert L.llmq_adamw_step(P + 8, info, words, None, None, None) == L.llmq_adamw_step(P, info, None, P + 2, None, None) == -3
     info[1] = 0
     assert L.llmq_adamw_step(P, info, words, None, None, None) == -2
+
+
+def test_plans_of_arrays_that_overlap():
+    a, b = entry(n=1000), entry(n=1000)
+    assert plan_of(a, b)[0] == 0 and plan_of(a, a)[0] == -8
+    bits8 = dict(flags=llmq.ADAMW_STATES_8BIT, m_scale=3 * P, v_scale=4 * P)
+    for shared in (dict(w_bf16=a.w_bf16), dict(w_f32=a.w_f32 + 3984), dict(m=a.v + 3984), dict(v=a.v - 3984), dict(grad=a.w_bf16 + 1984), dict(w_bf16=a.grad + 1984), dict(w_bf16=a.w_f32, w_f32=None),
+                   dict(bits8, m_scale=a.m + 3999), dict(bits8, v_scale=a.m - 7), dict(bits8, v_scale=3 * P + 7), dict(bits8, m=a.m - 992)):
+        for order in ((a, entry(n=1000, **shared)), (entry(n=1000, **shared), a)):
+            assert plan_of(*order)[0] == -8, shared
+    for apart in (dict(w_f32=a.w_f32 + 4000), dict(v=a.v - 4000), dict(grad=a.grad + 16), dict(w_bf16=a.grad + 2000), dict(w_bf16=a.grad - 2000), dict(bits8, v_scale=a.m - 8), dict(bits8, v_scale=3 * P + 8),
+                  dict(bits8, m=a.m - 1008), dict(m_scale=a.m, v_scale=a.m), dict(d_amax=P)):
+        for order in ((a, entry(n=1000, **apart)), (entry(n=1000, **apart), a)):
+            assert plan_of(*order)[0] == 0, apart
+    assert plan_of(entry(d_amax=P), entry(d_amax=P))[0] == 0
+    assert plan_of(entry(w_f32=None, m=a.m), entry(grad=a.m))[0] == plan_of(entry(n=1, m=a.grad, v=a.grad))[0] == -8
+    many = [entry(n=1 + 997 * k % 5000) for k in range(500)]
+    assert plan_of(*many)[0] == 0 and plan_of(*many, entry(v=many[250].v))[0] == -8
 
 
 def test_the_numbers_of_a_step():
