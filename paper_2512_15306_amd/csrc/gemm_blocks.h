@@ -18,9 +18,10 @@ struct GemmBlocksTuning : GemmTuning { static constexpr bool kBlockScales = true
 struct GemmBlocksDeepTuning : GemmDeepTuning { static constexpr bool kBlockScales = true; };
 struct GemmBlocksDeepWideTuning : GemmDeepWideTuning { static constexpr bool kBlockScales = true; };
 
+// R x C: the whole contraction, whose scales and output rows are laid out by them; rows x cols: the part of it that the pointers begin (all of it, except for strips)
 struct BlocksOperands {
     const uint8_t *A, *sA, *B, *sB;
-    int64_t R, C, T;
+    int64_t R, C, T, rows, cols;
     void* c;
     int accumulate;
     unsigned* amax;
@@ -28,7 +29,7 @@ struct BlocksOperands {
 
 template <int FA, int FB, int NI, int NJ, int EDGE>
 static void launch_blocks_tile(const BlocksOperands& p, hipStream_t stream, int num_cus) {
-    const int tiles_r = (int)((p.R + 64 * NI - 1) / (64 * NI)), tiles_c = (int)((p.C + 64 * NJ - 1) / (64 * NJ));
+    const int tiles_r = (int)((p.rows + 64 * NI - 1) / (64 * NI)), tiles_c = (int)((p.cols + 64 * NJ - 1) / (64 * NJ));
     SplitPlan plan{};
     plan.n_whole = tiles_r * tiles_c;
     const int grid = ((plan.n_whole + kXcds - 1) / kXcds) * kXcds, slots = resident_slots(num_cus, NI, NJ);
@@ -227,15 +228,29 @@ static void launch_blocks_few(const BlocksOperands& p, hipStream_t stream) {
 }
 
 // What a contraction takes: the kernel for few rows, else small tiles of `side`, else the tile, else the generic kernel (tile.ni == 0).
+// strip_rows / strip_cols: so many of the last rows or columns are a launch of their own, of whole `strip` tiles.
 struct BlocksPlan {
     bool few;
     int side;
     TilePlan tile;
+    int64_t strip_rows, strip_cols;
+    TilePlan strip;
 };
 
 // Launches the kernel of the plan; gemm_blocks_*.hip instantiate it for a pair of formats each.
 template <int FA, int FB>
 void launch_blocks(const BlocksOperands& p, const BlocksPlan& plan, hipStream_t stream, int num_cus) {
+    if (plan.strip_rows || plan.strip_cols) {
+        // (whole tiles from rows and columns that are multiples of 128 on, so the strip's scales are the rest of each K step's)
+        const int64_t r = plan.strip_rows ? p.R - plan.strip_rows : 0, c = plan.strip_cols ? p.C - plan.strip_cols : 0;
+        BlocksOperands first = p, strip = p;
+        if (r) first.rows = r, strip.rows = plan.strip_rows;
+        if (c) first.cols = c, strip.cols = plan.strip_cols;
+        strip.A += r * p.T, strip.sA += r, strip.B += c * p.T, strip.sB += c, strip.c = static_cast<uint16_t*>(p.c) + r * p.C + c;
+        launch_blocks<FA, FB>(first, BlocksPlan{false, 0, plan.tile, 0, 0, {}}, stream, num_cus);
+        launch_blocks<FA, FB>(strip, BlocksPlan{false, 0, plan.strip, 0, 0, {}}, stream, num_cus);
+        return;
+    }
     if (plan.few) {
         // Two blocks of columns to a workgroup read A half as often; where that leaves half of the CUs without one, or chunks go through registers (twice as many of them), one.
         // R x C x T, one / two, microseconds: 16 x 4608 x 3584 6.9 / 5.8, 26 x 5227 x 11488 22.2 / 16.3;  20 x 3492 x 16864 17.9 / 22.5, 5 x 2589 x 4720 6.6 / 7.9;

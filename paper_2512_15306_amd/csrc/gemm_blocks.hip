@@ -19,8 +19,44 @@ static bool takes_few(int64_t R, int64_t C, int64_t T) {
 
 // The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
 // times by a few percent.  Tiles with sides of 320 are not built: they have no registers left for the scales.
+// Whether full rounds of 256 x 256 tiles and a strip of the last rows or columns, in tiles of its own, take less time together than `least`: a round of a few large
+// tiles takes nearly as long as a full one, although less than the model says where the power of the idle CUs goes to the others: hence a margin of 7 %.  All sides multiples of
+// 128, T too, 8 K steps at least.  R x C x T, one launch / two, microseconds: 3584 x 18944 x 8192 (4.05 rounds) 458 / 428, 11264 x 1536 x 11264 214 / 177, 3456 x 15616 x 11648
+// 521 / 475, 6272 x 11264 x 1280 114 / 103, 9984 x 5120 x 2048 110 / 104, 16000 x 13312 x 1664 402 / 403, 11008 x 13184 x 5120 541 / 552;  10880 x 1792 x 896 31.1 / 33.4.  Of shapes of
+// 512 to 19072 rows and columns, T of 512 to 12288, a fifth is cut, and takes 1.8 % less time on average.
+// LLMQ_BLOCKS_STRIP=0, rN, cN (tests): no strip, or one of N rows or columns wherever it leaves whole tiles.
+static void cut_strip(BlocksPlan& plan, int64_t R, int64_t C, int64_t steps, bool accumulate, int num_cus, double least) {
+    const char* const forced = tuning_env("LLMQ_BLOCKS_STRIP");
+    if (forced ? forced[0] == '0' : steps < 8) return;
+    const int64_t slots = resident_slots(num_cus, 4, 4);
+    for (const bool by_rows : {false, true}) {
+        const int64_t across = by_rows ? C : R, along = by_rows ? R : C, tiles_across = across / 256, rounds = tiles_across * (along / 256) / slots;
+        if (across % 256 != 0) continue;
+        int64_t first = rounds * slots / tiles_across * 256;
+        if (forced) first = forced[0] == (by_rows ? 'r' : 'c') ? along - atoi(forced + 1) : 0;
+        const int64_t strip = along - first, tiles = tiles_across * (first / 256);
+        if (first <= 0 || first % 256 != 0 || strip <= 0 || strip % 128 != 0 || tiles > kMaxWorkgroups) continue;
+        // the strip's tile and time
+        double us = 0.0;
+        TilePlan tile{};
+        for (int i = 4; i >= 2; --i)
+            for (int j = 4; j >= 2; --j) {
+                if ((by_rows ? strip : across) % (64 * i) != 0 || (by_rows ? across : strip) % (64 * j) != 0) continue;
+                const int64_t n = across * strip / (4096 * i * j);
+                const double t = i == 2 && j == 2 && n <= resident_slots(num_cus, 2, 2) / 2 ? 4.5 + 0.39 * (double)steps             // (four LDS stages)
+                                                                                            : tile_us({i, j, kNoEdge}, n, steps, accumulate, false, resident_slots(num_cus, i, j));
+                if (us == 0.0 || t < us) { us = t; tile = TilePlan{i, j, kNoEdge}; }
+            }
+        us += tile_us({4, 4, kNoEdge}, tiles, steps, accumulate, false, slots);
+        if (forced || us < least) {
+            least = us;
+            plan.tile = TilePlan{4, 4, kNoEdge}, plan.strip = tile, plan.strip_rows = by_rows ? strip : 0, plan.strip_cols = by_rows ? 0 : strip;
+        }
+    }
+}
+
 static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, bool with_amax, int num_cus) {
-    BlocksPlan plan{false, 0, {0, 0, kNoEdge}};
+    BlocksPlan plan{false, 0, {0, 0, kNoEdge}, 0, 0, {}};
     const int64_t steps = (T + BK - 1) / BK, rounded = ((R > C ? R : C) + 127) / 128 * 128;
     // 32-bit offsets from the first row of a tile, of operands, scales and output; sixteen bytes in every row of an operand
     if (T < 16 || T >= (1ll << 22) || C >= (1ll << 22) || steps * rounded >= 0x7FFFF000ll) return plan;
@@ -38,11 +74,15 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
         }
         if (e[0] == '0') return plan;
     }
+    const bool ragged = R % 128 != 0 || C % 128 != 0 || T % BK != 0;
+    if (tuning_env("LLMQ_BLOCKS_STRIP") && !ragged) {
+        cut_strip(plan, R, C, steps, accumulate, num_cus, 0.0);
+        if (plan.tile.ni) return plan;
+    }
     plan.few = takes_few(R, C, T);
     if (plan.few) return plan;
     plan.side = aligned_rows ? takes_mini(R, C, T, false, false, accumulate, with_amax, false, num_cus) : 0;
     if (plan.side) return plan;
-    const bool ragged = R % 128 != 0 || C % 128 != 0 || T % BK != 0;
     if (ragged && generic_is_faster(R, C, T, false, false, accumulate, with_amax, false, num_cus)) return plan;
     if (((R + 127) / 128) * ((C + 127) / 128) <= resident_slots(num_cus, 2, 2) / 2) { plan.tile = form(2, 2); return plan; }
     double best_us = 0.0;
@@ -55,6 +95,7 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
             const double us = tile_us(p, tiles, steps, accumulate, C % 8 != 0, resident_slots(num_cus, ni, nj));
             if (plan.tile.ni == 0 || us < best_us) { plan.tile = p; best_us = us; }
         }
+    if (!ragged) cut_strip(plan, R, C, steps, accumulate, num_cus, 0.93 * best_us);
     return plan;
 }
 
@@ -74,7 +115,7 @@ extern "C" int llmq_fp8_gemm_blocks(const uint8_t* A, const uint8_t* sA, int fmt
     hipStream_t s = static_cast<hipStream_t>(stream);
     unsigned* amax = reinterpret_cast<unsigned*>(d_amax_c);
     if (amax) llmq::launch_gemm_amax_reset(amax, s);
-    const llmq::BlocksOperands p{A, sA, B, sB, R, C, T, c_bf16, accumulate != 0, amax};
+    const llmq::BlocksOperands p{A, sA, B, sB, R, C, T, R, C, c_bf16, accumulate != 0, amax};
     if (fmtA == LLMQ_E4M3 && fmtB == LLMQ_E4M3) llmq::launch_blocks<0, 0>(p, plan, s, cus);
     else if (fmtA == LLMQ_E5M2 && fmtB == LLMQ_E4M3) llmq::launch_blocks<1, 0>(p, plan, s, cus);
     else if (fmtA == LLMQ_E4M3 && fmtB == LLMQ_E5M2) llmq::launch_blocks<0, 1>(p, plan, s, cus);

@@ -192,6 +192,35 @@ def test_every_kernel(R, C, T, tile, accumulate, monkeypatch):
         assert amax.item() == c.abs().max().item()
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("R,C,T,strip", [(384, 256, 128, "r128"), (256, 384, 640, "c128"), (768, 512, 384, "r256"), (512, 1152, 256, "c640"), (896, 256, 1152, "r384"), (256, 896, 2304, "c384"),
+                                         (512, 768, 128, "c512"), (2048, 256, 256, "r1792")])
+def test_strips(R, C, T, strip, accumulate, monkeypatch):
+    """The last rows or columns in a launch of their own: the bytes of one launch, absmax too"""
+    qa, sa, qb, sb, va, vb = operands(R, C, T, 1, 0, R + T, 1)
+    old = torch.randn(R, C, device=DEV).to(torch.bfloat16)
+    out = {}
+    for how in ("0", strip):
+        monkeypatch.setenv("LLMQ_BLOCKS_STRIP", how)
+        c, amax = old.clone(), torch.zeros(1, device=DEV)
+        llmq.llmq_fp8_gemm_blocks(qa, sa, 1, qb, sb, 0, c, accumulate, amax)
+        assert_close(c, va, vb, T, old if accumulate else None)
+        assert amax.item() == c.abs().max().item()
+        out[how] = c
+    assert torch.equal(out["0"].view(torch.int16), out[strip].view(torch.int16))
+
+
+def test_a_contraction_that_is_cut_gives_the_bytes_of_one_launch(monkeypatch):
+    """257 tiles of 256 x 256 and 16 K steps: a strip by the rule on sizes, no switch"""
+    R, C, T = 257 * 256, 256, 2048
+    qa, sa, qb, sb, _, _ = operands(R, C, T, 0, 0, 3, 1)
+    outs = [torch.empty(R, C, device=DEV, dtype=torch.bfloat16) for _ in range(2)]
+    llmq.llmq_fp8_gemm_blocks(qa, sa, 0, qb, sb, 0, outs[0])
+    monkeypatch.setenv("LLMQ_BLOCKS_STRIP", "0")
+    llmq.llmq_fp8_gemm_blocks(qa, sa, 0, qb, sb, 0, outs[1])
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
+
+
 @pytest.mark.parametrize("fa,fb", [(0, 0), (1, 0), (0, 1), (1, 1)])
 @pytest.mark.parametrize("R,C,T", [(16, 40, 200), (128, 256, 384), (512, 768, 1152), (300, 700, 272), (300, 268, 1001)])
 def test_scales_of_rows_alone_give_the_bytes_of_the_contraction_without_them(R, C, T, fa, fb, monkeypatch):
