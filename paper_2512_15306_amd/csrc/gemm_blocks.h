@@ -7,6 +7,9 @@
 // the instruction without them.  Scales that are ordinary numbers would need a second set of accumulators, and a multiply-add of every output in every K step:
 // 4 vector instructions behind each MFMA.  A product of a code and a power of two is exact, so nothing is rounded but the sums.
 //
+// 8192 x 4608 x 3584 in E4M3: 118 us, 2.3 PFLOP/s (107 to 115 with one scale an operand); 3584 x 18944 x 8192, E5M2 by E4M3, added to the output: 430 us, 2.6 PFLOP/s; bound by the power
+// that the matrix instructions and the operands' way to them take.
+//
 // The kernels are those of the tensor-wise contraction (gemm_tile.h, gemm_small.h) with the scales of a K step in two to four registers.  Where a row's
 // block was 128 rows high, every row has a copy of its code: 1/128 of a byte per operand byte, and one form of operand instead of three.
 #pragma once

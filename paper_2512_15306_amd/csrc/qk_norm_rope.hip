@@ -11,6 +11,9 @@
 // values a lane in two pieces of 8 bytes that hold both halves of its pairs: no exchange between lanes but the sums of a head.
 // The sums of dw stay in a lane's registers over all tokens and heads of its wave; each workgroup leaves one row of them, which a second kernel adds
 // in the order of the workgroups (no atomics).
+//
+// Heads of 128 values.  Forward: 8192 tokens of 28 + 4 heads (135 MB) 26 us, 5.2 TB/s; 32 tokens 4 us, one trip to memory and back behind the angles.  Backward: 8192 tokens of
+// 40 + 8 (337 MB) 76 us, 4.4 TB/s, of which the second kernel's 4; 1777 tokens of 9 + 3 heads of 80 (12 MB) 12 us: two launches, each a chain of waits.
 #include "api_checks.h"
 #include "llmq_device.h"
 
