@@ -62,9 +62,9 @@ static void launch_blocks_tile(const BlocksOperands& p, hipStream_t stream, int 
     launch_form(GemmBlocksTuning{});
 }
 
-// ---- Few rows: 16 RB of them at most (decoding, one row a sequence).
+// ---- Few rows: 16 RB of them (decoding, one row a sequence), or groups of so many along the grid's second dimension.
 //
-// What there is to do is to read B once.  The small tiles have a workgroup for every 32 columns, whose waves meet at two barriers every four K steps; here a workgroup has
+// What there is to do is to read B once (for every group).  The small tiles have a workgroup for every 32 columns, whose waves meet at two barriers every four K steps; here a workgroup has
 // 16 CB columns, its four waves take every fourth K step each, with LDS of their own, and meet once, to add their sums in the order of the waves.  A wave keeps
 // the operands of four of its steps on their way (four slots of LDS): slabs of 16 rows x 128 bytes with eight lanes to a row, as in the tile kernel, and for the same reason
 // through LDS: loads straight into the layout of the matrix instruction have 16 rows side by side, which the memory pipeline takes 16 bytes at a time (80 cycles for a load of
@@ -82,15 +82,15 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
     __shared__ __attribute__((aligned(1024))) uint8_t s_2[kFewWaves * kSlot];
     __shared__ __attribute__((aligned(1024))) uint8_t s_3[kFewWaves * kSlot];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int c0 = (int)blockIdx.x * (16 * CB), steps = (T + BK - 1) / BK, mine = (steps - wave + kFewWaves - 1) / kFewWaves;      // steps wave, wave + 4, ...
-    const int rows_a = R < 16 * RB ? R : 16 * RB, rows_b = Cn - c0 < 16 * CB ? Cn - c0 : 16 * CB;
-    const uint8_t* const b0 = B + (int64_t)c0 * T;
-    const __amdgpu_buffer_rsrc_t rsA = make_rsrc(A, (unsigned)((int64_t)rows_a * T)), rsB = make_rsrc(b0, (unsigned)((int64_t)rows_b * T));
+    const int r0 = (int)blockIdx.y * (16 * RB), c0 = (int)blockIdx.x * (16 * CB), steps = (T + BK - 1) / BK, mine = (steps - wave + kFewWaves - 1) / kFewWaves;      // steps wave, wave + 4, ...
+    const int rows_a = R - r0 < 16 * RB ? R - r0 : 16 * RB, rows_b = Cn - c0 < 16 * CB ? Cn - c0 : 16 * CB;
+    const uint8_t *const a0 = A + (int64_t)r0 * T, *const b0 = B + (int64_t)c0 * T;
+    const __amdgpu_buffer_rsrc_t rsA = make_rsrc(a0, (unsigned)((int64_t)rows_a * T)), rsB = make_rsrc(b0, (unsigned)((int64_t)rows_b * T));
     const int pitchA = (R + 127) & ~127, pitchB = (Cn + 127) & ~127;
     const __amdgpu_buffer_rsrc_t rsSA = make_rsrc(sA, (unsigned)(steps * pitchA)), rsSB = make_rsrc(sB, (unsigned)(steps * pitchB));
     int code_a[RB], code_b[CB];
 #pragma unroll
-    for (int i = 0; i < RB; ++i) code_a[i] = (int)block_scale_offset(16 * i + (lane & 15), 0, R);
+    for (int i = 0; i < RB; ++i) code_a[i] = (int)block_scale_offset(r0 + 16 * i + (lane & 15), 0, R);
 #pragma unroll
     for (int j = 0; j < CB; ++j) code_b[j] = (int)block_scale_offset(c0 + 16 * j + (lane & 15), 0, Cn);
     // a wave's n-th step in a slot: slabs of A, then of B, load p rows 8 p .. of them
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
                 const int rows = of_a ? rows_a : rows_b;
                 held.c[p] = v4u{0, 0, 0, 0};
                 if (there && row < rows) {
-                    const uint8_t* src = (of_a ? A : b0) + (int64_t)row * T + k;
+                    const uint8_t* src = (of_a ? a0 : b0) + (int64_t)row * T + k;
                     if (k + 16 <= T) held.c[p] = *reinterpret_cast<const v4u_any*>(src);
                     else held.c[p] = load16_upto(src, T - k);
                 }
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
         v4f y = s_sum[block * kWave + lane];
 #pragma unroll
         for (int w = 1; w < kFewWaves; ++w) y += s_sum[(w * (RB * CB) + block) * kWave + lane];
-        const int r = 16 * (block / CB) + (lane & 15), c = c0 + 16 * (block % CB) + (lane >> 4) * 4, left = Cn - c;
+        const int r = r0 + 16 * (block / CB) + (lane & 15), c = c0 + 16 * (block % CB) + (lane >> 4) * 4, left = Cn - c;
         if (r >= R || left <= 0) continue;
         uint16_t* dst = C + (int64_t)r * Cn + c;
         if (Cn % 4 == 0) {
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
 template <int FA, int FB, int RB, int CB>
 static void launch_blocks_few(const BlocksOperands& p, hipStream_t stream) {
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.C + 16 * CB - 1) / (16 * CB))), dim3(kFewWaves * kWave), 0, stream, p.A, p.sA, p.B, p.sB, reinterpret_cast<uint16_t*>(p.c), (int)p.R, (int)p.C,
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.C + 16 * CB - 1) / (16 * CB)), (unsigned)((p.R + 16 * RB - 1) / (16 * RB))), dim3(kFewWaves * kWave), 0, stream, p.A, p.sA, p.B, p.sB, reinterpret_cast<uint16_t*>(p.c), (int)p.R, (int)p.C,
                            (int)p.T, p.accumulate, p.amax);
     };
     if (p.T % 16 == 0) launch(gemm_blocks_few_kernel<FA, FB, RB, CB, true>);

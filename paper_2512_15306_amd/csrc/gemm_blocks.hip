@@ -9,16 +9,18 @@ namespace llmq {
 // it, R x C x T, microseconds: 1 x 4608 x 3584 8.2 / 5.8, 16 x 1024 x 8192 13.8 / 7.3, 16 x 18944 x 3584 23.8 / 19.9, 5 x 39782 x 6960 80.5 / 50.6, 32 x 512 x 512 4.2 / 3.1,
 // 5 x 700 x 333 9.9 / 3.2, 9 x 5305 x 4643 40.2 / 17.0, 2 x 11141 x 12797 122 / 81;  and where they are faster 3 x 26124 x 1632 12.6 / 15.2, 28 x 20369 x 1120 10.9 / 12.8,
 // 3 x 9669 x 480 4.8 / 5.0, 2 x 6136 x 128 2.9 / 3.4, 2 x 25206 x 2203 26.4 / 31.8.
-// LLMQ_FEW=0 / 1 (tests): never, or for up to 32 rows always.
-static bool takes_few(int64_t R, int64_t C, int64_t T) {
-    if (R > 32) return false;
-    if (const char* e = tuning_env("LLMQ_FEW")) return atoi(e) != 0;
+// Rows that are no whole 16-byte chunks leave other contractions of few outputs to 128 x 128 tiles or to bytes one by one: those take this kernel too, in groups of 32 rows, where two
+// rounds of its workgroups at most are the faster ones by the fitted times below.  The others / it: 99 x 406 x 612 11.9 / 5.4, 500 x 500 x 333 13.3 / 8.2, 100 x 512 x 9999 63.6 / 41.5,
+// 1 x 333 x 20 6.2 / 4.0, 300 x 300 x 127 7.5 / 5.1;  145 x 2091 x 890 15.3 / 17.6, 777 x 333 x 1999 24.3 / 28.7, 1000 x 1000 x 200 8.7 / 24.4.
+// LLMQ_FEW=0 / 1 (tests): never, or for up to 4096 rows always.
+static bool takes_few(int64_t R, int64_t C, int64_t T, int num_cus) {
+    if (const char* e = tuning_env("LLMQ_FEW")) return atoi(e) != 0 && R <= 4096;
     const int64_t steps = (T + BK - 1) / BK;
-    return steps > 1 && (C <= 8192 || steps >= (T % 16 == 0 ? 20 : 40));
+    if (R <= 32 && steps > 1 && (C <= 8192 || steps >= (T % 16 == 0 ? 20 : 40))) return true;
+    const int64_t rounds = ((R + 31) / 32 * ((C + 15) / 16) + num_cus - 1) / num_cus;
+    return T % 16 != 0 && rounds <= (steps > 1 ? 2 : 1) && 1.9 + 2.6 * (double)rounds + (rounds == 1 ? 0.39 : 0.95) * (double)steps < 5.5 + 0.85 * (double)steps + (C % 8 != 0 ? 2.5 : 0.0);
 }
 
-// The models of the tensor-wise contraction (tile_us, takes_mini), whose kernels these are: over the cases they were compared on the scales change the
-// times by a few percent.  Tiles with sides of 320 are not built: they have no registers left for the scales.
 // Whether full rounds of 256 x 256 tiles and a strip of the last rows or columns, in tiles of its own, take less time together than `least`: a round of a few large
 // tiles takes nearly as long as a full one, although less than the model says where the power of the idle CUs goes to the others: hence a margin of 7 %.  All sides multiples of
 // 128, T too, 8 K steps at least.  R x C x T, one launch / two, microseconds: 3584 x 18944 x 8192 (4.05 rounds) 458 / 428, 11264 x 1536 x 11264 214 / 177, 3456 x 15616 x 11648
@@ -79,7 +81,7 @@ static BlocksPlan plan_blocks(int64_t R, int64_t C, int64_t T, bool accumulate, 
         cut_strip(plan, R, C, steps, accumulate, num_cus, 0.0);
         if (plan.tile.ni) return plan;
     }
-    plan.few = takes_few(R, C, T);
+    plan.few = takes_few(R, C, T, num_cus);
     if (plan.few) return plan;
     plan.side = aligned_rows ? takes_mini(R, C, T, false, false, accumulate, with_amax, false, num_cus) : 0;
     if (plan.side) return plan;

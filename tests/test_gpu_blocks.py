@@ -244,9 +244,10 @@ def test_scales_of_rows_alone_give_the_bytes_of_the_contraction_without_them(R, 
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
-@pytest.mark.parametrize("R,C,T", [(1, 16, 16), (1, 5, 200), (3, 50, 131), (16, 64, 2048), (9, 4200, 640), (16, 100, 1999), (17, 33, 4112), (32, 4099, 512), (25, 4096, 272), (31, 1000, 777), (2, 40, 20000)])
+@pytest.mark.parametrize("R,C,T", [(1, 16, 16), (1, 5, 200), (3, 50, 131), (16, 64, 2048), (9, 4200, 640), (16, 100, 1999), (17, 33, 4112), (32, 4099, 512), (25, 4096, 272), (31, 1000, 777), (2, 40, 20000),
+                                   (33, 40, 129), (100, 70, 1999), (130, 16, 612), (200, 333, 77), (64, 4200, 512), (257, 48, 1000), (1000, 33, 19)])
 def test_few_rows(R, C, T, accumulate, monkeypatch):
-    """The kernel for few rows, one and two blocks of columns to a workgroup, whole chunks and any, fewer steps than waves and many more."""
+    """The kernel for few rows, one and two blocks of columns to a workgroup, whole chunks and any, fewer steps than waves and many more, groups of rows."""
     monkeypatch.setenv("LLMQ_FEW", "1")
     for fa, fb in ((0, 0), (1, 0), (0, 1), (1, 1)):
         qa, sa, qb, sb, va, vb = operands(R, C, T, fa, fb, R + T, 1 if C % 2 else 128)
