@@ -16,8 +16,8 @@
 // and a root above zero is kept above zero: a moment that came up beside a root that went to zero would make a step without bound.
 // Weights in BF16 without a master copy can be rounded the same way, for the same reason.
 //
-// 233 million elements in 8 tensors, moments in 8 bits and a master copy (3.74 GB): 680 us, 5.5 TB/s; 12.5 million in 96 tensors of 128 to 520662 elements, moments in binary32
-// (351 MB): 68 us, 5.2 TB/s.
+// 233 million elements in 8 tensors, moments in 8 bits and a master copy (3.74 GB): 650 us, 5.7 TB/s; 12.5 million in 96 tensors of 128 to 520662 elements, moments in binary32
+// (351 MB): 59 us, 5.9 TB/s: a large copy has 5.85.
 #include <math.h>
 #include <string.h>
 
@@ -44,9 +44,10 @@ struct AdamWHyper { float b1, b2, c1, c2, lr_decay, lr_m, root_scale, eps; unsig
 static_assert(sizeof(AdamWHyper) == 4 * LLMQ_ADAMW_HYPER_WORDS, "");
 
 constexpr float kRootMeanBeta = 0.96875f;
-// A lane has four elements of a group, a wave 256 that follow each other, so that every load and store of a wave is one piece of memory; a workgroup's piece of a
-// tensor is several groups one after the other, the next one's loads on their way while one is computed.
-constexpr int kAdamThreads = 256, kAdamLane = 4, kAdamGroup = kAdamThreads * kAdamLane, kAdamTrips = 4, kAdamPiece = kAdamGroup * kAdamTrips;
+// A lane has four elements, a wave 256 that follow each other, so that every load and store of a wave is one piece of memory.  A workgroup's piece of a tensor is no more than that
+// for its four waves: many short workgroups keep more loads on their way than fewer that go through several such groups, also with the next group's loads ahead of the step for
+// the last.  Pieces of 1024 / 4096, microseconds: 255816 elements 4.9 / 9.8, 1.6 million 8.8 / 11.9, 12.5 million in binary32 59.6 / 68.7, 233 million in 8 bits 652 / 676.
+constexpr int kAdamThreads = 256, kAdamLane = 4, kAdamPiece = kAdamThreads * kAdamLane;
 
 // 32 well mixed bits for a counter under a key.  The multipliers are odd numbers from the golden ratio and the square roots of 2 and 3.
 __host__ __device__ inline unsigned mixed_bits(uint64_t counter, unsigned key) {
@@ -247,17 +248,9 @@ __device__ inline unsigned step_of(const AdamWTensor& t, const AdamWHyper& h, fl
 
 template <class K>
 __device__ inline unsigned step_of_piece(const AdamWTensor& t, const AdamWHyper& h, float grad_scale, int64_t at) {
-    Group<K> r[2];
-    unsigned mag = 0;
-    request(t, at, r[0]);
-#pragma unroll
-    for (int k = 0; k < kAdamTrips; ++k) {
-        if (k + 1 < kAdamTrips) request(t, at + kAdamGroup, r[(k + 1) % 2]);
-        const unsigned a = step_of(t, h, grad_scale, at, r[k % 2]);
-        mag = mag > a ? mag : a;
-        at += kAdamGroup;
-    }
-    return mag;
+    Group<K> r;
+    request(t, at, r);
+    return step_of(t, h, grad_scale, at, r);
 }
 
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamWTensor* tensors, const AdamWPiece* pieces, unsigned first, const AdamWHyper by_value, const AdamWHyper* d_hyper,

@@ -86,8 +86,8 @@ def plan_of(*entries):
 
 def test_plans():
     status, table, info = plan_of(entry(n=4096), entry(n=4097, first_counter=9, flags=llmq.ADAMW_STATES_8BIT, m_scale=P, v_scale=2 * P), entry(n=1, d_amax=P))
-    assert status == 0 and info == [3, 4, 1, 0] and len(table) == 512 + 4 * 8
-    assert [struct.unpack_from("ii", table, 512 + 8 * k) for k in range(4)] == [(0, 0), (1, 0), (1, 1), (2, 0)]
+    assert status == 0 and info == [3, 10, 1, 0] and len(table) == 512 + 10 * 8
+    assert [struct.unpack_from("ii", table, 512 + 8 * k) for k in range(10)] == [(0, k) for k in range(4)] + [(1, k) for k in range(5)] + [(2, 0)]
     assert plan_of(entry())[2][2] == 0
     for bad, want in ((dict(grad=None), -1), (dict(m=None), -1), (dict(v=None), -1), (dict(w_bf16=None, w_f32=None), -1), (dict(flags=2), -1), (dict(w_bf16=None, d_amax=P), -1),
                       (dict(n=0), -2), (dict(n=1 << 40), -2), (dict(first_counter=-1), -2), (dict(flags=16), -7), (dict(flags=8), -7), (dict(grad=P + 8), -3), (dict(w_f32=P + 4), -3), (dict(d_amax=P + 2), -3)):
