@@ -12,7 +12,7 @@
 // The sums of dw stay in a lane's registers over all tokens and heads of its wave; each workgroup leaves one row of them, which a second kernel adds
 // in the order of the workgroups (no atomics).
 //
-// Heads of 128 values.  Forward: 8192 tokens of 28 + 4 heads (135 MB) 26 us, 5.2 TB/s; 32 tokens 4 us, one trip to memory and back behind the angles.  Backward: 8192 tokens of
+// Heads of 128 values.  Forward: 8192 tokens of 28 + 4 heads (135 MB) 25.4 us, 5.3 TB/s; 32 tokens 4 us, one trip to memory and back behind the angles.  Backward: 8192 tokens of
 // 40 + 8 (337 MB) 76 us, 4.4 TB/s, of which the second kernel's 4; 1777 tokens of 9 + 3 heads of 80 (12 MB) 12 us: two launches, each a chain of waits.
 #include "api_checks.h"
 #include "llmq_device.h"
@@ -193,7 +193,8 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
     if constexpr (NORM) {
         if (at.there) { unpack(at.weights(a.wq), wq); unpack(at.weights(a.wk), wk); }
     }
-    constexpr int kAtOnce = 4;
+    // (one / two / four passes in a batch, with six, six and five workgroups to a CU: 8192 tokens of 28 + 4 heads of 128 28.0 / 27.4 / 29.0 us, 512 of them 4.9 / 5.2 / 6.0, 2048 12.3 / 11.7 / 11.9)
+    constexpr int kAtOnce = 2;
     for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
         float c[4], s[4];
         at.angles(a.rot ? a.positions[m] : 0, c, s);
@@ -554,7 +555,7 @@ static int launch_qk_fwd(QkArgs a, hipStream_t stream, int cus) {
         if (a.wq) hipLaunchKernelGGL(qk_fwd_any_kernel<true>, grid, dim3(kQkThreads), 0, stream, a);
         else hipLaunchKernelGGL(qk_fwd_any_kernel<false>, grid, dim3(kQkThreads), 0, stream, a);
     } else {
-        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 8 * cus, kQkWaves, cus * 5);
+        const QkGrid g = qk_grid(a.M, (a.Hq + kWave / G - 1) / (kWave / G) + (a.Hkv + kWave / G - 1) / (kWave / G), 8 * cus, kQkWaves, cus * 6);
         a.split = g.split;
         auto launch = [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
