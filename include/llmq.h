@@ -473,8 +473,9 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
  *   grad            BF16, or binary32 with LLMQ_ADAMW_GRAD_F32.
  *   m, v            binary32, zeros before the first step.  LLMQ_ADAMW_STATES_8BIT: one byte each, E4M3 codes of m and of sqrt(v) with m_scale and v_scale [ceil(n / 128)], a
  *                   power-of-two scale for each 128 elements as llmq_quantize_fp8_blocks has them; codes 0 and scales 127 before the first step.  Codes are rounded up or
- *                   down with the probability that keeps the mean (below 2^-6 to the nearest; a root above 0 stays above 0), for beta2 > 31/32 the mean of the root's square, without
- *                   which v would grow by its rounding; up to 31/32 that growth is at most 4 % of v.  A gradient that is not finite makes
+ *                   down with the probability that keeps the mean, to 2^-16 of their distance (but a root above 0 stays above 0: at least the smallest code, 2^-18 to 2^-17 of the block's largest
+ *                   root, so weights whose gradients are below that move less than they would); of a root below 2^-6, and of all for beta2 > 31/32, the mean of its
+ *                   square, without which v would grow by its rounding; up to 31/32 the others' growth is 4 % of v at most.  A gradient that is not finite makes
  *                   its whole block NaN.
  *   d_amax          [1] float or NULL: absmax of the new w_bf16 (canonical NaN as llmq_amax), of all tensors that name the same word: the next quantization of these
  *                   weights then needs no pass of its own (llmq_scale_from_amax).

@@ -12,8 +12,11 @@
 // 16 random bits from a hash of element and step: the same bits on every run.  For the root there are two means to keep.  Its own: then its square comes out larger by the
 // variance, 0.13 % a step on average over the codes (a sixth of the square of the spacing, 1/8 to 1/16), which the average over 1 / (1 - b2) steps multiplies: 2.5 % of v
 // for b2 = 0.95, and without bound from 0.9987 on.  Its square's, by the probability f (2 n + f) / (2 n + 1) for n + f units: v is right for any b2.  The first is what roots
-// get for b2 up to 31/32, the second above.  Below 2^-6 (2^-15 of the block's largest value) codes are rounded to the nearest,
-// and a root above zero is kept above zero: a moment that came up beside a root that went to zero would make a step without bound.
+// get for b2 up to 31/32, the second above.
+// Below 2^-6 (2^-15 of the block's largest value) the codes are as far apart as at 2^-6 and are rounded up or down too: to the nearest, 4 would stay 4 under b1 = 0.9, and a weight whose
+// gradient has stopped would go on by a share of lr a step without end (79 lr in 1000 steps on average, where it is 2.2 rounded so and in exact moments).  There roots keep their square's mean for any b2: by their own,
+// v would come out 10 to 70 % too large (roots of 1 to 4 times the smallest code).  Only a root above zero is kept above zero: a moment that came up beside a root that went to zero would make a step
+// without bound.
 // Weights in BF16 without a master copy can be rounded the same way, for the same reason.
 //
 // 233 million elements in 8 tensors, moments in 8 bits and a master copy (3.74 GB): 650 us, 5.7 TB/s; 12.5 million in 96 tensors of 128 to 520662 elements, moments in binary32
@@ -71,19 +74,40 @@ __device__ inline unsigned max_of_32(unsigned v) {
     return r[0] > r[1] ? r[0] : r[1];
 }
 
-// E4M3 code (its low 8 bits) of a magnitude x with x 2^(127 - scale) <= 448, by 16 random bits.  x is brought to 2^8 times that: the low byte of the exponent
-// and the first three bits of the mantissa is then the code of a normal value, and below 2^-6 the last bits of x + 2^22, which rounds to nearest even at the spacing of those codes.
-// SQUARE: the mean of the code's square is kept instead of its own.
-template <bool SQUARE>
-__device__ inline unsigned code_of(float x, int scale, unsigned rnd) {
-    const float a = __builtin_amdgcn_ldexpf(x, 135 - scale);
-    const unsigned bits = __float_as_uint(a), small = __float_as_uint(a + 4194304.0f);
-    unsigned normal = (bits + (rnd << 4)) >> 20;
-    if constexpr (SQUARE) {
-        const float f = (float)(bits & 0xFFFFFu) * 0x1p-20f, n2 = (float)(16u + 2u * ((bits >> 20) & 7u));
-        normal = (bits >> 20) + (((float)rnd + 0.5f) * (n2 + 1.0f) < f * (n2 + f) * 65536.0f ? 1u : 0u);
+// E4M3 code of a magnitude below 2^-6, brought to 2^8 times that: the last bits of a + 4 are whole steps of 2^-9 and 20 bits behind them, by which it is rounded up or down.  ROOT: so that the
+// mean of the code's square is kept.
+template <bool ROOT>
+__device__ inline unsigned small_code(float a, unsigned rnd) {
+    const unsigned at = __float_as_uint(a + 4.0f) - 0x40800000u;
+    if constexpr (!ROOT) return (at + (rnd << 4)) >> 20;
+    const float f = (float)(at & 0xFFFFFu) * 0x1p-20f, n2 = (float)(2u * (at >> 20));
+    const unsigned code = (at >> 20) + (((float)rnd + 0.5f) * (n2 + 1.0f) < f * (n2 + f) * 65536.0f ? 1u : 0u);
+    return code == 0 && a > 0.0f ? 1u : code;
+}
+// E4M3 codes (their low 7 bits) of the magnitudes of x with |x| 2^(127 - scale) <= 448, by 16 random bits each.  They are brought to 2^8 times that: the low byte of the exponent
+// and the first three bits of the mantissa is then the code of a normal value, with 20 bits behind it.  Few waves hold values below 2^-6 (one in 40 where the gradients of a block are alike), and the others do not
+// pay for them: the step is near what the vector units do while it waits for memory (233 million elements 622 us, 725 with both computed for every value).
+// SQUARE: the mean of the codes' squares is kept instead of their own.
+template <bool ROOT, bool SQUARE>
+__device__ inline void codes_of(const v4f& x, int scale, const unsigned (&rnd)[4], unsigned (&codes)[4]) {
+    float a[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = __builtin_amdgcn_ldexpf(__builtin_fabsf(x[i]), 135 - scale);
+        const unsigned bits = __float_as_uint(a[i]);
+        if constexpr (SQUARE) {
+            const float f = (float)(bits & 0xFFFFFu) * 0x1p-20f, n2 = (float)(16u + 2u * ((bits >> 20) & 7u));
+            codes[i] = (bits >> 20) + (((float)rnd[i] + 0.5f) * (n2 + 1.0f) < f * (n2 + f) * 65536.0f ? 1u : 0u);
+        } else {
+            codes[i] = (bits + (rnd[i] << 4)) >> 20;
+        }
     }
-    return a >= 4.0f ? normal : small;
+    const float least = __builtin_fminf(__builtin_fminf(a[0], a[1]), __builtin_fminf(a[2], a[3]));
+    if (__builtin_amdgcn_ballot_w64(least < 4.0f)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (a[i] < 4.0f) codes[i] = small_code<ROOT>(a[i], rnd[i]);
+    }
 }
 __device__ inline unsigned pack_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
@@ -202,13 +226,18 @@ __device__ inline unsigned step_of(const AdamWTensor& t, const AdamWHyper& h, fl
         }
         const unsigned ms = scale_code<0>(max_of_32(m_mag)), vs = scale_code<0>(max_of_32(v_mag));
         auto codes = [&](auto square) __attribute__((always_inline)) {
-            unsigned mc[4], vc[4];
+            unsigned mc[4], vc[4], m_rnd[4], v_rnd[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const unsigned rnd = mixed_bits(counter + i, h.key);
-                mc[i] = (code_of<false>(__builtin_fabsf(m[i]), (int)ms, rnd & 0xFFFFu) & 0x7Fu) | (__float_as_uint(m[i]) >> 24 & 0x80u);
-                vc[i] = code_of<decltype(square)::value>(root[i], (int)vs, rnd >> 16) & 0x7Fu;
-                vc[i] = vc[i] == 0 && root[i] > 0.0f ? 1u : vc[i];
+                m_rnd[i] = rnd & 0xFFFFu, v_rnd[i] = rnd >> 16;
+            }
+            codes_of<false, false>(m, (int)ms, m_rnd, mc);
+            codes_of<true, decltype(square)::value>(root, (int)vs, v_rnd, vc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                mc[i] = (mc[i] & 0x7Fu) | (__float_as_uint(m[i]) >> 24 & 0x80u);
+                vc[i] &= 0x7Fu;
             }
             store4<K::GUARD>(static_cast<uint8_t*>(t.m) + at, valid, pack_bytes(mc[0], mc[1], mc[2], mc[3]));
             store4<K::GUARD>(static_cast<uint8_t*>(t.v) + at, valid, pack_bytes(vc[0], vc[1], vc[2], vc[3]));

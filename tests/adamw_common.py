@@ -39,20 +39,18 @@ def powers(bytes_, n):
     return np.repeat(np.exp2(bytes_.astype(np.float64) - 127), 128)[:n].astype(f32)
 
 
-def codes_of(x, rnd, square):
-    """(codes of the magnitudes, scale bytes) of binary32 values in blocks of 128."""
+def codes_of(x, rnd, square, root=False):
+    """(codes of the magnitudes, scale bytes) of binary32 values in blocks of 128.  square: the mean of a code's square is kept, of roots below 2^-6 always."""
     n = x.size
     blocks = np.abs(np.pad(x, (0, -n % 128))).reshape(-1, 128)
     b = np.array([scale_code(float(v), 0) for v in blocks.max(1)])
     a = (blocks.astype(np.float64) * np.exp2(127.0 - b)[:, None]).reshape(-1)[:n].astype(f32)
-    bits = a.view(np.uint32).astype(np.int64)
-    if square:
-        f, unit = (bits & 0xFFFFF).astype(f32) * f32(2.0 ** -20), (16 + 2 * ((bits >> 20) & 7)).astype(f32)
-        up = (rnd.astype(f32) + f32(0.5)) * (unit + f32(1)) < f * (unit + f) * f32(65536)
-        normal = (bits >> 20) - 960 + up
-    else:
-        normal = ((bits + (rnd.astype(np.int64) << 4)) >> 20) - 960
-    return np.where(a >= 2.0 ** -6, normal, np.rint(a * f32(512)).astype(np.int64)), b
+    small = a < 2.0 ** -6
+    # the code and 20 bits behind it, of a normal value its exponent and mantissa, below 2^-6 steps of 2^-9
+    at = np.where(small, np.rint(a.astype(np.float64) * 2.0 ** 29).astype(np.int64), a.view(np.uint32).astype(np.int64) - (960 << 20))
+    f, unit = (at & 0xFFFFF).astype(f32) * f32(2.0 ** -20), (2 * np.where(small, at >> 20, 8 + ((at >> 20) & 7))).astype(f32)
+    up = (rnd.astype(f32) + f32(0.5)) * (unit + f32(1)) < f * (unit + f) * f32(65536)
+    return np.where(square | (root & small), (at >> 20) + up, (at + (rnd.astype(np.int64) << 4)) >> 20), b
 
 
 class State:
@@ -94,7 +92,7 @@ def step_as_rounded(state, g, t, lr, b1, b2, eps, wd, seed=0, scale=1.0, decay=T
     if state.m_scale is not None:
         rnd = mixed(counter, key)
         mc, out.m_scale = codes_of(m, rnd & np.uint64(0xFFFF), False)
-        vc, out.v_scale = codes_of(root, rnd >> np.uint64(16), b2 > 0.96875)
+        vc, out.v_scale = codes_of(root, rnd >> np.uint64(16), b2 > 0.96875, True)
         out.m, out.v = np.where(m < 0, mc | 128, mc).astype(np.uint8), np.where((vc == 0) & (root > 0), 1, vc).astype(np.uint8)
     out.master = w if state.master is not None else None
     if state.w is not None:
