@@ -76,9 +76,10 @@ __device__ inline float group_sum(float v) {
     return v;
 }
 
-// 1 / sqrt(x): the hardware's, to within a unit in the last place, and a Newton step
+// 1 / sqrt(x): the hardware's, to within a unit in the last place, and a Newton step.  The instruction takes subnormals for zeros, so those are brought up first (heads of values below 2^-63 without eps).
 __device__ inline float inverse_root(float x) {
-    const float y = __builtin_amdgcn_rsqf(x);
+    const bool subnormal = x < 0x1p-126f;
+    const float y = __builtin_amdgcn_rsqf(subnormal ? x * 0x1p24f : x) * (subnormal ? 0x1p12f : 1.0f);
     const float e = __builtin_fmaf(-x * y, y, 1.0f);
     return e == e ? __builtin_fmaf(0.5f * y, e, y) : y;      // (0 and infinity: y is infinity and 0)
 }
