@@ -427,7 +427,7 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
  * is the dY of the QKV projection.
  *
  *   qkv [M, (Hq + 2 Hkv) D] BF16: a row is Hq query heads, Hkv key heads and Hkv value heads of D values each.
- *   n[i] = (x[i] rstd) w[i],   rstd = 1 / sqrt(mean of x^2 over the head + eps),   w = wq or wk, [D] BF16; both NULL: no norm, n = x
+ *   n[i] = (x[i] rstd) w[i],   rstd = 1 / sqrt(mean of x^2 over the head + eps),   w = wq or wk, [D] BF16; both NULL: no norm, n = x.  0 <= eps, finite (LLMQ_ERR_VALUE)
  *   the first `rot` values of a head (even, 0 .. D) are turned in pairs, the others stay:  interleaved == 0: i with i + rot/2;  1: 2 i with 2 i + 1
  *     y_a = n_a cos t - n_b sin t,   y_b = n_b cos t + n_a sin t,   t = d_positions[m] d_inv_freq[pair]
  *   d_positions [M] int64 (any value; those of a cache go on where it ends), d_inv_freq [rot/2] double, radians per position, finite.  The angle is found in 64-bit

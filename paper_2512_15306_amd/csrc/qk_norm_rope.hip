@@ -641,6 +641,7 @@ int llmq_qk_norm_rope_fwd(const void* qkv_bf16, int64_t qkv_stride, int64_t M, i
     const int st = check_qk(M, Hq, Hkv, D, rot, interleaved);
     if (st != LLMQ_OK) return st;
     if (!stride_ok(M, (int64_t)(Hq + 2 * Hkv) * D, qkv_stride) || !stride_ok(M, (int64_t)Hq * D, q_stride) || !stride_ok(M, (int64_t)Hkv * D, k_stride)) return LLMQ_ERR_SHAPE;
+    if (wq_bf16 && !(eps >= 0.0f && eps <= 3.402823466e+38f)) return LLMQ_ERR_VALUE;
     if (!aligned(qkv_bf16, 2) || !aligned(q_bf16, 2) || !aligned(k_bf16, 2) || !aligned(wq_bf16, 2) || !aligned(wk_bf16, 2) || !aligned(d_positions, 8) ||
         !aligned(d_inv_freq, 8) || !aligned(rstd, 4))
         return LLMQ_ERR_ALIGN;

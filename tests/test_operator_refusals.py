@@ -1,0 +1,21 @@
+"""Calls of the query and key norms and of AdamW that are refused on the host, without a GPU."""
+import ctypes
+
+import pytest
+
+from paper_2512_15306_amd import llmq
+
+P = 0x10000               # never dereferenced: every call below fails validation on the host
+
+
+def forward(**o):
+    a = dict(dict(x=P, xs=512, M=3, Hq=4, Hkv=2, D=64, wq=P, wk=P, eps=1e-6, pos=P, freq=P, rot=64, inter=0, q=P, qs=256, k=P, ks=128, rstd=P), **o)
+    return llmq.lib().llmq_qk_norm_rope_fwd(a["x"], a["xs"], a["M"], a["Hq"], a["Hkv"], a["D"], a["wq"], a["wk"], a["eps"], a["pos"], a["freq"], a["rot"], a["inter"], a["q"], a["qs"], a["k"], a["ks"],
+                                            a["rstd"], None)
+
+
+def test_eps_has_to_be_a_number_from_zero_on():
+    for eps in (float("nan"), -1e-6, float("inf"), -float("inf")):
+        assert forward(eps=eps) == -8
+    assert forward(eps=0.0, x=P + 1) == forward(eps=1e38, x=P + 1) == -3          # (stopped by an address at an odd byte)
+    assert forward(eps=float("nan"), wq=None, wk=None, x=P + 1) == -3             # without a norm there is no eps
