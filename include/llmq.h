@@ -437,7 +437,8 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
  *   The values V stay where they are.  q and k may be the query and key columns of qkv themselves (in place).
  * llmq_qk_norm_rope_bwd: dq, dk of q and k, dv of V (or NULL: V's columns of dqkv already hold it, or dv points at them) -> dqkv, laid out as qkv, and
  *     g = dy turned back;   dw[i] = sum over rows and heads of g[i] x[i] rstd;   dx[i] = rstd (g[i] w[i] - x[i] rstd mean(g w x rstd))
- *   dwq, dwk [D] float, added to if accumulate != 0; NULL: not wanted (and there are none without a norm: LLMQ_ERR_NULL).  The sums are taken in an order that depends on the sizes alone.  d_amax, d_scale [1] float or
+ *   dwq, dwk [D] float, added to if accumulate != 0; NULL: not wanted (and there are none without a norm: LLMQ_ERR_NULL).  They share no memory (LLMQ_ERR_VALUE): the gradient of one weight for both is the
+ *   sum of the two.  The sums are taken in an order that depends on the sizes alone.  d_amax, d_scale [1] float or
  *   NULL: absmax of all of dqkv and its scale for fmt, bit for bit as llmq_amax of dqkv has them.  qkv and rstd are not read without a norm (and may be NULL).
  *   dq and dk may be the query and key columns of dqkv.  ws: llmq_qk_norm_rope_workspace_bytes bytes, 16-byte aligned, contents irrelevant (calls that may overlap on
  *   the device, graphs among them, need different ones); NULL if neither dw nor d_amax is wanted.

@@ -678,6 +678,8 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
         !aligned(d_positions, 8) || !aligned(d_inv_freq, 8) || !aligned(dqkv_bf16, 2) || !aligned(dwq, 4) || !aligned(dwk, 4) || !aligned(d_amax, 4) || !aligned(d_scale, 4) || !aligned(ws, 16))
         return LLMQ_ERR_ALIGN;
     if ((sums || d_amax) && ws_bytes < qk_workspace(D)) return LLMQ_ERR_WORKSPACE;
+    // (two workgroups would write the same sums)
+    if (dwq && dwk && dwq < dwk + D && dwk < dwq + D) return LLMQ_ERR_VALUE;
     typedef llmq::u16 u16;
     llmq::QkArgs a{};
     a.M = M, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.rot = rot, a.interleaved = interleaved;

@@ -19,3 +19,16 @@ def test_eps_has_to_be_a_number_from_zero_on():
         assert forward(eps=eps) == -8
     assert forward(eps=0.0, x=P + 1) == forward(eps=1e38, x=P + 1) == -3          # (stopped by an address at an odd byte)
     assert forward(eps=float("nan"), wq=None, wk=None, x=P + 1) == -3             # without a norm there is no eps
+
+
+def backward(**o):
+    a = dict(dict(dq=P, dqs=256, dk=P, dks=128, dv=P, dvs=128, x=P, xs=512, M=3, Hq=4, Hkv=2, D=64, wq=P, wk=P, rstd=P, pos=P, freq=P, rot=64, inter=0, dx=P, dxs=512, dwq=P, dwk=2 * P, fmt=0, amax=P,
+                  scale=P, ws=P, bytes=llmq.llmq_qk_norm_rope_workspace_bytes(3, 4, 2, 64)), **o)
+    return llmq.lib().llmq_qk_norm_rope_bwd(a["dq"], a["dqs"], a["dk"], a["dks"], a["dv"], a["dvs"], a["x"], a["xs"], a["M"], a["Hq"], a["Hkv"], a["D"], a["wq"], a["wk"], a["rstd"], a["pos"], a["freq"],
+                                            a["rot"], a["inter"], a["dx"], a["dxs"], a["dwq"], a["dwk"], 0, a["fmt"], a["amax"], a["scale"], a["ws"], ctypes.c_size_t(a["bytes"]), None)
+
+
+def test_the_sums_for_queries_and_keys_lie_apart():
+    """One buffer for both (a weight that queries and keys share) would be written by two workgroups at once."""
+    for dwk in (P, P + 4, P + 252, P - 4, P - 252):
+        assert backward(dwk=dwk) == -8
