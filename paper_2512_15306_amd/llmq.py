@@ -684,9 +684,12 @@ def llmq_adamw_step(plan: AdamWPlan, hyper: torch.Tensor, grad_scale: Optional[t
         return _check(status, "llmq_adamw_step") if status else None
     if hyper.dtype != torch.int32 or hyper.numel() != ADAMW_HYPER_WORDS or not hyper.is_contiguous():
         raise ValueError("hyper must be %d int32 words" % ADAMW_HYPER_WORDS)
+    info = plan.info                                      # read by the host during the call, wherever the table is
+    if not info.is_cpu or info.dtype != torch.int64 or info.numel() != 4 or not info.is_contiguous():
+        raise ValueError("the plan's info must be its 4 int64 words in host memory, got %s %s on %s" % (tuple(info.shape), info.dtype, info.device))
     on_device = hyper.is_cuda
     words = _here(hyper, torch.int32, "hyper") if on_device else hyper.data_ptr()
-    _check(lib().llmq_adamw_step(_here(plan.table, torch.uint8, "plan"), plan.info.data_ptr(), None if on_device else words, words if on_device else None,
+    _check(lib().llmq_adamw_step(_here(plan.table, torch.uint8, "plan"), info.data_ptr(), None if on_device else words, words if on_device else None,
                                  _here(grad_scale, torch.float32, "grad_scale", 1), _stream()), "llmq_adamw_step")
 
 

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2512_15306_amd import llmq
 
@@ -32,3 +33,20 @@ def test_the_sums_for_queries_and_keys_lie_apart():
     """One buffer for both (a weight that queries and keys share) would be written by two workgroups at once."""
     for dwk in (P, P + 4, P + 252, P - 4, P - 252):
         assert backward(dwk=dwk) == -8
+
+
+def test_the_words_of_a_plan_stay_on_the_host():
+    """They are read during the call; a plan moved to the device as a whole would be read there."""
+    words = llmq.llmq_adamw_hyper(1, 1e-3, 0.9, 0.95, 1e-8, 0.1)
+    for info in (torch.zeros(4, dtype=torch.int64, device="meta"), torch.zeros(4, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), torch.zeros(8, dtype=torch.int64)[::2]):
+        with pytest.raises(ValueError, match="info"):
+            llmq.llmq_adamw_step(llmq.AdamWPlan(torch.zeros(64, dtype=torch.uint8), info, ()), words)
+
+
+@pytest.mark.gpu
+def test_a_plan_moved_to_the_device_is_refused():
+    on = dict(device="cuda:0")
+    t = llmq.AdamWTensor(None, torch.zeros(64, **on), torch.zeros(64, **on), torch.zeros(64, **on), torch.zeros(64, **on))
+    plan = llmq.llmq_adamw_plan([t])
+    with pytest.raises(ValueError, match="info"):
+        llmq.llmq_adamw_step(plan._replace(info=plan.info.to("cuda:0")), llmq.llmq_adamw_hyper(1, 1e-3, 0.9, 0.95, 1e-8, 0.1))
