@@ -485,8 +485,8 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
  *
  * llmq_adamw_plan (host code): checks `count` tensors and writes the table that a step reads into `plan`, llmq_adamw_plan_bytes bytes of HOST memory, which the caller copies to
  *   device memory (16-byte aligned) once; info [4]: host words that llmq_adamw_step takes back.  The plan holds as long as the pointers do.
- * llmq_adamw_hyper (host code): the numbers of a step (1, 2, ...) as LLMQ_ADAMW_HYPER_WORDS 32-bit words.  0 <= beta < 1, lr and weight_decay >= 0, eps > 0 in binary32, else
- *   LLMQ_ERR_VALUE.
+ * llmq_adamw_hyper (host code): the numbers of a step (1, 2, ...) as LLMQ_ADAMW_HYPER_WORDS 32-bit words.  0 <= beta < 1, lr and weight_decay >= 0, eps > 0 in binary32, and eps and
+ *   the factors of a step finite there, else LLMQ_ERR_VALUE.
  * llmq_adamw_step: exactly one of hyper (HOST words, read during the call) and d_hyper (the same words in device memory, read when the step runs: a captured step takes new ones with
  *   every replay) is given.
  */

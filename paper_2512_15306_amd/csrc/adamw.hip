@@ -422,6 +422,7 @@ int llmq_adamw_hyper(int64_t step, double lr, double beta1, double beta2, double
     llmq::AdamWHyper h{};
     h.b1 = (float)beta1, h.b2 = (float)beta2, h.c1 = (float)(1 - beta1), h.c2 = (float)(1 - beta2);
     h.lr_decay = (float)(lr * weight_decay), h.lr_m = (float)(lr / (1 - pow(beta1, (double)step))), h.root_scale = (float)(1 / sqrt(1 - pow(beta2, (double)step))), h.eps = (float)eps;
+    if (!isfinite(h.lr_decay) || !isfinite(h.lr_m) || !isfinite(h.root_scale) || !isfinite(h.eps)) return LLMQ_ERR_VALUE;
     h.key = llmq::mixed_bits((uint64_t)step, llmq::mixed_bits(seed, 0));
     memcpy(hyper, &h, sizeof(h));
     return LLMQ_OK;

@@ -50,3 +50,13 @@ def test_a_plan_moved_to_the_device_is_refused():
     plan = llmq.llmq_adamw_plan([t])
     with pytest.raises(ValueError, match="info"):
         llmq.llmq_adamw_step(plan._replace(info=plan.info.to("cuda:0")), llmq.llmq_adamw_hyper(1, 1e-3, 0.9, 0.95, 1e-8, 0.1))
+
+
+def test_the_numbers_of_a_step_are_finite_in_binary32():
+    good = dict(step=1, lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
+    for bad in (dict(lr=1e39), dict(lr=1e38, beta1=0.99), dict(lr=1e20, weight_decay=1e20), dict(eps=1e39)):      # (infinities in the words, and NaN in the weights)
+        with pytest.raises(llmq.LlmqError) as e:
+            llmq.llmq_adamw_hyper(**dict(good, **bad))
+        assert e.value.status == -8
+    words = llmq.llmq_adamw_hyper(**dict(good, lr=3e37, beta1=0.9, beta2=1 - 2.0 ** -53, weight_decay=1.0))[:8].view(torch.float32)
+    assert torch.isfinite(words).all() and words.max() > 1e37
