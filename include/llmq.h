@@ -479,7 +479,7 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
  *                   square, without which v would grow by its rounding; up to 31/32 the others' growth is 4 % of v at most.  A gradient that is not finite makes
  *                   its whole block NaN.
  *   d_amax          [1] float or NULL: absmax of the new w_bf16 (canonical NaN as llmq_amax), of all tensors that name the same word: the next quantization of these
- *                   weights then needs no pass of its own (llmq_scale_from_amax).
+ *                   weights then needs no pass of its own (llmq_scale_from_amax).  The word lies in no array of the call, read or written (llmq_adamw_plan does not look at that; llmq.py refuses it).
  *   first_counter   number of the tensor's first element among all that are rounded at random (>= 0): element i takes its bits from first_counter + i, the seed and the step.
  *                   Tensors should not share numbers.  Same inputs, same bytes.
  *

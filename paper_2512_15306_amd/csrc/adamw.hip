@@ -345,7 +345,7 @@ int check_adamw(const llmq_adamw_tensor* t, int64_t count, int64_t& pieces) {
     return LLMQ_OK;
 }
 
-// Whether an array that a step writes shares memory with another one of the plan: its workgroups run in any order.  (Absmax words may be shared; gradients are only read.)
+// Whether an array that a step writes shares memory with another one of the plan: its workgroups run in any order.  (Gradients are only read, and may be shared.  Absmax words are left to the caller.)
 int check_apart(const llmq_adamw_tensor* t, int64_t count) {
     struct Range { uintptr_t first, end; bool written; };
     Range* const r = new (std::nothrow) Range[(size_t)count * 7];

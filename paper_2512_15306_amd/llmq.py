@@ -5,7 +5,9 @@ library's kernels.  There is no fallback: a missing library or a missing GPU rai
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
+import itertools
 import os
 import warnings
 from typing import NamedTuple, Optional, Sequence, Tuple
@@ -646,6 +648,24 @@ class AdamWPlan(NamedTuple):
     tensors: Tuple[AdamWTensor, ...]
 
 
+def _check_absmax_words(entries: Sequence[_AdamWTensor]) -> None:
+    """A step clears and raises the absmax words while it reads and writes the arrays, so none lies in an array (several tensors may share one)."""
+    words = {e.d_amax for e in entries if e.d_amax}
+    if not words:
+        return
+    ranges = []
+    for e in entries:
+        codes, scales = e.flags & ADAMW_STATES_8BIT, (e.n + 127) // 128
+        ranges += [(p, p + size) for p, size in ((e.w_bf16, 2 * e.n), (e.w_f32, 4 * e.n), (e.grad, (4 if e.flags & ADAMW_GRAD_F32 else 2) * e.n), (e.m, (1 if codes else 4) * e.n),
+                                                 (e.v, (1 if codes else 4) * e.n), (e.m_scale, scales), (e.v_scale, scales)) if p]
+    ranges.sort()
+    starts, ends = [r[0] for r in ranges], list(itertools.accumulate((r[1] for r in ranges), max))
+    for word in words:
+        before = bisect.bisect_left(starts, word + 4)      # arrays that begin before the word's end
+        if before and ends[before - 1] > word:
+            raise ValueError("amax lies in another array of the step")
+
+
 def llmq_adamw_plan(tensors: Sequence[AdamWTensor]) -> AdamWPlan:
     """The plan of a step over `tensors`, in memory of its own on the current device."""
     entries = (_AdamWTensor * max(len(tensors), 1))()
@@ -664,6 +684,7 @@ def llmq_adamw_plan(tensors: Sequence[AdamWTensor]) -> AdamWPlan:
         e.m_scale, e.v_scale = _here(t.m_scale, torch.uint8, "m_scale", scales), _here(t.v_scale, torch.uint8, "v_scale", scales)
         e.d_amax, e.n, e.first_counter = _here(t.amax, torch.float32, "amax", 1), n, t.first_counter
         e.flags = (ADAMW_GRAD_F32 if t.grad.dtype == torch.float32 else 0) | (ADAMW_STATES_8BIT if codes else 0) | (0 if t.decay else ADAMW_NO_DECAY) | (ADAMW_STOCHASTIC if t.stochastic else 0)
+    _check_absmax_words(entries)
     nbytes = int(lib().llmq_adamw_plan_bytes(entries, len(tensors)))
     table, info = torch.empty(max(nbytes, 1), dtype=torch.uint8), torch.zeros(4, dtype=torch.int64)
     _check(lib().llmq_adamw_plan(entries, len(tensors), table.data_ptr(), nbytes, info.data_ptr()), "llmq_adamw_plan")

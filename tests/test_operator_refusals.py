@@ -60,3 +60,38 @@ def test_the_numbers_of_a_step_are_finite_in_binary32():
         assert e.value.status == -8
     words = llmq.llmq_adamw_hyper(**dict(good, lr=3e37, beta1=0.9, beta2=1 - 2.0 ** -53, weight_decay=1.0))[:8].view(torch.float32)
     assert torch.isfinite(words).all() and words.max() > 1e37
+
+
+def test_absmax_words_lie_in_no_array():
+    n, at = 1000, 1 << 20
+    arrays = dict(w_bf16=2 * n, w_f32=4 * n, grad=2 * n, m=n, v=n, m_scale=8, v_scale=8)
+
+    def entries(word, **o):
+        e = llmq._AdamWTensor(n=n, flags=llmq.ADAMW_STATES_8BIT, d_amax=word, **{name: (k + 1) * at for k, name in enumerate(arrays)})
+        other = llmq._AdamWTensor(n=n, d_amax=word, w_bf16=at << 8, grad=(at << 8) + 8192, m=(at << 9), v=(at << 9) + 8192, **o)
+        return e, other
+
+    for k, size in enumerate(arrays.values()):
+        first = (k + 1) * at
+        for word in (first, first + (size - 1) // 4 * 4):
+            with pytest.raises(ValueError, match="amax"):
+                llmq._check_absmax_words(entries(word))
+        for word in (first - 4, first + (size + 3) // 4 * 4):
+            llmq._check_absmax_words(entries(word))
+    for word in ((at << 9) + 3996, (at << 8) + 8192 + 1996):          # moments of binary32, gradients of BF16
+        with pytest.raises(ValueError, match="amax"):
+            llmq._check_absmax_words(entries(word))
+    llmq._check_absmax_words(entries((at << 8) + 8192 + 2000))
+    with pytest.raises(ValueError, match="amax"):
+        llmq._check_absmax_words(entries((at << 8) + 8192 + 2000, flags=llmq.ADAMW_GRAD_F32))
+    llmq._check_absmax_words(entries(None))
+
+
+@pytest.mark.gpu
+def test_an_absmax_word_in_a_moment_is_refused():
+    on = dict(device="cuda:0")
+    w, m = torch.zeros(64, dtype=torch.bfloat16, **on), torch.zeros(64, **on)
+    t = llmq.AdamWTensor(w, None, torch.zeros(64, **on), m, torch.zeros(64, **on), amax=m[8:9])
+    with pytest.raises(ValueError, match="amax"):
+        llmq.llmq_adamw_plan([t])
+    llmq.llmq_adamw_plan([t._replace(amax=torch.zeros(1, **on))])
