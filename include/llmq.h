@@ -229,8 +229,10 @@ int llmq_bf16_gemm_tn(const void* A_bf16, const void* B_bf16, int64_t R, int64_t
  *   Other values of block_rows: LLMQ_ERR_FLAGS.  All pointers 16-byte aligned.  Multiples of 128 rows and columns are fastest.
  *
  * llmq_fp8_gemm_blocks: c[r,cc] = bf16( sum_t A[r,t] dA[r,t/128] B[cc,t] dB[cc,t/128] )   (+ c[r,cc] first when accumulate != 0, one rounding)
- *   A [R,T] and B [C,T], rows of T contiguous bytes, any mix of formats; sA, sB their scale bytes.  Products are exact, sums in binary32 on the matrix
- *   cores.  d_amax_c as in llmq_fp8_gemm_tn.  Error of each element bounded as there, by 2^-7 of the sum of the products' magnitudes.  Fastest with R and C
+ *   A [R,T] and B [C,T], rows of T contiguous bytes, any mix of formats; sA, sB their scale bytes.  Products are exact; the matrix cores
+ *   align the 128 products of a K step to the largest before they add them (up to 2^-12.3 of the sum of their magnitudes was seen to be lost, as in llmq_fp8_gemm_tn) and add the steps in binary32.  Up to 32 rows, and some
+ *   small outputs whose T is no multiple of 16, take a kernel that adds every fourth step by itself and joins the four sums: the last bits of a row may differ from those the same row has in a larger call (the same call
+ *   gives the same bytes).  d_amax_c as in llmq_fp8_gemm_tn.  Error of each element bounded as there, by 2^-7 of the sum of the products' magnitudes.  Fastest with R and C
  *   multiples of 256 and T a multiple of 128 (16 at least).  T < 16, T or C >= 2^22 and scales of 2 GB take a slow generic kernel, which has R < 2^21 and
  *   C < 2^28 (LLMQ_ERR_SHAPE otherwise).
  *   forward         Y = X W^T     A = q of X,      B = q of W
@@ -431,7 +433,8 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
  *   the first `rot` values of a head (even, 0 .. D) are turned in pairs, the others stay:  interleaved == 0: i with i + rot/2;  1: 2 i with 2 i + 1
  *     y_a = n_a cos t - n_b sin t,   y_b = n_b cos t + n_a sin t,   t = d_positions[m] d_inv_freq[pair]
  *   d_positions [M] int64 (any value; those of a cache go on where it ends), d_inv_freq [rot/2] double, radians per position, finite.  The angle is found in 64-bit
- *   fractions of a turn: to 2^-52 of the frequency times the position, for any position.  Sums and everything else in binary32, one rounding to BF16.
+ *   fractions of a turn: off by at most |position| (2^-52 of the frequency + 2^-64 of a turn; 2^-54 of a turn for negative frequencies) + 2^-32 of a turn, for any position; its sine and cosine by 2^-22.
+ *   Sums and everything else in binary32, one rounding to BF16.
  *
  * llmq_qk_norm_rope_fwd: q [M, Hq D] and k [M, Hkv D] BF16; rstd [M, Hq + Hkv] float, kept for the backward pass, or NULL (not with NULL weights: ignored).
  *   The values V stay where they are.  q and k may be the query and key columns of qkv themselves (in place).
@@ -484,7 +487,8 @@ int llmq_qk_norm_rope_bwd(const void* dq_bf16, int64_t dq_stride, const void* dk
  *                   Tensors should not share numbers.  Same inputs, same bytes.
  *
  * llmq_adamw_plan (host code): checks `count` tensors and writes the table that a step reads into `plan`, llmq_adamw_plan_bytes bytes of HOST memory, which the caller copies to
- *   device memory (16-byte aligned) once; info [4]: host words that llmq_adamw_step takes back.  The plan holds as long as the pointers do.
+ *   device memory (16-byte aligned) once; info [4]: host words that llmq_adamw_step takes back.  The plan holds as long as the pointers do.  Making one sorts the arrays and writes
+ *   8 bytes for every 1024 elements: 0.2 to 1 ms with the copy for 8 tensors of 233 million elements together, 0.6 ms for 96 small ones through llmq.py, so gradients keep their place from step to step.
  * llmq_adamw_hyper (host code): the numbers of a step (1, 2, ...) as LLMQ_ADAMW_HYPER_WORDS 32-bit words.  0 <= beta < 1, lr and weight_decay >= 0, eps > 0 in binary32, and eps and
  *   the factors of a step finite there, else LLMQ_ERR_VALUE.
  * llmq_adamw_step: exactly one of hyper (HOST words, read during the call) and d_hyper (the same words in device memory, read when the step runs: a captured step takes new ones with

@@ -12,15 +12,16 @@
 // 16 random bits from a hash of element and step: the same bits on every run.  For the root there are two means to keep.  Its own: then its square comes out larger by the
 // variance, 0.13 % a step on average over the codes (a sixth of the square of the spacing, 1/8 to 1/16), which the average over 1 / (1 - b2) steps multiplies: 2.5 % of v
 // for b2 = 0.95, and without bound from 0.9987 on.  Its square's, by the probability f (2 n + f) / (2 n + 1) for n + f units: v is right for any b2.  The first is what roots
-// get for b2 up to 31/32, the second above.
+// get for b2 up to 31/32, the second above: it would be right everywhere, but a step of the 233 million elements below takes 667 us with it and 622 with the first (back to back), more
+// than 4 % of v, 2 % of a weight's step, are worth.
 // Below 2^-6 (2^-15 of the block's largest value) the codes are as far apart as at 2^-6 and are rounded up or down too: to the nearest, 4 would stay 4 under b1 = 0.9, and a weight whose
 // gradient has stopped would go on by a share of lr a step without end (79 lr in 1000 steps on average, where it is 2.2 rounded so and in exact moments).  There roots keep their square's mean for any b2: by their own,
 // v would come out 10 to 70 % too large (roots of 1 to 4 times the smallest code).  Only a root above zero is kept above zero: a moment that came up beside a root that went to zero would make a step
 // without bound.
 // Weights in BF16 without a master copy can be rounded the same way, for the same reason.
 //
-// 233 million elements in 8 tensors, moments in 8 bits and a master copy (3.74 GB): 650 us, 5.7 TB/s; 12.5 million in 96 tensors of 128 to 520662 elements, moments in binary32
-// (351 MB): 59 us, 5.9 TB/s: a large copy has 5.85.
+// 233 million elements in 8 tensors, moments in 8 bits and a master copy (3.74 GB): 634 us, 5.9 TB/s; 12.5 million in 96 tensors of 128 to 520662 elements, moments in binary32
+// (351 MB): 59 us, 6.0 TB/s: a large copy has 5.85.  With an absmax word for every tensor 30 us more for the first, 44 for the second (back to back): each workgroup finds the largest of its piece and looks at the word.
 #include <math.h>
 #include <string.h>
 
@@ -49,7 +50,8 @@ static_assert(sizeof(AdamWHyper) == 4 * LLMQ_ADAMW_HYPER_WORDS, "");
 constexpr float kRootMeanBeta = 0.96875f;
 // A lane has four elements, a wave 256 that follow each other, so that every load and store of a wave is one piece of memory.  A workgroup's piece of a tensor is no more than that
 // for its four waves: many short workgroups keep more loads on their way than fewer that go through several such groups, also with the next group's loads ahead of the step for
-// the last.  Pieces of 1024 / 4096, microseconds: 255816 elements 4.9 / 9.8, 1.6 million 8.8 / 11.9, 12.5 million in binary32 59.6 / 68.7, 233 million in 8 bits 652 / 676.
+// the last.  Pieces of 1024 / 4096, microseconds: 255816 elements 4.9 / 9.8, 1.6 million 8.8 / 11.9, 12.5 million in binary32 59.6 / 68.7, 233 million in 8 bits 652 / 676 (before codes_of left small
+// codes to the waves that hold some).
 constexpr int kAdamThreads = 256, kAdamLane = 4, kAdamPiece = kAdamThreads * kAdamLane;
 
 // 32 well mixed bits for a counter under a key.  The multipliers are odd numbers from the golden ratio and the square roots of 2 and 3.

@@ -5,15 +5,15 @@
 //   backward: g = the same rotation by -t of dy;  dw += g x rstd;  dx = rstd (g w - x rstd mean(g w x rstd))
 //
 // HBM-bound: 2 bytes read and 2 written per value (backward 4 and 2).  What there is to compute is arranged around the angles: t = position f mod one turn is
-// a product of 64-bit whole numbers, with the frequency as a 64-bit fraction of a turn, exact for every position, so that far positions lose nothing and no table
-// is read; a sine and a cosine by their series then cost about 25 instructions, which a lane pays once per token for its four pairs and uses
+// a product of 64-bit whole numbers, with the frequency as a 64-bit fraction of a turn (off by 2^-52 of itself and 2^-64 of a turn at most): the product is exact, so far positions lose no more than that times the position, and no
+// table is read; a sine and a cosine by their series then cost about 25 instructions, which a lane pays once per token for its four pairs and uses
 // for all heads.  For that a wave takes a token and walks over its heads, as many at a time as fit (four of 128 values), eight
 // values a lane in two pieces of 8 bytes that hold both halves of its pairs: no exchange between lanes but the sums of a head.
 // The sums of dw stay in a lane's registers over all tokens and heads of its wave; each workgroup leaves one row of them, which a second kernel adds
 // in the order of the workgroups (no atomics).
 //
-// Heads of 128 values.  Forward: 8192 tokens of 28 + 4 heads (135 MB) 25.4 us, 5.3 TB/s; 32 tokens 4 us, one trip to memory and back behind the angles.  Backward: 8192 tokens of
-// 40 + 8 (337 MB) 76 us, 4.4 TB/s, of which the second kernel's 4; 1777 tokens of 9 + 3 heads of 80 (12 MB) 12 us: two launches, each a chain of waits.
+// Heads of 128 values, buffers changing from call to call.  Forward: 8192 tokens of 28 + 4 heads (135 MB) 25.4 us, 5.3 TB/s; 32 tokens 4 us, one trip to memory and back behind the angles.  Backward: 8192 tokens of
+// 40 + 8 (337 MB) 75 us, 4.5 TB/s, of which the second kernel's 4; 1777 tokens of 9 + 3 heads of 80 (12 MB) 11.5 us: two launches, each a chain of waits.
 #include "api_checks.h"
 #include "llmq_device.h"
 
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_kernel(const QkArgs a) {
     if constexpr (NORM) {
         if (at.there) { unpack(at.weights(a.wq), wq); unpack(at.weights(a.wk), wk); }
     }
-    // (one / two / four passes in a batch, with six, six and five workgroups to a CU: 8192 tokens of 28 + 4 heads of 128 28.0 / 27.4 / 29.0 us, 512 of them 4.9 / 5.2 / 6.0, 2048 12.3 / 11.7 / 11.9)
+    // (one / two / four passes in a batch, with six, six and five workgroups to a CU, back to back on the same buffers: 8192 tokens of 28 + 4 heads of 128 28.0 / 27.4 / 29.0 us, 512 of them 4.9 / 5.2 / 6.0, 2048 12.3 / 11.7 / 11.9)
     constexpr int kAtOnce = 2;
     for (int64_t m = wave / a.split; m < a.M; m += waves / a.split) {
         float c[4], s[4];
@@ -411,7 +411,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_fwd_any_kernel(const QkArgs a) 
     }
 }
 
-// A workgroup's sums of dw lie in LDS, a row for each wave (heads of at most kQkAnyWidth values; wider ones have no norm here)
+// A workgroup's sums of dw lie in LDS, a row for each wave, room for the widest heads there are
 constexpr int kQkAnyWidth = 1024;
 template <bool NORM>
 __global__ __launch_bounds__(kQkThreads) void qk_bwd_any_kernel(const QkArgs a) {
@@ -617,7 +617,7 @@ static int launch_qk_bwd(QkArgs a, const QkFinal& f, hipStream_t stream, int cus
 
 namespace {
 
-constexpr int64_t kMaxHeads = 1 << 16, kMaxHead = 1024;
+constexpr int64_t kMaxHeads = 1 << 16, kMaxHead = llmq::kQkAnyWidth;
 
 int check_qk(int64_t M, int64_t Hq, int64_t Hkv, int64_t D, int rot, int interleaved) {
     if (!dim_ok(M) || Hq < 1 || Hq > kMaxHeads || Hkv < 1 || Hkv > kMaxHeads || D < 1 || D > kMaxHead || M * (Hq + 2 * Hkv) * D >= kMaxElems) return LLMQ_ERR_SHAPE;
