@@ -642,7 +642,7 @@ class AdamWTensor(NamedTuple):
 
 
 class AdamWPlan(NamedTuple):
-    """What llmq_adamw_step reads: the table on the device, the words that belong to it, and the tensors it points at."""
+    """What llmq_adamw_step reads: the table on the device, the words that belong to it (on the host), and the tensors it points at.  To be kept until the last step over it has run, on whatever stream."""
     table: torch.Tensor
     info: torch.Tensor
     tensors: Tuple[AdamWTensor, ...]
