@@ -425,6 +425,29 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
                                  void* y_bf16, void* stream);
 
 /*
+ * The same norm in front of a contraction with block scales, and its gradient.
+ *
+ * llmq_rmsnorm_fwd_fp8_blocks: res', rstd as llmq_rmsnorm_fwd leaves them, and y as llmq_quantize_fp8_blocks with block_rows 1 would write it, bit for bit:
+ *   q [M, C] and s: codes of y with a scale for each row and 128 columns;   q_t [C, M] and s_t: of the transposed tensor, a scale for each column and 128 rows.
+ *   q and s may be NULL together, or q_t and s_t; one pair must be there.  Without q_t (serving) it is one pass.  y is rounded to BF16 before its codes are made, so that both copies
+ *   are made from the same values; y_bf16 receives them if it is not NULL.  x, res_out as in llmq_rmsnorm_fwd (x may be NULL, res_out may be res).  No workspace, no absmax.
+ *   0 <= eps, finite (LLMQ_ERR_VALUE).  M < 2^25, C < 2^24.  All pointers 16-byte aligned, rstd too.
+ * llmq_rmsnorm_bwd: dy [M, C], the gradient of y; dres [M, C] or NULL, the gradient of the stored stream res' from where else it is read; res [M, C] = res' (the stored stream); w, rstd:
+ *     n = res' rstd,  g = dy w:    dx[m,c] = bf16( dres + rstd (g - n mean_c(g n)) ),    dw[c] = sum_m dy[m,c] n[m,c]
+ *   dx [M, C] BF16 is the gradient of both terms of the addition; it may be dy or dres itself.  dw [C] float, added to if accumulate != 0; NULL: not wanted.  d_amax, d_scale [1] float or NULL: absmax of dx
+ *   and its scale for fmt, bit for bit as llmq_amax of dx has them.  Sums in binary32, in an order that the sizes alone decide.
+ *   ws: llmq_rmsnorm_bwd_workspace_bytes(M, C) bytes, 16-byte aligned, contents irrelevant (calls that may overlap on the device, graphs among them, need different ones); NULL if
+ *   neither dw nor d_amax is wanted.  C < 2^24; rows of C <= 16384 are read once, wider ones take a slow kernel.  C % 8 == 0 is fastest.
+ */
+int llmq_rmsnorm_fwd_fp8_blocks(const void* res_bf16, const void* x_bf16, const void* w_bf16, int64_t M, int64_t C,
+                                float eps, void* res_out_bf16, float* rstd, int fmt, uint8_t* q, uint8_t* s,
+                                uint8_t* q_t, uint8_t* s_t, void* y_bf16, void* stream);
+size_t llmq_rmsnorm_bwd_workspace_bytes(int64_t M, int64_t C);
+int llmq_rmsnorm_bwd(const void* dy_bf16, const void* dres_bf16, const void* res_bf16, const void* w_bf16,
+                     const float* rstd, int64_t M, int64_t C, void* dx_bf16, float* dw, int accumulate, int fmt,
+                     float* d_amax, float* d_scale, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * RMSNorm of every query and key head joined with the rotation by position, between the QKV projection and attention, and the gradient of both, which
  * is the dY of the QKV projection.
  *

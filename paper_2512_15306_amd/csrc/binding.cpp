@@ -372,6 +372,42 @@ LLMQ_BINDING(fp8_gemm_blocks) {
     });
 }
 
+LLMQ_BINDING(rmsnorm_fwd_fp8_blocks) {
+    return run(args, n, 12, [](Args& args_) {
+        HereArgs a(args_);
+        int64_t M = 0, C = 0;
+        a.dims(0, kBf16, M, C);
+        void *res = a.pointer(0, kBf16, -1, true), *x = a.pointer(1, kBf16, M * C, false), *w = a.pointer(2, kBf16, C, true), *res_out = a.pointer(4, kBf16, M * C, false);
+        if (!PyFloat_CheckExact(a.a[3])) a.ok = false;
+        const float eps = a.ok ? (float)PyFloat_AS_DOUBLE(a.a[3]) : 0.0f;
+        float* rstd = static_cast<float*>(a.pointer(5, kF32, M, true));
+        const int fmt = a.i32(6);
+        uint8_t *q = a.codes(7, M * C, false), *s = a.codes(8, (int64_t)llmq_block_scales_bytes(M, C), false);
+        uint8_t *qt = a.codes(9, M * C, false), *st = a.codes(10, (int64_t)llmq_block_scales_bytes(C, M), false);
+        void* y = a.pointer(11, kBf16, M * C, false);
+        args_.ok = a.ok;
+        return [=](void* stream) { return llmq_rmsnorm_fwd_fp8_blocks(res, x, w, M, C, eps, res_out, rstd, fmt, q, s, qt, st, y, stream); };
+    });
+}
+
+LLMQ_BINDING(rmsnorm_bwd) {
+    return run(args, n, 12, [](Args& args_) {
+        HereArgs a(args_);
+        int64_t M = 0, C = 0;
+        a.dims(2, kBf16, M, C);
+        void *dy = a.pointer(0, kBf16, M * C, true), *dres = a.pointer(1, kBf16, M * C, false), *res = a.pointer(2, kBf16, -1, true), *w = a.pointer(3, kBf16, C, true);
+        float* rstd = static_cast<float*>(a.pointer(4, kF32, M, true));
+        void* dx = a.pointer(5, kBf16, M * C, true);
+        float* dw = static_cast<float*>(a.pointer(6, kF32, C, false));
+        const int accumulate = a.truth(7), fmt = a.i32(8);
+        float *am = static_cast<float*>(a.pointer(9, kF32, 1, false)), *sc = static_cast<float*>(a.pointer(10, kF32, 1, false));
+        void* ws = a.pointer(11, kU8, -1, false);
+        const size_t bytes = (size_t)a.numel_of(11);
+        args_.ok = a.ok;
+        return [=](void* s) { return llmq_rmsnorm_bwd(dy, dres, res, w, rstd, M, C, dx, dw, accumulate, fmt, am, sc, ws, bytes, s); };
+    });
+}
+
 LLMQ_BINDING(qk_norm_rope_fwd) {
     return run(args, n, 13, [](Args& args_) {
         HereArgs a(args_);
@@ -447,7 +483,7 @@ LLMQ_BINDING(adamw_step) {
 PyMethodDef g_methods[] = {LLMQ_METHOD(linear_fwd), LLMQ_METHOD(linear_dgrad), LLMQ_METHOD(linear_wgrad), LLMQ_METHOD(amax), LLMQ_METHOD(quantize_fp8),
                            LLMQ_METHOD(quantize_fp8_slabs), LLMQ_METHOD(bf16_gemm_tn), LLMQ_METHOD(swiglu_fwd), LLMQ_METHOD(swiglu_fwd_fp8),
                            LLMQ_METHOD(swiglu_fwd_fp8_slabs), LLMQ_METHOD(swiglu_bwd), LLMQ_METHOD(rmsnorm_fwd), LLMQ_METHOD(rmsnorm_apply_fp8),
-                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), LLMQ_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(rmsnorm_fwd_fp8_blocks), LLMQ_METHOD(rmsnorm_bwd), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), LLMQ_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -207,6 +207,13 @@ int launch_rmsnorm_apply_fp8(const void* res, const void* w, const float* rstd, 
                              const float* d_qscale, int fmt, uint8_t* q, uint8_t* q_t, void* y, hipStream_t stream,
                              bool qt_slabs = false);
 
+// The same with block scales: residual sum and statistics, with the row-wise codes in the same pass (q, s; y optional) or without codes (q NULL); and both
+// copies of the codes, or the transposed one (q NULL), in tiles from the stored sum and its statistics.
+int launch_rmsnorm_rows(const void* res, const void* x, const void* w, int64_t M, int64_t C, float eps, void* res_out, void* y, float* rstd, int fmt,
+                        uint8_t* q, uint8_t* s, hipStream_t stream, int num_cus);
+int launch_norm_quantize_blocks(const void* res, const void* w, const float* rstd, int64_t M, int64_t C, int fmt, uint8_t* q, uint8_t* s,
+                                uint8_t* q_t, uint8_t* s_t, void* y, hipStream_t stream);
+
 int launch_calibrate_mfma(int fmtA, int fmtB, int random_bits, int iters, float* d_sink, hipStream_t stream,
                           int num_cus);
 int launch_calibrate_copy(const void* src, void* dst, size_t bytes, hipStream_t stream);

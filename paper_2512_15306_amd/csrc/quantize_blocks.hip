@@ -10,31 +10,19 @@
 // store one after the other.
 #include "api_checks.h"
 #include "blocks.h"
+#include "rmsnorm.h"
 
 namespace llmq {
-
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef short v2s __attribute__((ext_vector_type(2)));
 
 struct QuantBlocks {
     const uint16_t* x;
     int64_t rows, cols;
     uint8_t *q, *s, *qt, *st;
     SmallGrid grid;                             // of 128 x 128 tiles
+    const uint16_t* w;                          // NORM: the norm's weight and statistics, and y or NULL
+    const float* rstd;
+    uint16_t* y;
 };
-
-// Two BF16 values divided by 2^(code - 127) as two codes in the low or high half of old.  The instruction reads the exponent of its scale, rounds to
-// nearest even, and nothing it is given here is beyond the format's largest value.
-template <int FMT, bool HIGH>
-__device__ inline unsigned cvt_scaled(unsigned pair, unsigned code, unsigned old) {
-    const float d = __uint_as_float(code << 23);
-    if constexpr (FMT == 0) return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(__builtin_bit_cast(v2s, old), __builtin_bit_cast(v2bf, pair), d, HIGH));
-    else return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(__builtin_bit_cast(v2s, old), __builtin_bit_cast(v2bf, pair), d, HIGH));
-}
-template <int FMT>
-__device__ inline unsigned cvt_four(unsigned p0, unsigned p1, unsigned code) {
-    return cvt_scaled<FMT, true>(p1, code, cvt_scaled<FMT, false>(p0, code, 0u));
-}
 
 // Packed maxima over the lanes side by side (wave_patch: bits 0, 1, 4 and 5 of the lane), and over those stacked (bits 2 and 3)
 __device__ inline unsigned max_beside(unsigned v) {
@@ -67,7 +55,8 @@ __device__ inline void tile_write_transposed_upto(const uint8_t* s_t, uint8_t* d
 
 // SQUARE: blocks of 128 x 128 (both copies have the same codes), else 1 x 128 of each copy's rows.  ROWS / COLS: which copies are wanted.
 // STREAM: the row-wise copy is stored with the streaming hint.
-template <int FMT, bool SQUARE, bool ROWS, bool COLS, bool GUARD, bool STREAM>
+// NORM: the codes are those of y = bf16((x rstd) w) (llmq_rmsnorm_fwd_fp8_blocks).
+template <int FMT, bool SQUARE, bool ROWS, bool COLS, bool GUARD, bool STREAM, bool NORM = false>
 __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const QuantBlocks t) {
     __shared__ __attribute__((aligned(16))) uint8_t s_t[COLS ? kTileLdsBytes : 16];
     __shared__ __attribute__((aligned(16))) unsigned s_mag[4][64];           // column pairs of each wave
@@ -86,6 +75,35 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Qua
     } else {
 #pragma unroll
         for (int i = 0; i < kPatchRows; ++i) in[i] = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(src + (int64_t)i * cols));
+    }
+    if constexpr (NORM) {
+        v4u wv;
+        float rs[kPatchRows];
+        if constexpr (GUARD) {
+            // (what does not exist counts as zero times zero)
+            wv = load8_upto(t.w + c0, c0, cols - c0);
+#pragma unroll
+            for (int i = 0; i < kPatchRows; ++i) rs[i] = r0 + i < t.rows ? t.rstd[r0 + i] : 0.0f;
+        } else {
+            wv = *reinterpret_cast<const v4u*>(t.w + c0);
+#pragma unroll
+            for (int i = 0; i < kPatchRows; i += 4) {
+                const v4f four = *reinterpret_cast<const v4f*>(t.rstd + r0 + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rs[i + k] = four[k];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPatchRows; ++i) in[i] = normalize8(in[i], rs[i], wv);
+        if (t.y) {
+            uint16_t* dst = t.y + r0 * cols + c0;
+            if constexpr (GUARD) {
+                store_patch_upto(in, dst, cols, t.rows - r0, cols - c0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPatchRows; ++i) *reinterpret_cast<v4u*>(dst + (int64_t)i * cols) = in[i];
+            }
+        }
     }
     // magnitudes: of rows i and i + 1 in one register each, of columns 2 k and 2 k + 1
     unsigned row_mag[kPatchRows / 2], col_mag[4] = {0, 0, 0, 0};
@@ -196,7 +214,7 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Qua
     }
 }
 
-template <int FMT, bool SQUARE, bool ROWS, bool COLS>
+template <int FMT, bool SQUARE, bool ROWS, bool COLS, bool NORM = false>
 static int launch_quantize_blocks(QuantBlocks t, hipStream_t stream) {
     const bool whole = t.rows % kTileRows == 0 && t.cols % kTileCols == 0;
     SmallGrid g{};
@@ -211,9 +229,9 @@ static int launch_quantize_blocks(QuantBlocks t, hipStream_t stream) {
     small_launches(g, [&](const SmallGrid& part, unsigned blocks) {
         t.grid = part;
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kTileThreads), 0, stream, t); };
-        if (!whole) launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, true, false>);
-        else if (stream_q) launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false, ROWS>);
-        else launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false, false>);
+        if (!whole) launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, true, false, NORM>);
+        else if (stream_q) launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false, ROWS, NORM>);
+        else launch(quantize_blocks_kernel<FMT, SQUARE, ROWS, COLS, false, false, NORM>);
     });
     return hipGetLastError() == hipSuccess ? LLMQ_OK : LLMQ_ERR_DEVICE;
 }
@@ -223,6 +241,12 @@ static int launch_copies(const QuantBlocks& t, hipStream_t stream) {
     if (t.q && t.qt) return launch_quantize_blocks<FMT, SQUARE, true, true>(t, stream);
     if (t.q) return launch_quantize_blocks<FMT, SQUARE, true, false>(t, stream);
     return launch_quantize_blocks<FMT, SQUARE, false, true>(t, stream);
+}
+
+int launch_norm_quantize_blocks(const void* res, const void* w, const float* rstd, int64_t M, int64_t C, int fmt, uint8_t* q, uint8_t* s, uint8_t* q_t, uint8_t* s_t, void* y, hipStream_t stream) {
+    const QuantBlocks t{static_cast<const uint16_t*>(res), M, C, q, s, q_t, s_t, {}, static_cast<const uint16_t*>(w), rstd, static_cast<uint16_t*>(y)};
+    if (fmt == LLMQ_E4M3) return q ? launch_quantize_blocks<0, false, true, true, true>(t, stream) : launch_quantize_blocks<0, false, false, true, true>(t, stream);
+    return q ? launch_quantize_blocks<1, false, true, true, true>(t, stream) : launch_quantize_blocks<1, false, false, true, true>(t, stream);
 }
 
 }  // namespace llmq
@@ -241,7 +265,7 @@ int llmq_quantize_fp8_blocks(const void* x_bf16, int64_t rows, int64_t cols, int
     if (!fmt_ok(fmt)) return LLMQ_ERR_FORMAT;
     if (block_rows != 1 && block_rows != 128) return LLMQ_ERR_FLAGS;
     if (!aligned(x_bf16, 16) || !aligned(q, 16) || !aligned(s, 16) || !aligned(q_t, 16) || !aligned(s_t, 16)) return LLMQ_ERR_ALIGN;
-    const llmq::QuantBlocks t{static_cast<const uint16_t*>(x_bf16), rows, cols, q, s, q_t, s_t, {}};
+    const llmq::QuantBlocks t{static_cast<const uint16_t*>(x_bf16), rows, cols, q, s, q_t, s_t, {}, nullptr, nullptr, nullptr};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (fmt == LLMQ_E4M3) return block_rows == 128 ? llmq::launch_copies<0, true>(t, st) : llmq::launch_copies<0, false>(t, st);
     return block_rows == 128 ? llmq::launch_copies<1, true>(t, st) : llmq::launch_copies<1, false>(t, st);

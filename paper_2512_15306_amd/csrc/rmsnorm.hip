@@ -22,33 +22,17 @@
 // 1 + 1 B written per element).
 #include <stdlib.h>
 
-#include "llmq_device.h"
-#include "llmq_kernels.h"
+#include "blocks.h"
+#include "rmsnorm.h"
 
 #pragma clang fp contract(off)
 
 namespace llmq {
 template <int N> struct IntTag { static constexpr int value = N; };
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float v2f __attribute__((ext_vector_type(2)));
-
 constexpr int kRnThreads = 256;
 constexpr int kRnRowsPerBlock = kRnThreads / kWave;        // one wavefront per row
 constexpr int64_t kRnVecOrderC = 8192;                      // widest row that one wave sums vector by vector
-
-__device__ inline unsigned rn_pack(float lo, float hi) {
-    v2f v = {lo, hi};
-    return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
-}
-__device__ inline float rn_lo(unsigned w) { return __uint_as_float(w << 16); }
-__device__ inline float rn_hi(unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-__device__ inline float wave_sum_f32(float v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
-    return v;
-}
 
 __device__ inline void add_squares(const v4u& r, float& ss) {
 #pragma unroll
@@ -72,25 +56,6 @@ __device__ inline float sum_by_elements(const uint16_t* s_row, int C, int lane) 
 __device__ inline unsigned fold_pairs(unsigned m0, unsigned m1, unsigned m2, unsigned m3) {
     m0 = pk_max_mag(pk_max_mag(m0, m1), pk_max_mag(m2, m3));
     return (m0 & 0xFFFFu) > (m0 >> 16) ? (m0 & 0xFFFFu) : (m0 >> 16);
-}
-
-// y = bf16((r * rstd) * w) for the eight elements of one 16-byte vector
-__device__ inline v4u normalize8(const v4u& r, float rstd, const v4u& w) {
-    v4u o;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float a = rn_lo(r[j]) * rstd, b = rn_hi(r[j]) * rstd;
-        o[j] = rn_pack(a * rn_lo(w[j]), b * rn_hi(w[j]));
-    }
-    return o;
-}
-
-// The first `valid` of eight elements, zeros for the others: what lies behind the end of a row counts for nothing, also where
-// 0 * rstd * w is NaN (a row whose squares underflow, eps = 0: rstd is infinite and the row's own results are too).
-__device__ inline v4u keep_upto(v4u v, int valid) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] &= (2 * j < valid ? 0xFFFFu : 0u) | (2 * j + 1 < valid ? 0xFFFF0000u : 0u);
-    return v;
 }
 
 // Vector idx of a row of C elements; EDGE: of any C, at any even address
@@ -132,14 +97,39 @@ __device__ inline void rn_store(uint16_t* row, int idx, int C, const v4u& v) {
     else store8_upto(row + 8 * idx, v, C - 8 * idx);
 }
 
+// What a forward kernel leaves of y: the values and a partial absmax for each workgroup; nothing (the statistics and the sum are all that is wanted: the codes are made in
+// tiles then, which hold every block of both copies whole); or codes with a scale for every 128 values of a row (kNormCodes + format), and the values if y is not NULL.
+constexpr int kNormY = 0, kNormStats = 1, kNormCodes = 2;
+struct NormCodes {
+    uint8_t *q, *s;
+    int64_t padded;                             // rows rounded up to a multiple of 128, bytes of a K step
+};
+
+// Codes of the vector idx of a row, which 15 neighbouring lanes' vectors share a block with; all lanes of the wave take part.
+template <int FMT, bool EDGE>
+__device__ inline void put_codes(const v4u& o, bool there, const NormCodes& out, int64_t row, int idx, int C) {
+    unsigned m = pk_max_u16(pk_max_u16(o[0] & 0x7FFF7FFFu, o[1] & 0x7FFF7FFFu), pk_max_u16(o[2] & 0x7FFF7FFFu, o[3] & 0x7FFF7FFFu));
+    m = max_of_16_lanes((m & 0xFFFFu) > (m >> 16) ? m & 0xFFFFu : m >> 16);
+    if (!there) return;
+    const unsigned code = scale_code<FMT>(m << 16), lo = cvt_four<FMT>(o[0], o[1], code), hi = cvt_four<FMT>(o[2], o[3], code);
+    uint8_t* dst = out.q + row * C + 8 * idx;
+    if constexpr (EDGE) store8_codes_upto(dst, lo, hi, C - 8 * idx);
+    else *reinterpret_cast<v2u*>(dst) = v2u{lo, hi};
+    if (idx % (kBlock / 8) == 0) out.s[(idx / (kBlock / 8)) * out.padded + code_place(row)] = (uint8_t)code;
+}
+// Codes of rows that do not exist, of which the last group of 128 may hold some
+__device__ inline void pad_codes(const NormCodes& out, int64_t row, int64_t C, int lane, int lanes) {
+    for (int64_t k = lane; k < (C + kBlock - 1) / kBlock; k += lanes) out.s[k * out.padded + code_place(row)] = 127;
+}
+
 // One wavefront per row, VPL vectors per lane in registers.  EDGE: any C (the rows start at any even address, the last
 // vector of a row may be a part of one); else C % 8 == 0.  HAS_X false: no addition (res is normalised as it is, res_out is not
 // written).
-template <bool HAS_X, bool EDGE, int VPL>
+template <bool HAS_X, bool EDGE, int VPL, int OUT = kNormY>
 __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
     const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
     int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
-    float* __restrict__ rstd_out, unsigned* __restrict__ partial) {
+    float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
     // res_out may be res (addition in place): every lane reads its elements before it writes them
     __shared__ unsigned s_part[kRnThreads / kWave];
     __shared__ v4u s_rows[kRnRowsPerBlock][EDGE ? VPL * kWave : 1];
@@ -187,6 +177,21 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
         const float ms = ss / (float)C;
         const float rstd = 1.0f / __builtin_sqrtf(ms + eps);
         if (lane == 0) rstd_out[row] = rstd;
+        if constexpr (OUT >= kNormCodes) {
+#pragma unroll
+            for (int k = 0; k < VPL; ++k) {
+                const int idx = k * kWave + lane;
+                if (k * kWave >= nvec) break;
+                v4u o = {0, 0, 0, 0};
+                if (idx < nvec) {
+                    o = normalize8(r[k], rstd, EDGE ? load8_upto(w + 8 * idx, 8 * idx, C - 8 * idx) : reinterpret_cast<const v4u*>(w)[idx]);
+                    if (EDGE && idx == nvec - 1) o = keep_upto(o, C % 8);
+                    if (y) store(y + row * C, idx, o);
+                }
+                put_codes<OUT - kNormCodes, EDGE>(o, idx < nvec, codes, row, idx, C);
+            }
+        }
+        if constexpr (OUT != kNormY) return;
         unsigned m0 = 0, m1 = 0, m2 = 0, m3 = 0;
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
@@ -205,9 +210,13 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
             }
         }
         mag = fold_pairs(m0, m1, m2, m3);
+    } else if constexpr (OUT >= kNormCodes) {
+        if (row < codes.padded) pad_codes(codes, row, C, lane, kWave);
     }
-    mag = block_max_u32<kRnThreads>(mag, s_part);
-    if (threadIdx.x == 0) partial[blockIdx.x] = mag;
+    if constexpr (OUT == kNormY) {
+        mag = block_max_u32<kRnThreads>(mag, s_part);
+        if (threadIdx.x == 0) partial[blockIdx.x] = mag;
+    }
 }
 
 // Wider rows: the four rows of a workgroup are read by all of its lanes (VPL vectors per lane and row, two rows at a time),
@@ -217,12 +226,13 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
 // instead of 73).  Measured against
 // one wave per row with up to 16 vectors per lane, with the addition: 16384 x 5120 137 -> 130 us (5.2 TB/s), 8192 x 3584
 // 52 -> 46, 4096 x 7680 59 -> 51, 279 x 7680 21 -> 14; all four rows at a time took 134, 48, 63 and 14.
-template <bool HAS_X, bool EDGE, int VPL, bool STREAM>
+// PER_BLOCK: rows of a workgroup; one where there are so few that each has a workgroup to itself.
+template <bool HAS_X, bool EDGE, int VPL, bool STREAM, int OUT = kNormY, int PER_BLOCK = kRnRowsPerBlock>
 __global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
     const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
     int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
-    float* __restrict__ rstd_out, unsigned* __restrict__ partial) {
-    constexpr int ROWS = VPL <= 4 ? 2 : 1;
+    float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
+    constexpr int ROWS = VPL <= 4 && PER_BLOCK > 1 ? 2 : 1;
     constexpr bool ONE_WAVE = !EDGE && VPL * kRnThreads * 8 <= kRnVecOrderC;        // sums a row (VPL > 4 is for wider ones)
     constexpr int kWaves = kRnThreads / kWave;
     __shared__ unsigned s_part[kWaves];
@@ -233,9 +243,15 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
     const int nvec = EDGE ? (C + 7) / 8 : C / 8;
     unsigned m0 = 0, m1 = 0, m2 = 0, m3 = 0;
 #pragma unroll 1
-    for (int p = 0; p < kRnRowsPerBlock; p += ROWS) {
-        const int64_t row = (int64_t)blockIdx.x * kRnRowsPerBlock + p;
-        if (row >= M) break;                                 // the same for the whole workgroup
+    for (int p = 0; p < PER_BLOCK; p += ROWS) {
+        const int64_t row = (int64_t)blockIdx.x * PER_BLOCK + p;
+        if (row >= M) {                                      // the same for the whole workgroup
+            if constexpr (OUT >= kNormCodes) {
+                for (int i = 0; i < PER_BLOCK - p; ++i)
+                    if (row + i < codes.padded) pad_codes(codes, row + i, C, threadIdx.x, kRnThreads);
+            }
+            break;
+        }
         // Byte offset of the lane's k-th vector.  Opaque in every trip, or the compiler keeps an address for each vector of each tensor across them.
         unsigned lane_at = 16u * threadIdx.x;
         if constexpr (EDGE) asm volatile("" : "+v"(lane_at));
@@ -305,6 +321,33 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
                 if (threadIdx.x == 0 && row + i < M) rstd_out[row + i] = rstd[i];
             }
         }
+        if constexpr (OUT >= kNormCodes) {
+#pragma unroll
+            for (int k = 0; k < VPL; ++k) {
+                const int idx = k * kRnThreads + threadIdx.x;
+                v4u wv = {0, 0, 0, 0};
+                if (idx < nvec) {
+                    if constexpr (EDGE) wv = *rn_vector(w, at(k), C);
+                    else wv = reinterpret_cast<const v4u*>(w)[idx];
+                }
+                rn_last<EDGE>(wv, k, nvec - 1, C);
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    if (row + i >= M) {
+                        if (k == 0 && row + i < codes.padded) pad_codes(codes, row + i, C, threadIdx.x, kRnThreads);
+                        continue;
+                    }
+                    v4u o = {0, 0, 0, 0};
+                    if (idx < nvec) {
+                        o = normalize8(r[i][k], rstd[i], wv);
+                        if (EDGE && idx == nvec - 1) o = keep_upto(o, C % 8);
+                        if (y) rn_store_wide<EDGE, false>(y + (row + i) * C, idx, at(k), nvec - 1, C, o);
+                    }
+                    put_codes<OUT - kNormCodes, EDGE>(o, idx < nvec, codes, row + i, idx, C);
+                }
+            }
+        }
+        if constexpr (OUT != kNormY) continue;
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
             const int idx = k * kRnThreads + threadIdx.x;
@@ -327,16 +370,19 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
             }
         }
     }
-    const unsigned mag = block_max_u32<kRnThreads>(fold_pairs(m0, m1, m2, m3), s_part);
-    if (threadIdx.x == 0) partial[blockIdx.x] = mag;
+    if constexpr (OUT == kNormY) {
+        const unsigned mag = block_max_u32<kRnThreads>(fold_pairs(m0, m1, m2, m3), s_part);
+        if (threadIdx.x == 0) partial[blockIdx.x] = mag;
+    }
 }
 
 // More than 16384 columns: one wavefront per row, element-wise strided loops; the row is read again for the second pass
 // (from res_out when the addition was done).
+template <int OUT = kNormY>
 __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_generic_kernel(
     const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
     int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
-    float* __restrict__ rstd_out, unsigned* __restrict__ partial) {
+    float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
     __shared__ unsigned s_part[kRnThreads / kWave];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = threadIdx.x / kWave;
@@ -358,15 +404,38 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_generic_kernel(
         const float rstd = 1.0f / __builtin_sqrtf(ms + eps);
         if (lane == 0) rstd_out[row] = rstd;
         const uint16_t* src = x ? res_out : res;          // this lane re-reads exactly the elements it wrote
+        if constexpr (OUT >= kNormCodes) {
+            // a block of 128 columns at a time, of which a lane has columns lane and lane + 64
+            for (int64_t c0 = 0; c0 < C; c0 += kBlock) {
+                unsigned o[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t c = c0 + h * kWave + lane;
+                    o[h] = 0;
+                    if (c < C) o[h] = rn_pack((__uint_as_float((unsigned)src[row * C + c] << 16) * rstd) * __uint_as_float((unsigned)w[c] << 16), 0.0f) & 0xFFFFu;
+                    if (y && c < C) y[row * C + c] = (uint16_t)o[h];
+                }
+                const unsigned a = o[0] & 0x7FFFu, b = o[1] & 0x7FFFu, code = scale_code<OUT - kNormCodes>(wave_max_u32(a > b ? a : b) << 16);
+                const unsigned two = cvt_scaled<OUT - kNormCodes, false>(o[0] | o[1] << 16, code, 0u);
+                if (c0 + lane < C) codes.q[row * C + c0 + lane] = (uint8_t)two;
+                if (c0 + kWave + lane < C) codes.q[row * C + c0 + kWave + lane] = (uint8_t)(two >> 8);
+                if (lane == 0) codes.s[(c0 / kBlock) * codes.padded + code_place(row)] = (uint8_t)code;
+            }
+        }
+        if constexpr (OUT != kNormY) return;
         for (int64_t c = lane; c < C; c += kWave) {
             const float t = __uint_as_float((unsigned)src[row * C + c] << 16) * rstd;
             const unsigned o = rn_pack(t * __uint_as_float((unsigned)w[c] << 16), 0.0f) & 0xFFFFu;
             y[row * C + c] = (uint16_t)o;
             mag = pk_max_mag(mag, o);
         }
+    } else if constexpr (OUT >= kNormCodes) {
+        if (row < codes.padded) pad_codes(codes, row, C, lane, kWave);
     }
-    mag = block_max_u32<kRnThreads>(mag & 0xFFFFu, s_part);
-    if (threadIdx.x == 0) partial[blockIdx.x] = mag;
+    if constexpr (OUT == kNormY) {
+        mag = block_max_u32<kRnThreads>(mag & 0xFFFFu, s_part);
+        if (threadIdx.x == 0) partial[blockIdx.x] = mag;
+    }
 }
 
 // Recompute path: rstd [M] and the scale are given, no transposed copy.  Lane = 4 rows x 8 columns; M % 4 == 0, C % 8 == 0.
@@ -580,7 +649,7 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
     uint16_t* res_out = reinterpret_cast<uint16_t*>(res_out_);
     uint16_t* y = reinterpret_cast<uint16_t*>(y_);
     const dim3 grid((unsigned)rmsnorm_blocks(M)), block(kRnThreads);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, partial); };
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, partial, NormCodes{}); };
     const bool edge = C % 8 != 0;
     auto row = [&](auto vpl) {
         constexpr int V = decltype(vpl)::value;
@@ -596,7 +665,7 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
         else { if (edge) launch(rmsnorm_rows_kernel<false, true, V, false>); else if (out) launch(rmsnorm_rows_kernel<false, false, V, true>); else launch(rmsnorm_rows_kernel<false, false, V, false>); }
     };
     switch (norm_kind(M, C, x != nullptr)) {
-        case kNormGeneric: hipLaunchKernelGGL(rmsnorm_row_generic_kernel, grid, block, 0, stream, res, x, w, M, C, eps, res_out, y, rstd, partial); break;
+        case kNormGeneric: hipLaunchKernelGGL(rmsnorm_row_generic_kernel<>, grid, block, 0, stream, res, x, w, M, C, eps, res_out, y, rstd, partial, NormCodes{}); break;
         case kNormRow:
             // (As few registers as the row needs, but for a few workgroups per CU: those are dealt out evenly only if few fit
             // on one.  3000 x 3584 with 8 and 16 vectors per lane: 21.4 / 19.1 us, 4001 x 3584 24.7 / 29.4.)
@@ -614,6 +683,64 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
     }
     if (hipGetLastError() != hipSuccess) return -6;
     return launch_amax_final(partial, (int)rmsnorm_blocks(M), fmt, d_amax, d_scale, stream);
+}
+
+// The statistics and the residual sum, and the row-wise codes with block scales if there are any (codes.q): the kernels and the order of the sums of launch_rmsnorm_fwd.
+template <int OUT>
+static void launch_rows_out(const uint16_t* res, const uint16_t* x, const uint16_t* w, int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* y, float* rstd, const NormCodes& codes,
+                            hipStream_t stream, int cus) {
+    const int64_t rows_written = OUT >= kNormCodes ? codes.padded : M;
+    const bool edge = C % 8 != 0;
+    auto launch = [&](auto kernel, int per_block) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows_written + per_block - 1) / per_block)), dim3(kRnThreads), 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, nullptr, codes);
+    };
+    auto row = [&](auto vpl) {
+        constexpr int V = decltype(vpl)::value;
+        if constexpr (V <= 4) {
+            if (edge) { if (x) launch(rmsnorm_row_kernel<true, true, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_kernel<false, true, V, OUT>, kRnRowsPerBlock); return; }
+        }
+        if (x) launch(rmsnorm_row_kernel<true, false, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_kernel<false, false, V, OUT>, kRnRowsPerBlock);
+    };
+    const bool one = M <= 2 * cus;
+    auto rows = [&](auto vpl) {
+        constexpr int V = decltype(vpl)::value;
+        auto of = [&](auto has_x, auto at_edge) {
+            constexpr bool X = decltype(has_x)::value, E = decltype(at_edge)::value;
+            if (one) launch(rmsnorm_rows_kernel<X, E, V, false, OUT, 1>, 1);
+            else launch(rmsnorm_rows_kernel<X, E, V, false, OUT>, kRnRowsPerBlock);
+        };
+        if (x) edge ? of(std::true_type{}, std::true_type{}) : of(std::true_type{}, std::false_type{});
+        else edge ? of(std::false_type{}, std::true_type{}) : of(std::false_type{}, std::false_type{});
+    };
+    NormKind kind = norm_kind(M, C, x != nullptr);
+    if (kind == kNormRow && one && C > 4 * kWave * 8) kind = kNormRows;
+    switch (kind) {
+        case kNormGeneric:
+            hipLaunchKernelGGL(rmsnorm_row_generic_kernel<OUT>, dim3((unsigned)((rows_written + kRnRowsPerBlock - 1) / kRnRowsPerBlock)), dim3(kRnThreads), 0, stream, res, x, w, M, C, eps, res_out, y, rstd,
+                               nullptr, codes);
+            break;
+        case kNormRow:
+            if (C <= 4 * kWave * 8) row(IntTag<4>{});
+            else if (C <= 8 * kWave * 8) row(IntTag<8>{});
+            else if (C <= 12 * kWave * 8) row(IntTag<12>{});
+            else row(IntTag<16>{});
+            break;
+        case kNormRows:
+            if (C <= 2 * kRnThreads * 8) rows(IntTag<2>{});
+            else if (C <= 3 * kRnThreads * 8) rows(IntTag<3>{});
+            else if (C <= 4 * kRnThreads * 8) rows(IntTag<4>{});
+            else rows(IntTag<8>{});
+    }
+}
+
+int launch_rmsnorm_rows(const void* res_, const void* x_, const void* w_, int64_t M, int64_t C, float eps, void* res_out_, void* y_, float* rstd, int fmt, uint8_t* q, uint8_t* s, hipStream_t stream, int cus) {
+    const uint16_t *res = static_cast<const uint16_t*>(res_), *x = static_cast<const uint16_t*>(x_), *w = static_cast<const uint16_t*>(w_);
+    uint16_t *res_out = static_cast<uint16_t*>(res_out_), *y = static_cast<uint16_t*>(y_);
+    const NormCodes codes{q, s, (M + kBlock - 1) / kBlock * kBlock};
+    if (!q) launch_rows_out<kNormStats>(res, x, w, M, C, eps, res_out, y, rstd, codes, stream, cus);
+    else if (fmt == 0) launch_rows_out<kNormCodes + 0>(res, x, w, M, C, eps, res_out, y, rstd, codes, stream, cus);
+    else launch_rows_out<kNormCodes + 1>(res, x, w, M, C, eps, res_out, y, rstd, codes, stream, cus);
+    return hipGetLastError() == hipSuccess ? 0 : -6;
 }
 
 // The recompute call's kernel where it is not the large tile's or, without the transposed copy, that of whole 4 x 8 patches.

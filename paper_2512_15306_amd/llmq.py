@@ -38,6 +38,7 @@ EXPORTS = ["llmq_status_string", "llmq_version", "llmq_amax_workspace_bytes", "l
            "llmq_fp8_linear_fwd", "llmq_fp8_linear_dgrad", "llmq_fp8_linear_wgrad",
            "llmq_scale_from_amax", "llmq_swiglu_workspace_bytes", "llmq_swiglu_fwd", "llmq_swiglu_fwd_fp8", "llmq_swiglu_fwd_fp8_slabs",
            "llmq_swiglu_bwd", "llmq_rmsnorm_workspace_bytes", "llmq_rmsnorm_fwd", "llmq_rmsnorm_apply_fp8", "llmq_rmsnorm_apply_fp8_slabs",
+           "llmq_rmsnorm_fwd_fp8_blocks", "llmq_rmsnorm_bwd_workspace_bytes", "llmq_rmsnorm_bwd",
            "llmq_block_scales_bytes", "llmq_quantize_fp8_blocks", "llmq_fp8_gemm_blocks",
            "llmq_qk_norm_rope_fwd", "llmq_qk_norm_rope_workspace_bytes", "llmq_qk_norm_rope_bwd",
            "llmq_adamw_plan_bytes", "llmq_adamw_plan", "llmq_adamw_hyper", "llmq_adamw_step",
@@ -125,6 +126,12 @@ def lib() -> ctypes.CDLL:
     L.llmq_rmsnorm_apply_fp8.argtypes = [vp, vp, vp, i64, i64, vp, i32, vp, vp, vp, vp]
     L.llmq_rmsnorm_apply_fp8_slabs.restype = i32
     L.llmq_rmsnorm_apply_fp8_slabs.argtypes = [vp, vp, vp, i64, i64, vp, i32, vp, vp, vp, vp]
+    L.llmq_rmsnorm_fwd_fp8_blocks.restype = i32
+    L.llmq_rmsnorm_fwd_fp8_blocks.argtypes = [vp, vp, vp, i64, i64, c.c_float, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    L.llmq_rmsnorm_bwd_workspace_bytes.restype = sz
+    L.llmq_rmsnorm_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.llmq_rmsnorm_bwd.restype = i32
+    L.llmq_rmsnorm_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, i32, i32, vp, vp, vp, sz, vp]
     L.llmq_block_scales_bytes.restype = sz
     L.llmq_block_scales_bytes.argtypes = [i64, i64]
     L.llmq_quantize_fp8_blocks.restype = i32
@@ -561,6 +568,37 @@ def llmq_fp8_gemm_blocks(A: torch.Tensor, sA: torch.Tensor, fmtA: int, B: torch.
                                       _here(B, torch.uint8, "B"), _here(sB, torch.uint8, "sB", llmq_block_scales_bytes(C, T)), fmtB, R, C, T,
                                       _here(c, torch.bfloat16, "c"), int(bool(accumulate)), _here(d_amax_c, torch.float32, "d_amax_c", 1), _stream()),
            "llmq_fp8_gemm_blocks")
+
+
+def llmq_rmsnorm_fwd_fp8_blocks(res: torch.Tensor, x: Optional[torch.Tensor], w: torch.Tensor, eps: float, res_out: Optional[torch.Tensor], rstd: torch.Tensor, fmt: int,
+                                q: Optional[torch.Tensor], s: Optional[torch.Tensor], q_t: Optional[torch.Tensor] = None, s_t: Optional[torch.Tensor] = None,
+                                y: Optional[torch.Tensor] = None) -> None:
+    """s and s_t: uint8, llmq_block_scales_bytes(M, C) and llmq_block_scales_bytes(C, M) elements."""
+    status = _fast.rmsnorm_fwd_fp8_blocks(res, x, w, eps, res_out, rstd, fmt, q, s, q_t, s_t, y)
+    if status is not None:
+        return _check(status, "llmq_rmsnorm_fwd_fp8_blocks") if status else None
+    M, C = _matrix(res, "res")
+    n, bf16 = M * C, torch.bfloat16
+    _check(lib().llmq_rmsnorm_fwd_fp8_blocks(_here(res, bf16, "res"), _here(x, bf16, "x", n), _here(w, bf16, "w", C), M, C, float(eps), _here(res_out, bf16, "res_out", n),
+                                             _here(rstd, torch.float32, "rstd", M), fmt, _here(q, torch.uint8, "q", n), _here(s, torch.uint8, "s", llmq_block_scales_bytes(M, C)),
+                                             _here(q_t, torch.uint8, "q_t", n), _here(s_t, torch.uint8, "s_t", llmq_block_scales_bytes(C, M)), _here(y, bf16, "y", n), _stream()),
+           "llmq_rmsnorm_fwd_fp8_blocks")
+
+
+def llmq_rmsnorm_bwd_workspace_bytes(M: int, C: int) -> int:
+    return int(lib().llmq_rmsnorm_bwd_workspace_bytes(M, C))
+
+
+def llmq_rmsnorm_bwd(dy: torch.Tensor, dres: Optional[torch.Tensor], res: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor, dw: Optional[torch.Tensor], accumulate: bool,
+                     fmt: int, d_amax: Optional[torch.Tensor], d_scale: Optional[torch.Tensor], ws: Optional[torch.Tensor]) -> None:
+    status = _fast.rmsnorm_bwd(dy, dres, res, w, rstd, dx, dw, accumulate, fmt, d_amax, d_scale, ws)
+    if status is not None:
+        return _check(status, "llmq_rmsnorm_bwd") if status else None
+    M, C = _matrix(res, "res")
+    n, bf16, f32 = M * C, torch.bfloat16, torch.float32
+    _check(lib().llmq_rmsnorm_bwd(_here(dy, bf16, "dy", n), _here(dres, bf16, "dres", n), _here(res, bf16, "res"), _here(w, bf16, "w", C), _here(rstd, f32, "rstd", M), M, C,
+                                  _here(dx, bf16, "dx", n), _here(dw, f32, "dw", C), int(bool(accumulate)), fmt, _here(d_amax, f32, "d_amax", 1), _here(d_scale, f32, "d_scale", 1),
+                                  _here(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(), _stream()), "llmq_rmsnorm_bwd")
 
 
 def _rows(t: Optional[torch.Tensor], M: int, width: int, name: str) -> Tuple[Optional[int], int]:
