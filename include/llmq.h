@@ -246,6 +246,30 @@ int llmq_fp8_gemm_blocks(const uint8_t* A, const uint8_t* sA, int fmtA, const ui
                          int64_t R, int64_t C, int64_t T, void* c_bf16, int accumulate, float* d_amax_c, void* stream);
 
 /*
+ * The two products of a gated feed-forward block that meet its SwiGLU, from operands with block scales, each with the non-linearity in the same kernel.
+ *
+ * llmq_fp8_gemm_blocks_swiglu_fwd: both projections of a block and its non-linearity.  A [M, T] codes of the input and sA; W [2 I, T] codes of the gate and up weights and sW, as one operand: rows [0, I) are the
+ *   gate's, rows [I, 2 I) the up branch's (the layout of GU that llmq_swiglu_fwd reads):
+ *     g[m,i] = sum_t A[m,t] dA W[i,t] dW,   u[m,i] = sum_t A[m,t] dA W[I+i,t] dW,   h[m,i] = bf16( silu(g) u ),  silu(g) = g sg,  sg = 1 / (1 + e^-g)
+ *   h [M, I] BF16; gu [M, 2 I] BF16 receives bf16(g) and bf16(u) for the backward pass if it is not NULL.  h is made from the sums in binary32, not from their rounded values, and does not depend on whether gu is wanted.
+ * llmq_fp8_gemm_blocks_swiglu_bwd: the gradient through the down projection and the non-linearity.  A [M, T] codes of dY (T the model's width) and sA; B [I, T] codes of the transposed copy of the down projection's weight
+ *   [T, I] and sB; gu [M, 2 I] what the forward pass kept:
+ *     dh[m,i] = sum_t A[m,t] dA B[i,t] dB  (binary32, not rounded);   dgu[m, i] = bf16( dh u sg (1 + g (1 - sg)) ),   dgu[m, I+i] = bf16( dh g sg )
+ *   dgu [M, 2 I] BF16, the dY of the gate and up projections; h [M, I] BF16 receives bf16( g sg u ) of the kept gu for the down projection's weight gradient if it is not NULL.  dgu may be gu itself.
+ *   d_amax_h, d_amax_dgu [1] float or NULL: absmax of h or dgu, as llmq_amax of them has it.
+ * Sums as in llmq_fp8_gemm_blocks: products exact, their error bounded by 2^-7 of the sum of the products' magnitudes; up to 32 rows take a kernel that adds in another order.  The exponential and the reciprocal are the
+ *   hardware's: sg is off by at most 2^-20 + 2^-24 |g| of it; for g < -87, where |silu(g)| < 2^-118, h may be +-0.  A sum that is no number makes its own output NaN, no other.
+ * fmtA: E4M3 or E5M2, the weights E4M3 (LLMQ_ERR_FORMAT otherwise).  16 <= T < 2^22, I < 2^21, (rows of an operand rounded up to 128) ceil(T / 128) < 2^31 - 4096, 128 x 64 tiles of [M, I] below 2^24 (LLMQ_ERR_SHAPE).
+ * Fastest with M a multiple of 256, I of 128 and T of 128; I a multiple of 32 (forward; any multiple of 8 backward) and T of 16 otherwise.  All pointers 16-byte aligned (d_amax: 4).
+ */
+int llmq_fp8_gemm_blocks_swiglu_fwd(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* W, const uint8_t* sW,
+                                    int fmtW, int64_t M, int64_t I, int64_t T, void* h_bf16, void* gu_bf16,
+                                    float* d_amax_h, void* stream);
+int llmq_fp8_gemm_blocks_swiglu_bwd(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* B, const uint8_t* sB,
+                                    int fmtB, const void* gu_bf16, int64_t M, int64_t I, int64_t T, void* dgu_bf16,
+                                    void* h_bf16, float* d_amax_dgu, void* stream);
+
+/*
  * Workspace of the three linear-layer calls below, for one (M, N, K).  It holds the FP8 copies
  *   Xq [M,K], Wq [N,K], dYq [M,N], then 12 KB of scratch for the LLMQ_JIT_* flags, then
  *   Xq_t [K,M], Wq_t [K,N], dYq_t [N,M],

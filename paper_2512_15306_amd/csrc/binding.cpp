@@ -372,6 +372,51 @@ LLMQ_BINDING(fp8_gemm_blocks) {
     });
 }
 
+LLMQ_BINDING(fp8_gemm_blocks_swiglu_fwd) {
+    return run(args, n, 9, [](Args& args_) {
+        HereArgs a(args_);
+        int64_t M = 0, T = 0, both = 0, T2 = 0, M2 = 0, I = 0;
+        a.dims(0, kU8, M, T);
+        a.dims(3, kU8, both, T2);
+        a.dims(6, kBf16, M2, I);
+        if (T != T2 || M2 != M || both != 2 * I) a.ok = false;
+        uint8_t *A = a.codes(0, -1, true), *sA = a.codes(1, (int64_t)llmq_block_scales_bytes(M, T), true);
+        const int fmt_a = a.i32(2), fmt_b = a.i32(5);
+        uint8_t *W = a.codes(3, -1, true), *sW = a.codes(4, (int64_t)llmq_block_scales_bytes(both, T), true);
+        void* h = a.pointer(6, kBf16, -1, true);
+        int64_t M3 = M, both3 = both;
+        if (a.ok && a.a[7] != Py_None) a.dims(7, kBf16, M3, both3);
+        if (M3 != M || both3 != both) a.ok = false;
+        void* gu = a.pointer(7, kBf16, -1, false);
+        float* amax = static_cast<float*>(a.pointer(8, kF32, 1, false));
+        args_.ok = a.ok;
+        return [=](void* stream) { return llmq_fp8_gemm_blocks_swiglu_fwd(A, sA, fmt_a, W, sW, fmt_b, M, I, T, h, gu, amax, stream); };
+    });
+}
+
+LLMQ_BINDING(fp8_gemm_blocks_swiglu_bwd) {
+    return run(args, n, 10, [](Args& args_) {
+        HereArgs a(args_);
+        int64_t M = 0, T = 0, I = 0, T2 = 0, M2 = 0, both = 0, M3 = 0, both3 = 0;
+        a.dims(0, kU8, M, T);
+        a.dims(3, kU8, I, T2);
+        a.dims(6, kBf16, M2, both);
+        a.dims(7, kBf16, M3, both3);
+        if (T != T2 || M2 != M || M3 != M || both != 2 * I || both3 != 2 * I) a.ok = false;
+        uint8_t *A = a.codes(0, -1, true), *sA = a.codes(1, (int64_t)llmq_block_scales_bytes(M, T), true);
+        const int fmt_a = a.i32(2), fmt_b = a.i32(5);
+        uint8_t *B = a.codes(3, -1, true), *sB = a.codes(4, (int64_t)llmq_block_scales_bytes(I, T), true);
+        void *gu = a.pointer(6, kBf16, -1, true), *dgu = a.pointer(7, kBf16, -1, true);
+        int64_t M4 = M, I4 = I;
+        if (a.ok && a.a[8] != Py_None) a.dims(8, kBf16, M4, I4);
+        if (M4 != M || I4 != I) a.ok = false;
+        void* h = a.pointer(8, kBf16, -1, false);
+        float* amax = static_cast<float*>(a.pointer(9, kF32, 1, false));
+        args_.ok = a.ok;
+        return [=](void* stream) { return llmq_fp8_gemm_blocks_swiglu_bwd(A, sA, fmt_a, B, sB, fmt_b, gu, M, I, T, dgu, h, amax, stream); };
+    });
+}
+
 LLMQ_BINDING(rmsnorm_fwd_fp8_blocks) {
     return run(args, n, 12, [](Args& args_) {
         HereArgs a(args_);
@@ -483,7 +528,7 @@ LLMQ_BINDING(adamw_step) {
 PyMethodDef g_methods[] = {LLMQ_METHOD(linear_fwd), LLMQ_METHOD(linear_dgrad), LLMQ_METHOD(linear_wgrad), LLMQ_METHOD(amax), LLMQ_METHOD(quantize_fp8),
                            LLMQ_METHOD(quantize_fp8_slabs), LLMQ_METHOD(bf16_gemm_tn), LLMQ_METHOD(swiglu_fwd), LLMQ_METHOD(swiglu_fwd_fp8),
                            LLMQ_METHOD(swiglu_fwd_fp8_slabs), LLMQ_METHOD(swiglu_bwd), LLMQ_METHOD(rmsnorm_fwd), LLMQ_METHOD(rmsnorm_apply_fp8),
-                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(rmsnorm_fwd_fp8_blocks), LLMQ_METHOD(rmsnorm_bwd), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), LLMQ_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                           LLMQ_METHOD(rmsnorm_apply_fp8_slabs), LLMQ_METHOD(quantize_fp8_blocks), LLMQ_METHOD(fp8_gemm_blocks), LLMQ_METHOD(fp8_gemm_blocks_swiglu_fwd), LLMQ_METHOD(fp8_gemm_blocks_swiglu_bwd), LLMQ_METHOD(rmsnorm_fwd_fp8_blocks), LLMQ_METHOD(rmsnorm_bwd), LLMQ_METHOD(qk_norm_rope_fwd), LLMQ_METHOD(qk_norm_rope_bwd), LLMQ_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

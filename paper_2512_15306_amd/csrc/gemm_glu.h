@@ -1,0 +1,518 @@
+// Contractions of FP8 operands with block scales, joined with the SwiGLU behind them (llmq_fp8_gemm_blocks_swiglu_fwd) or in front of them (_bwd).
+//
+//   forward   g = A Wg^T, u = A Wu^T;   h = bf16( silu(g) u ),  silu(g) = g sg,  sg = 1 / (1 + e^-g);   GU = bf16(g), bf16(u) if wanted
+//   backward  dh = A B^T;   dG = bf16( dh u sg (1 + g (1 - sg)) ),  dU = bf16( dh g sg ) from the kept GU;   h = bf16( g sg u ) if wanted
+//
+// The contraction is the tile kernel's (gemm_tile.h) and that for few rows; what is joined to it works on the sums where they are, so that GU (forward) and dh (backward) need not be
+// written and read again, and dh is not rounded in between.  In the forward pass a tile's columns are pairs: half of them of gate rows, half of the up rows that belong to them, dealt out so that a lane has both sums of
+// a pair.  e^-g and the reciprocal are the hardware's (v_exp_f32, v_rcp_f32: errors of 2^-23 and, from the product in front of the exponential, |g| 2^-24 of the result), which BF16 does not see and which
+// take 5 instructions; every one of them is time in which the matrix cores of its CU wait.
+#pragma once
+#include "gemm_small.h"
+
+namespace llmq {
+
+struct GluPlan {
+    int n_whole;                                // tiles
+    const uint16_t* gu;                         // backward: the kept GU [M, 2 I]
+    uint16_t *gu_out, *h_out;                   // forward: GU, backward: h; or NULL
+};
+
+__device__ inline float glu_sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g)); }
+__device__ inline float glu_value(float g, float u) { return g * glu_sigmoid(g) * u; }
+// dG and dU, and h
+__device__ inline void glu_gradient(float dh, float g, float u, float& dg, float& du, float& h) {
+    const float sg = glu_sigmoid(g), s = g * sg, d = dh * sg;
+    du = dh * s;
+    dg = d * u * __builtin_fmaf(g, 1.0f - sg, 1.0f);
+    h = s * u;
+}
+__device__ inline float bf16_lo(unsigned w) { return __uint_as_float(w << 16); }
+__device__ inline float bf16_hi(unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ inline v2u bf16_of(const v4f& v) { return __builtin_bit_cast(v2u, __builtin_convertvector(v, bf16x4)); }
+
+// A wave's part of a BF16 matrix whose rows are `ld` elements apart, 32 rows of it at a time and eight columns to a lane and piece.
+// EDGE kinds go through a buffer that ends with the last element there is; widths that are no multiples of 8 element by element.
+template <int EDGE>
+struct GluRows {
+    uint16_t* base;
+    __amdgpu_buffer_rsrc_t rs;
+    int ld, rows_left, cols_left;
+    bool vector;
+    // first element of the part; rows_left, cols_left of the whole matrix from there on (may be <= 0)
+    __device__ GluRows(const uint16_t* p, int ld_, int tile_rows, int rows_left_, int cols_left_, bool vector_)
+        : base(const_cast<uint16_t*>(p)), ld(ld_), rows_left(rows_left_), cols_left(cols_left_), vector(vector_) {
+        const int here = rows_left < tile_rows ? rows_left : tile_rows;
+        if constexpr (EDGE != kNoEdge) rs = make_rsrc(base, here > 0 && cols_left > 0 ? (unsigned)(((size_t)(here - 1) * ld + cols_left) * 2) : 0u);
+    }
+    static constexpr int kOut = 0x7FFFFF00;
+    __device__ int offset(int r, int c) const { return c < cols_left ? (r * ld + c) * 2 : kOut; }
+    __device__ v4u load(int r, int c) const {
+        if constexpr (EDGE == kNoEdge) return *reinterpret_cast<const v4u*>(base + (size_t)r * ld + c);
+        if (vector) return __builtin_amdgcn_raw_buffer_load_b128(rs, offset(r, c), 0, 0);
+        v4u v = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, offset(r, c + 2 * e), 0, 0) |
+                   (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, offset(r, c + 2 * e + 1), 0, 0) << 16;
+        return v;
+    }
+    // and the magnitudes of what is stored
+    __device__ void store(int r, int c, const v4u& v, unsigned& mag) const {
+        if constexpr (EDGE == kNoEdge) {
+            *reinterpret_cast<v4u*>(base + (size_t)r * ld + c) = v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mag = pk_max_mag(mag, v[e]);
+        } else if (vector) {
+            __builtin_amdgcn_raw_buffer_store_b128(v, rs, offset(r, c), 0, 0);
+            if (r < rows_left && c < cols_left) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mag = pk_max_mag(mag, v[e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned short bits = (unsigned short)(e & 1 ? v[e >> 1] >> 16 : v[e >> 1]);
+                __builtin_amdgcn_raw_buffer_store_b16(bits, rs, offset(r, c + e), 0, 0);
+                if (r < rows_left && c + e < cols_left) mag = pk_max_mag(mag, (unsigned)bits);
+            }
+        }
+    }
+};
+
+// Epilogue of the forward tile.  A lane holds, of block (i, j), four consecutive pairs of a row: their gates in columns j of the wave tile and their ups in columns MJ / 2 + j.  The wave's
+// results go through its part of LDS 32 rows at a time and leave in rows (gemm_tile.h, the epilogue of the plain contraction, has the layout and its reasons).
+template <int NI, int MI, int MJ, int EDGE, class Acc>
+__device__ __attribute__((always_inline)) inline unsigned glu_forward_out(const Acc& acc, uint8_t* stage, uint16_t* h, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
+    constexpr int HJ = MJ / 2, kSlots = 2 * HJ, kPitch = 16 * kSlots, kPlane = 32 * kPitch, kPieces = 32 * kSlots / kWave;
+    static_assert(kPieces >= 1 && kWave % kSlots == 0, "every lane moves whole pieces");
+    const int fr_row = lane & 15, fr_q = lane >> 4, slot0 = fr_q >> 1, half_off = (fr_q & 1) << 3;
+    const bool vector = EDGE == kNoEdge || I % 8 == 0;
+    const GluRows<EDGE> out(h + (size_t)row0 * I + col0, I, 32 * NI, M - row0, I - col0, vector);
+    unsigned mag = 0;
+    auto body = [&](auto keep) __attribute__((always_inline)) {
+        constexpr bool KEEP = decltype(keep)::value;
+        const uint16_t* gu = KEEP ? plan.gu_out + (size_t)row0 * 2 * I + col0 : h;
+        const GluRows<EDGE> gate(gu, 2 * I, 32 * NI, M - row0, I - col0, vector), up(gu + (KEEP ? I : 0), 2 * I, 32 * NI, M - row0, I - col0, vector);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii) {
+                const int row = 16 * ii + fr_row;
+#pragma unroll
+                for (int j = 0; j < HJ; ++j) {
+                    const v4f g = acc.get(2 * i + ii, j), u = acc.get(2 * i + ii, HJ + j);
+                    v4f y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = glu_value(g[e], u[e]);
+                    uint8_t* dst = stage + row * kPitch + ((((2 * j + slot0 + row) % kSlots) << 4) | half_off);
+                    *reinterpret_cast<v2u*>(dst) = bf16_of(y);
+                    if constexpr (KEEP) {
+                        *reinterpret_cast<v2u*>(dst + kPlane) = bf16_of(g);
+                        *reinterpret_cast<v2u*>(dst + 2 * kPlane) = bf16_of(u);
+                    }
+                }
+            }
+            v4u piece[KEEP ? 3 : 1][kPieces];
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
+#pragma unroll
+                for (int n = 0; n < (KEEP ? 3 : 1); ++n) piece[n][k] = *reinterpret_cast<const v4u*>(stage + n * kPlane + r * kPitch + (((sl + r) % kSlots) << 4));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            unsigned ignored = 0;
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                const int p = lane + k * kWave, r = 32 * i + p / kSlots, c = 8 * (p % kSlots);
+                out.store(r, c, piece[0][k], mag);
+                if constexpr (KEEP) {
+                    gate.store(r, c, piece[1][k], ignored);
+                    up.store(r, c, piece[2][k], ignored);
+                }
+            }
+        }
+    };
+    if (plan.gu_out) body(BoolTag<true>{});
+    else body(BoolTag<false>{});
+    return mag;
+}
+
+// Eight columns of a row: dG, dU and h as BF16
+__device__ inline void glu_gradient8(const v4f (&dh)[2], const v4u& g, const v4u& u, v4u& dg, v4u& du, v4u& h) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        v4f a, b, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned gw = g[2 * half + e / 2], uw = u[2 * half + e / 2];
+            float x, z, w;
+            glu_gradient(dh[half][e], e & 1 ? bf16_hi(gw) : bf16_lo(gw), e & 1 ? bf16_hi(uw) : bf16_lo(uw), x, z, w);
+            a[e] = x, b[e] = z, y[e] = w;
+        }
+        const v2u wa = bf16_of(a), wb = bf16_of(b), wy = bf16_of(y);
+        dg[2 * half] = wa[0], dg[2 * half + 1] = wa[1];
+        du[2 * half] = wb[0], du[2 * half + 1] = wb[1];
+        h[2 * half] = wy[0], h[2 * half + 1] = wy[1];
+    }
+}
+
+// Epilogue of the backward tile: dh through LDS in binary32, 32 rows at a time, so that a lane has eight consecutive columns of a row, as GU is loaded and dGU stored.
+template <int NI, int MI, int MJ, int EDGE, class Acc>
+__device__ __attribute__((always_inline)) inline unsigned glu_backward_out(const Acc& acc, uint8_t* stage, uint16_t* dgu, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
+    constexpr int kSlots = 2 * MJ, kPitch = 32 * kSlots, kPieces = 32 * kSlots / kWave, kAtOnce = kPieces < 4 ? kPieces : 4;
+    static_assert(kPieces >= 1 && kWave % kSlots == 0 && kPieces % kAtOnce == 0, "every lane moves whole pieces");
+    const int fr_row = lane & 15, fr_q = lane >> 4, piece0 = fr_q >> 1, unit_off = (fr_q & 1) * (16 * kSlots);
+    const bool vector = EDGE == kNoEdge || I % 8 == 0;
+    const size_t at = (size_t)row0 * 2 * I + col0;
+    const GluRows<EDGE> gate(plan.gu + at, 2 * I, 32 * NI, M - row0, I - col0, vector), up(plan.gu + at + I, 2 * I, 32 * NI, M - row0, I - col0, vector);
+    const GluRows<EDGE> dgate(dgu + at, 2 * I, 32 * NI, M - row0, I - col0, vector), dup(dgu + at + I, 2 * I, 32 * NI, M - row0, I - col0, vector);
+    const GluRows<EDGE> h(plan.h_out ? plan.h_out + (size_t)row0 * I + col0 : dgu, I, 32 * NI, M - row0, I - col0, vector);
+    unsigned mag = 0, ignored = 0;
+    auto row_of = [&](int i, int k) -> int { return 32 * i + (lane + k * kWave) / kSlots; };
+    auto col_of = [&](int k) -> int { return 8 * ((lane + k * kWave) % kSlots); };
+    auto staged = [&](int k, v4f (&dh)[2]) __attribute__((always_inline)) {
+        const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
+        const uint8_t* src = stage + r * kPitch + (((sl + r) % kSlots) << 4);
+        dh[0] = *reinterpret_cast<const v4f*>(src);
+        dh[1] = *reinterpret_cast<const v4f*>(src + 16 * kSlots);
+    };
+    auto finish = [&](int i, int k, const v4f (&dh)[2], const v4u& g, const v4u& u) __attribute__((always_inline)) {
+        v4u dg, du, y;
+        glu_gradient8(dh, g, u, dg, du, y);
+        dgate.store(row_of(i, k), col_of(k), dg, mag);
+        dup.store(row_of(i, k), col_of(k), du, mag);
+        if (plan.h_out) h.store(row_of(i, k), col_of(k), y, ignored);
+    };
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        v4u g[kPieces], u[kPieces];                // requested first: their way from memory hides behind the staging
+        if (vector) {
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                g[k] = gate.load(row_of(i, k), col_of(k));
+                u[k] = up.load(row_of(i, k), col_of(k));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ii = 0; ii < 2; ++ii) {
+            const int row = 16 * ii + fr_row;
+#pragma unroll
+            for (int j = 0; j < MJ; ++j) *reinterpret_cast<v4f*>(stage + row * kPitch + unit_off + (((2 * j + piece0 + row) % kSlots) << 4)) = acc.get(2 * i + ii, j);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (vector) {
+#pragma unroll
+            for (int k0 = 0; k0 < kPieces; k0 += kAtOnce) {
+                v4f dh[kAtOnce][2];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) staged(k0 + k, dh[k]);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) finish(i, k0 + k, dh[k], g[k0 + k], u[k0 + k]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            if constexpr (EDGE != kNoEdge) {
+#pragma unroll 1
+                for (int k = 0; k < kPieces; ++k) {
+                    v4f dh[2];
+                    staged(k, dh);
+                    finish(i, k, dh, gate.load(row_of(i, k), col_of(k)), up.load(row_of(i, k), col_of(k)));
+                }
+            }
+        }
+    }
+    return mag;
+}
+
+template <int DIR, class Base, bool LOOSE = false>
+struct GluTuning : Base {
+    static constexpr bool kBlockScales = true;
+    static constexpr int kGlu = DIR;
+    static constexpr bool kLooseRows = LOOSE;
+    typedef GluPlan Plan;
+    template <int NI, int MI, int MJ, int EDGE, class Acc>
+    static __device__ __attribute__((always_inline)) unsigned write_out(const Acc& acc, uint8_t* stage, uint16_t* c, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
+        if constexpr (DIR == kGluForward) return glu_forward_out<NI, MI, MJ, EDGE>(acc, stage, c, plan, row0, M, col0, I, lane);
+        else return glu_backward_out<NI, MI, MJ, EDGE>(acc, stage, c, plan, row0, M, col0, I, lane);
+    }
+};
+
+// M x I x T: rows, pairs (forward) or columns (backward), contraction
+struct GluOperands {
+    const uint8_t *A, *sA, *B, *sB;
+    int64_t M, I, T;
+    uint16_t* c;                                // forward: h, backward: dGU
+    GluPlan plan;
+    unsigned* amax;
+};
+
+// What a contraction takes: the kernel for few rows, else the tile.  loose: see GemmTuning::kLooseRows.
+struct GluChoice {
+    bool few;
+    TilePlan tile;
+    bool loose;
+};
+
+template <int FA, int FB, int DIR, int NI, int NJ, int EDGE>
+static void launch_glu_tile(const GluOperands& p, bool loose, hipStream_t stream, int num_cus) {
+    constexpr int kCols = DIR == kGluForward ? 32 * NJ : 64 * NJ;             // of h
+    const int tiles_r = (int)((p.M + 64 * NI - 1) / (64 * NI)), tiles_c = (int)((p.I + kCols - 1) / kCols);
+    GluPlan plan = p.plan;
+    plan.n_whole = tiles_r * tiles_c;
+    const int grid = (plan.n_whole + kXcds - 1) / kXcds * kXcds, slots = resident_slots(num_cus, NI, NJ);
+    const int touch = NI == 2 && NJ == 2 ? touch_ahead_pair() : touch_ahead(), band = band_rows();
+    const int share_b = band < tiles_r ? band : tiles_r, share_a = 4 < tiles_c ? 4 : tiles_c;
+    const int next_stride = EDGE == kNoEdge ? successor_stride(NI, NJ, plan.n_whole, slots) : 0;
+    auto launch = [&](auto tuning, int threads = kGemmThreads) {
+        hipLaunchKernelGGL((gemm_tile_kernel<FA, FB, NI, NJ, EDGE != kNoEdge, decltype(tuning), false, false, kWholeTiles, EDGE>), dim3(grid), dim3(threads), 0, stream, p.A, p.B, p.c, (int)p.I, (int)p.T,
+                           reinterpret_cast<const float*>(p.sA), reinterpret_cast<const float*>(p.sB), p.amax, tiles_r, tiles_c, touch, band, next_stride, (int)p.T, (int)p.T, BK, BK, share_a, share_b,
+                           plan, (int)p.M, 0);
+    };
+    if constexpr (NI == 2 && NJ == 2 && EDGE != kEdgeUnaligned) {
+        if (deep_stages(plan.n_whole, slots)) {
+            // (eight waves have a register for every block of 16 rows anyhow, and take loose rows as they are)
+            if (deep_takes_eight_waves((p.T + BK - 1) / BK, false)) launch(GluTuning<DIR, GemmDeepWideTuning, DIR == kGluForward>{}, 2 * kGemmThreads);
+            else if (DIR == kGluForward && loose) launch(GluTuning<DIR, GemmDeepTuning, DIR == kGluForward>{});
+            else launch(GluTuning<DIR, GemmDeepTuning>{});
+            return;
+        }
+    }
+    if constexpr (DIR == kGluForward && NI == 2 && NJ == 2) {
+        if (loose) { launch(GluTuning<DIR, GemmTuning, true>{}); return; }
+    }
+    launch(GluTuning<DIR, GemmTuning>{});
+}
+
+// ---- Few rows: see gemm_blocks_few_kernel, whose waves, slots and sums these are.  Forward: a workgroup has 16 pairs, block 0 of its columns their gate rows and block 1 their up rows.
+constexpr int kGluWaves = 4, kGluSlots = 4;
+template <int FA, int FB, int DIR, int RB, int CB, bool ALIGNED>
+__global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB,
+                                                                       uint16_t* __restrict__ C, const GluPlan plan, int M, int I, int T, unsigned* __restrict__ amax_bits) {
+    static_assert(DIR == kGluBackward || CB == 2, "gates and ups");
+    constexpr bool PAIRS = DIR == kGluForward;
+    constexpr int kRows = 16 * (RB + CB), kSlot = kRows * BK, kLoads = kRows / 8, kOutOfRange = 0x7FFFFF00, kGroups = PAIRS ? 2 : 1, kOfGroup = CB / kGroups;
+    // one LDS object per slot, which the compiler tells apart (see the tile kernel)
+    __shared__ __attribute__((aligned(1024))) uint8_t s_0[kGluWaves * kSlot];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_1[kGluWaves * kSlot];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_2[kGluWaves * kSlot];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_3[kGluWaves * kSlot];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r0 = (int)blockIdx.y * (16 * RB), c0 = (int)blockIdx.x * (16 * kOfGroup), steps = (T + BK - 1) / BK, mine = (steps - wave + kGluWaves - 1) / kGluWaves;      // steps wave, wave + 4, ...
+    const int rows_a = M - r0 < 16 * RB ? M - r0 : 16 * RB, rows_b = I - c0 < 16 * kOfGroup ? I - c0 : 16 * kOfGroup;      // of a group
+    const uint8_t *const a0 = A + (int64_t)r0 * T, *const b0 = B + (int64_t)c0 * T;
+    const int64_t group_bytes = (int64_t)I * T;
+    const __amdgpu_buffer_rsrc_t rsA = make_rsrc(a0, (unsigned)((int64_t)rows_a * T)), rsG = make_rsrc(b0, (unsigned)((int64_t)rows_b * T)),
+                                 rsU = PAIRS ? make_rsrc(b0 + group_bytes, (unsigned)((int64_t)rows_b * T)) : rsG;
+    const int rows_of_b = PAIRS ? 2 * I : I, pitchA = (M + 127) & ~127, pitchB = (rows_of_b + 127) & ~127;
+    const __amdgpu_buffer_rsrc_t rsSA = make_rsrc(sA, (unsigned)(steps * pitchA)), rsSB = make_rsrc(sB, (unsigned)(steps * pitchB));
+    int code_a[RB], code_b[CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i) code_a[i] = (int)block_scale_offset(r0 + 16 * i + (lane & 15), 0, M);
+#pragma unroll
+    for (int j = 0; j < CB; ++j) code_b[j] = (int)block_scale_offset((PAIRS && j >= kOfGroup ? I : 0) + c0 + 16 * (j % kOfGroup) + (lane & 15), 0, rows_of_b);
+    struct Codes { int a[RB], b[CB]; };
+    struct Chunks { v4u c[ALIGNED ? 1 : kLoads]; };
+    Codes codes[kGluSlots];
+    Chunks chunks[kGluSlots];
+    const int ld_row = lane >> 3;
+    auto request = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
+        const int step = wave + n * kGluWaves;
+        const bool there = n < mine;
+#pragma unroll
+        for (int i = 0; i < RB; ++i) e.a[i] = (int)(unsigned char)__builtin_amdgcn_raw_buffer_load_b8(rsSA, code_a[i], there ? step * pitchA : kOutOfRange, 0);
+#pragma unroll
+        for (int j = 0; j < CB; ++j) e.b[j] = (int)(unsigned char)__builtin_amdgcn_raw_buffer_load_b8(rsSB, code_b[j], there ? step * pitchB : kOutOfRange, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<kLoads>([&](auto piece) {
+            constexpr int p = decltype(piece)::value;
+            constexpr bool of_a = p < 2 * RB, of_up = PAIRS && p >= 2 * RB + 2 * kOfGroup;
+            constexpr int row0 = 8 * (of_a ? p : (p - 2 * RB) % (2 * kOfGroup));
+            const int row = row0 + ld_row, k = step * BK + (((lane & 7) ^ row_swizzle(row & 15)) << 4);
+            if constexpr (ALIGNED) {
+                // (T % 16 == 0: a chunk exists or not; rows behind the operand lie outside the buffer)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(of_a ? rsA : of_up ? rsU : rsG, (lds_void*)(slot + wave * kSlot + p * 8 * BK), 16, there && k < T ? row * T + k : kOutOfRange, 0, 0, 0);
+            } else {
+                held.c[p] = v4u{0, 0, 0, 0};
+                if (there && row < (of_a ? rows_a : rows_b)) {
+                    const uint8_t* src = (of_a ? a0 : of_up ? b0 + group_bytes : b0) + (int64_t)row * T + k;
+                    if (k + 16 <= T) held.c[p] = *reinterpret_cast<const v4u_any*>(src);
+                    else held.c[p] = load16_upto(src, T - k);
+                }
+            }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int fr_row = lane & 15, fr_q = lane >> 4, swz = row_swizzle(fr_row);
+    const int ch0 = ((fr_q * 2) ^ swz) << 4, ch1 = ((fr_q * 2 + 1) ^ swz) << 4;
+    v4f acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    // LDS runs a wave's accesses in order, and the direct loads that follow are requested behind the wait for the reads
+    auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
+        uint8_t* const slab = slot + wave * kSlot;
+        if constexpr (ALIGNED) {
+            wait_vmcnt<(kGluSlots - 1) * (kLoads + RB + CB)>();
+        } else {
+            static_for<kLoads>([&](auto piece) { *reinterpret_cast<v4u*>(slab + decltype(piece)::value * 8 * BK + lane * 16) = held.c[decltype(piece)::value]; });
+        }
+        auto fragment = [&](int first_row) -> v8i {
+            const uint8_t* p = slab + (first_row + fr_row) * BK;
+            const v4i lo = *reinterpret_cast<const v4i*>(p + ch0), hi = *reinterpret_cast<const v4i*>(p + ch1);
+            return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        };
+        v8i a[RB], b[CB];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) a[i] = fragment(16 * i);
+#pragma unroll
+        for (int j = 0; j < CB; ++j) b[j] = fragment(16 * (RB + j));
+        const Codes now = e;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, 0, now.b[j], 0, now.a[i]);
+        __builtin_amdgcn_sched_barrier(0);
+        request(slot, n + kGluSlots, e, held);
+    };
+    request(s_0, 0, codes[0], chunks[0]);
+    request(s_1, 1, codes[1], chunks[1]);
+    request(s_2, 2, codes[2], chunks[2]);
+    request(s_3, 3, codes[3], chunks[3]);
+    int n = 0;
+    for (; n + 3 < mine; n += 4) {
+        multiply(s_0, n, codes[0], chunks[0]);
+        multiply(s_1, n + 1, codes[1], chunks[1]);
+        multiply(s_2, n + 2, codes[2], chunks[2]);
+        multiply(s_3, n + 3, codes[3], chunks[3]);
+    }
+    if (n < mine) multiply(s_0, n, codes[0], chunks[0]);
+    if (n + 1 < mine) multiply(s_1, n + 1, codes[1], chunks[1]);
+    if (n + 2 < mine) multiply(s_2, n + 2, codes[2], chunks[2]);
+    wait_vmcnt<0>();                             // nothing lands in LDS any more
+    __syncthreads();
+    v4f* const s_sum = reinterpret_cast<v4f*>(s_0);                          // [wave][block][lane]
+    static_assert(RB * CB * kWave * sizeof(v4f) <= (size_t)kSlot, "the sums of a wave fit its slot");
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j) s_sum[(wave * (RB * CB) + i * CB + j) * kWave + lane] = acc[i][j];
+    __syncthreads();
+    auto sum_of = [&](int block) -> v4f {
+        v4f y = s_sum[block * kWave + lane];
+#pragma unroll
+        for (int w = 1; w < kGluWaves; ++w) y += s_sum[(w * (RB * CB) + block) * kWave + lane];
+        return y;
+    };
+    unsigned mag = 0;
+    // a lane's four columns of a row: whole where widths are multiples of 4, else element by element
+    auto store = [&](uint16_t* dst, const v4f& y, int left, bool counts) __attribute__((always_inline)) {
+        const v2u out = bf16_of(y);
+        if (I % 4 == 0) {
+            if (counts) mag = pk_max_mag(pk_max_mag(mag, out[0]), out[1]);
+            *reinterpret_cast<v2u*>(dst) = out;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) {
+                    const unsigned bits = e & 1 ? out[e >> 1] >> 16 : out[e >> 1] & 0xFFFFu;
+                    if (counts) mag = pk_max_mag(mag, bits);
+                    dst[e] = (uint16_t)bits;
+                }
+        }
+    };
+    // a wave finishes every fourth block (of pairs)
+    for (int block = wave; block < RB * kOfGroup; block += kGluWaves) {
+        const int i = block / kOfGroup, j = block % kOfGroup, r = r0 + 16 * i + (lane & 15), c = c0 + 16 * j + (lane >> 4) * 4, left = I - c;
+        const v4f sum = sum_of(i * CB + j);
+        v4f other = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (PAIRS) other = sum_of(i * CB + kOfGroup + j);
+        if (r >= M || left <= 0) continue;
+        const int64_t at = (int64_t)r * I + c, at2 = (int64_t)r * 2 * I + c;
+        if constexpr (PAIRS) {
+            v4f y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = glu_value(sum[e], other[e]);
+            store(C + at, y, left, true);
+            if (plan.gu_out) {
+                store(plan.gu_out + at2, sum, left, false);
+                store(plan.gu_out + at2 + I, other, left, false);
+            }
+        } else {
+            float g[4], u[4];
+            if (I % 4 == 0) {
+                const v2u gw = *reinterpret_cast<const v2u*>(plan.gu + at2), uw = *reinterpret_cast<const v2u*>(plan.gu + at2 + I);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g[e] = e & 1 ? bf16_hi(gw[e >> 1]) : bf16_lo(gw[e >> 1]), u[e] = e & 1 ? bf16_hi(uw[e >> 1]) : bf16_lo(uw[e >> 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g[e] = e < left ? bf16_lo(plan.gu[at2 + e]) : 0.0f, u[e] = e < left ? bf16_lo(plan.gu[at2 + I + e]) : 0.0f;
+            }
+            v4f dg, du, h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x, z, w;
+                glu_gradient(sum[e], g[e], u[e], x, z, w);
+                dg[e] = x, du[e] = z, h[e] = w;
+            }
+            store(C + at2, dg, left, true);
+            store(C + at2 + I, du, left, true);
+            if (plan.h_out) store(plan.h_out + at, h, left, false);
+        }
+    }
+    if (amax_bits) {
+        mag = wave_max_u32((mag & 0xFFFFu) > (mag >> 16) ? mag & 0xFFFFu : mag >> 16);
+        const unsigned bits = amax_bits_from_bf16_mag(mag);
+        if (lane == 0 && bits > __hip_atomic_load(amax_bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(amax_bits, bits);
+    }
+}
+
+template <int FA, int FB, int DIR, int RB, int CB>
+static void launch_glu_few(const GluOperands& p, hipStream_t stream) {
+    constexpr int kCols = DIR == kGluForward ? 8 * CB : 16 * CB;
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.I + kCols - 1) / kCols), (unsigned)((p.M + 16 * RB - 1) / (16 * RB))), dim3(kGluWaves * kWave), 0, stream, p.A, p.sA, p.B, p.sB, p.c, p.plan, (int)p.M, (int)p.I,
+                           (int)p.T, p.amax);
+    };
+    if (p.T % 16 == 0) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, true>);
+    else if constexpr (CB == 1 || DIR == kGluForward) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, false>);
+}
+
+// Launches the kernel of the choice; gemm_glu_*.hip instantiate it for a pair of formats and a direction each.
+template <int FA, int FB, int DIR>
+void launch_glu(const GluOperands& p, const GluChoice& choice, hipStream_t stream, int num_cus) {
+    if (choice.few) {
+        if constexpr (DIR == kGluForward) {
+            p.M <= 16 ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream) : launch_glu_few<FA, FB, DIR, 2, 2>(p, stream);
+        } else {
+            // (as in the plain contraction)
+            const bool two = p.T % 16 == 0 && (p.I + 31) / 32 >= num_cus / 2;
+            if (p.M <= 16) two ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream) : launch_glu_few<FA, FB, DIR, 1, 1>(p, stream);
+            else two ? launch_glu_few<FA, FB, DIR, 2, 2>(p, stream) : launch_glu_few<FA, FB, DIR, 2, 1>(p, stream);
+        }
+        return;
+    }
+#define LLMQ_GLU_CASE(I, J, KIND)                                                        \
+    case KIND * 64 + I * 8 + J:                                                          \
+        launch_glu_tile<FA, FB, DIR, I, J, KIND>(p, choice.loose, stream, num_cus);      \
+        return;
+    switch (choice.tile.edge * 64 + choice.tile.ni * 8 + choice.tile.nj) {
+        LLMQ_GLU_CASE(4, 4, kNoEdge) LLMQ_GLU_CASE(4, 2, kNoEdge) LLMQ_GLU_CASE(3, 4, kNoEdge) LLMQ_GLU_CASE(2, 4, kNoEdge) LLMQ_GLU_CASE(2, 2, kNoEdge)
+        LLMQ_GLU_CASE(4, 4, kEdge) LLMQ_GLU_CASE(4, 2, kEdge) LLMQ_GLU_CASE(2, 4, kEdge) LLMQ_GLU_CASE(2, 2, kEdge)
+        LLMQ_GLU_CASE(2, 2, kEdgeUnaligned)
+        default: break;
+    }
+#undef LLMQ_GLU_CASE
+}
+extern template void launch_glu<0, 0, kGluForward>(const GluOperands&, const GluChoice&, hipStream_t, int);
+extern template void launch_glu<1, 0, kGluForward>(const GluOperands&, const GluChoice&, hipStream_t, int);
+extern template void launch_glu<0, 0, kGluBackward>(const GluOperands&, const GluChoice&, hipStream_t, int);
+extern template void launch_glu<1, 0, kGluBackward>(const GluOperands&, const GluChoice&, hipStream_t, int);
+
+}  // namespace llmq

@@ -1,0 +1,92 @@
+// Choice of kernel and entry points of the contractions joined with a SwiGLU.
+#include "gemm_glu.h"
+
+#include "api_checks.h"
+
+namespace llmq {
+
+// M x I x T as in GluOperands.  LLMQ_GLU_FEW=0 / 1 (tests): the kernel for few rows never, or for up to 4096 rows always; LLMQ_GLU_TILE=IxJ: that tile where it is built for the shape.
+template <int DIR>
+static GluChoice choose_glu(int64_t M, int64_t I, int64_t T, int num_cus) {
+    GluChoice choice{false, {0, 0, kNoEdge}, DIR == kGluForward && I % 32 != 0};
+    const char* few = tuning_env("LLMQ_GLU_FEW");
+    choice.few = few ? atoi(few) != 0 && M <= 4096 : M <= 32;
+    if (choice.few) return choice;
+    const int64_t cols = DIR == kGluForward ? 2 * I : I, steps = (T + BK - 1) / BK;
+    auto form = [&](int ni, int nj) {
+        const bool whole = M % (64 * ni) == 0 && cols % (64 * nj) == 0 && T % BK == 0 && !choice.loose;
+        return TilePlan{ni, nj, whole ? kNoEdge : T % 16 == 0 ? kEdge : kEdgeUnaligned};
+    };
+    // what is not built: guarded tiles of 192 rows; other sides than 128 for chunks that go through registers; and where up rows do not start at multiples of the rows whose codes share a
+    // register, 64 of a tile of 256 columns and 32 of others, but for 128 x 128
+    auto built = [&](const TilePlan& p) {
+        if (p.ni == 2 && p.nj == 2) return true;
+        return p.edge != kEdgeUnaligned && (p.edge == kNoEdge || p.ni != 3) && (DIR == kGluBackward || I % (p.nj == 4 ? 64 : 32) == 0);
+    };
+    if (const char* e = tuning_env("LLMQ_GLU_TILE")) {
+        if (e[0] >= '2' && e[0] <= '4' && e[1] == 'x' && (e[2] == '2' || e[2] == '4') && !(e[0] == '3' && e[2] == '2')) {
+            const TilePlan p = form(e[0] - '0', e[2] - '0');
+            if (built(p)) { choice.tile = p; return choice; }
+        }
+    }
+    if (((M + 127) / 128) * ((cols + 127) / 128) <= resident_slots(num_cus, 2, 2) / 2) { choice.tile = form(2, 2); return choice; }
+    static const int forms[][2] = {{4, 4}, {3, 4}, {4, 2}, {2, 4}, {2, 2}};
+    double best_us = 0.0;
+    for (const auto& f : forms) {
+        const TilePlan p = form(f[0], f[1]);
+        const int64_t tiles = ((M + 64 * p.ni - 1) / (64 * p.ni)) * ((cols + 64 * p.nj - 1) / (64 * p.nj));
+        if (!built(p) || tiles > kMaxWorkgroups) continue;
+        const double us = tile_us(p, tiles, steps, DIR == kGluBackward, cols % 8 != 0, resident_slots(num_cus, p.ni, p.nj));
+        if (choice.tile.ni == 0 || us < best_us) { choice.tile = p; best_us = us; }
+    }
+    return choice;
+}
+
+}  // namespace llmq
+
+namespace {
+
+// 32-bit offsets from the first row of a tile, of operands, scales and outputs; sixteen bytes in every row of an operand
+int check_glu(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* B, const uint8_t* sB, int fmtB, int64_t M, int64_t I, int64_t T, int64_t rows_of_b, const void* gu, const void* out, const void* other,
+              const float* d_amax) {
+    if (!dim_ok(M) || !dim_ok(I) || !dim_ok(T) || T < 16 || T >= (1ll << 22) || I >= (1ll << 21)) return LLMQ_ERR_SHAPE;
+    const int64_t steps = (T + 127) / 128, rows = M > rows_of_b ? M : rows_of_b;
+    if (steps * ((rows + 127) / 128 * 128) >= 0x7FFFF000ll || M * I >= kMaxElems / 2 || ((M + 127) / 128) * ((I + 63) / 64) > (int64_t)llmq::kMaxWorkgroups) return LLMQ_ERR_SHAPE;
+    if (!fmt_ok(fmtA) || fmtB != LLMQ_E4M3) return LLMQ_ERR_FORMAT;
+    if (!aligned(A, 16) || !aligned(sA, 16) || !aligned(B, 16) || !aligned(sB, 16) || !aligned(gu, 16) || !aligned(out, 16) || !aligned(other, 16) || !aligned(d_amax, 4)) return LLMQ_ERR_ALIGN;
+    return LLMQ_OK;
+}
+
+template <int DIR>
+int run_glu(const llmq::GluOperands& p, int fmtA, void* stream) {
+    const int cus = num_cus();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (p.amax) llmq::launch_gemm_amax_reset(p.amax, s);
+    const llmq::GluChoice choice = llmq::choose_glu<DIR>(p.M, p.I, p.T, cus);
+    if (fmtA == LLMQ_E4M3) llmq::launch_glu<0, 0, DIR>(p, choice, s, cus);
+    else llmq::launch_glu<1, 0, DIR>(p, choice, s, cus);
+    return hipGetLastError() == hipSuccess ? LLMQ_OK : LLMQ_ERR_DEVICE;
+}
+
+}  // namespace
+
+extern "C" {
+
+int llmq_fp8_gemm_blocks_swiglu_fwd(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* W, const uint8_t* sW, int fmtW, int64_t M, int64_t I, int64_t T, void* h_bf16, void* gu_bf16, float* d_amax_h,
+                                    void* stream) {
+    if (!A || !sA || !W || !sW || !h_bf16) return LLMQ_ERR_NULL;
+    const int st = check_glu(A, sA, fmtA, W, sW, fmtW, M, I, T, 2 * I, gu_bf16, h_bf16, nullptr, d_amax_h);
+    if (st != LLMQ_OK) return st;
+    return run_glu<llmq::kGluForward>({A, sA, W, sW, M, I, T, static_cast<uint16_t*>(h_bf16), {0, nullptr, static_cast<uint16_t*>(gu_bf16), nullptr}, reinterpret_cast<unsigned*>(d_amax_h)}, fmtA, stream);
+}
+
+int llmq_fp8_gemm_blocks_swiglu_bwd(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* B, const uint8_t* sB, int fmtB, const void* gu_bf16, int64_t M, int64_t I, int64_t T, void* dgu_bf16,
+                                    void* h_bf16, float* d_amax_dgu, void* stream) {
+    if (!A || !sA || !B || !sB || !gu_bf16 || !dgu_bf16) return LLMQ_ERR_NULL;
+    const int st = check_glu(A, sA, fmtA, B, sB, fmtB, M, I, T, I, gu_bf16, dgu_bf16, h_bf16, d_amax_dgu);
+    if (st != LLMQ_OK) return st;
+    return run_glu<llmq::kGluBackward>({A, sA, B, sB, M, I, T, static_cast<uint16_t*>(dgu_bf16), {0, static_cast<const uint16_t*>(gu_bf16), nullptr, static_cast<uint16_t*>(h_bf16)},
+                                        reinterpret_cast<unsigned*>(d_amax_dgu)}, fmtA, stream);
+}
+
+}  // extern "C"

@@ -145,7 +145,15 @@ struct GemmTuning {
     static constexpr bool kIeeeMaximum = true;
     // Operands with a scale for each block of 128 contraction bytes (gemm_blocks.h).
     static constexpr bool kBlockScales = false;
+    // Contractions joined with a SwiGLU (gemm_glu.h): kGluForward pairs the columns of a tile, kGluBackward has another epilogue only.  Their tuning structs provide
+    //   template <...> static __device__ unsigned write_out(...), which returns packed magnitudes of what it stored.
+    static constexpr int kGlu = 0;
+    // kGluForward: the up rows of B do not start at a multiple of 64 rows (tiles of 256 columns) or 32 (others)
+    static constexpr bool kLooseRows = false;
+    // What the launch knows of its tiles
+    typedef SplitPlan Plan;
 };
+constexpr int kGluForward = 1, kGluBackward = 2;
 
 // For problems of at most one 128 x 128 tile per CU.  Alone on its CU, a workgroup of that size with two stages waits for its
 // loads in every K step: a slab is requested one step before it is needed, and a step (16 MFMAs per wave) is shorter than
@@ -390,7 +398,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, uint16_t* __restrict__ C,
     int Cn, int T, const float* __restrict__ d_sA, const float* __restrict__ d_sB,
     unsigned* __restrict__ amax_bits, int tiles_r, int tiles_c, int touch_ahead, int band_rows, int next_stride,
-    int ldA, int ldB, int ks_a, int ks_b, int share_a, int share_b, const SplitPlan plan, int Rn, int accumulate) {
+    int ldA, int ldB, int ks_a, int ks_b, int share_a, int share_b, const typename V::Plan plan, int Rn, int accumulate) {
     static_assert(EDGE == kNoEdge || (MODE == kWholeTiles && ACCUM), "ragged shapes: whole tiles, old values by run-time flag");
     constexpr bool UA = EDGE == kEdgeUnaligned;
     static_assert(!(TA || TB) || (FA != kFmtBf16 && FB != kFmtBf16), "the transposing reads move single bytes");
@@ -497,8 +505,16 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     };
     const __amdgpu_buffer_rsrc_t rsA = TA ? make_rsrc(A + (size_t)tr * BM, (unsigned)((size_t)T * ldA - (size_t)tr * BM))
                                           : make_rsrc(A + (size_t)tr * BM * ldA, bytes_of_rows(Rn - tr * BM, BM, ldA, ksA));
+    // kGluForward: Cn counts pairs.  B has their gate rows, then their up rows; of the BN columns of a tile every second W-th is of up rows, so that a wave's block columns
+    // are the gates of its pairs and then their ups, and what a wave loads are rows of one kind: it has the first of them as its operand.
+    constexpr bool PAIRS = V::kGlu == kGluForward;
+    static_assert(!PAIRS || (!TA && !TB && NJ % 2 == 0 && MODE == kWholeTiles), "pairs of columns: operands in rows, whole tiles of even sides");
+    auto first_row_of_wave = [&](int tile) -> int { return tile * (BN / 2) + (wave >> 1) * RB; };        // of the pairs
+    const int leftB = PAIRS ? Cn - first_row_of_wave(tc) : Cn - tc * BN;
+    // (a wave whose rows all lie beyond the last pair has those of the first: what they make is not stored)
+    const size_t rowB = !PAIRS ? (size_t)tc * BN : leftB > 0 ? (size_t)(wave & 1) * Cn + first_row_of_wave(tc) : 0;
     const __amdgpu_buffer_rsrc_t rsB = TB ? make_rsrc(B + (size_t)tc * BN, (unsigned)((size_t)T * ldB - (size_t)tc * BN))
-                                          : make_rsrc(B + (size_t)tc * BN * ldB, bytes_of_rows(Cn - tc * BN, BN, ldB, ksB));
+                                          : make_rsrc(B + rowB * ldB, PAIRS && leftB <= 0 ? 0u : bytes_of_rows(leftB, PAIRS ? RB : BN, ldB, ksB));
     const int ld_row = lane >> 3;                                   // row inside the group of 8
     auto rows_voff = [&](int m, int ld) {                           // rows 8 m + ld_row of a row-wise operand, `ld` bytes apart
         return ld_row * ld + (((lane & 7) ^ row_swizzle(8 * m + ld_row)) << 4);
@@ -523,7 +539,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         tail_voffA[m] = beyond ? kOutOfRange : ld_voffA[m];
         tail_voffB[m] = beyond ? kOutOfRange : ld_voffB[m];
     }
-    const int ld_soffA = wave * (TA ? RT : RA) * ldA, ld_soffB = wave * (TB ? RT : RB) * ldB;
+    const int ld_soffA = wave * (TA ? RT : RA) * ldA, ld_soffB = PAIRS ? 0 : wave * (TB ? RT : RB) * ldB;
     // The direct-to-LDS loads of one slab pair: pieces 0 .. LA - 1 fill the wave's share of the A slab, the
     // next LB that of the B slab.  step: K step of the slab, or a negative value for "no slab"
     // (nothing is fetched).
@@ -565,9 +581,9 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     };
     // kEdgeUnaligned: the same pieces through registers.  (A 4 x 4 tile has too few of them: the operand pointers are kept in scratch memory and read back where the last slab is rewritten.)
     const uint8_t* uaA = TA ? A + (size_t)tr * BM : A + (size_t)tr * BM * ldA;
-    const uint8_t* uaB = TB ? B + (size_t)tc * BN : B + (size_t)tc * BN * ldB;
+    const uint8_t* uaB = TB ? B + (size_t)tc * BN : B + rowB * ldB;
     auto last16 = [&](int64_t bytes) -> unsigned { return bytes - 16 < 0x7FFFFFF0ll ? (unsigned)(bytes - 16) : 0x7FFFFFF0u; };
-    const unsigned endA = UA ? last16((int64_t)Rn * T - (uaA - A)) : 0, endB = UA ? last16((int64_t)Cn * T - (uaB - B)) : 0;
+    const unsigned endA = UA ? last16((int64_t)Rn * T - (uaA - A)) : 0, endB = UA ? last16((int64_t)(PAIRS ? 2 * Cn : Cn) * T - (uaB - B)) : 0;
     v4u staged[UA ? kLoadsPerStep : 1];
     auto fetch = [&](int step, auto piece) {                        // any step: offsets are cut to the operand's end
         constexpr int p = decltype(piece)::value;
@@ -610,7 +626,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
 #pragma unroll 1
         for (int j = 0; j < LB; ++j)
             *reinterpret_cast<v4u*>(slabB + wave * RB * BK + j * 8 * BK + lane * 16) =
-                fix_piece(SB{}, TB, B, (int64_t)tc * BN, Cn, ldB, ksB, wave * RB, j, IntTag<SB::kPeriod>{});
+                fix_piece(SB{}, TB, B, (int64_t)rowB, PAIRS ? 2 * Cn : Cn, ldB, ksB, PAIRS ? 0 : wave * RB, j, IntTag<SB::kPeriod>{});
     };
     // The wave tile as 16 x 16 blocks: MI x MJ of them, handled in halves of HI block rows / HJ block columns.
     constexpr int MI = 2 * NI, MJ = 4 * NJ / WC, HI = MI / 2, HJ = MJ / 2;
@@ -678,15 +694,28 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     // that a lane's row of four neighbouring blocks of 16 rows is one register.  A side of 192 starts a wave's rows at a multiple of 32: there two blocks
     // share a register.  A step's registers are requested two steps ahead, into those of the step that has just ended, as its newest loads.
     static_assert(!BS || (NI <= 4 && NJ <= 4 && MODE == kWholeTiles && FA != kFmtBf16), "sides of 320 have no registers left for scales");
-    constexpr int PA = NI == 3 ? 2 : 4, PB = NJ == 3 ? 2 : 4, WA = (MI + PA - 1) / PA, WB = (MJ + PB - 1) / PB;
-    constexpr int kScaleLoads = BS ? (NI == 3 ? WA : 1) + (NJ == 3 ? WB : 1) : 0;
+    constexpr int PA = NI == 3 ? 2 : 4, PB = PAIRS ? (MJ == 2 || V::kLooseRows ? 1 : NJ) : NJ == 3 ? 2 : 4, WA = (MI + PA - 1) / PA, WB = (MJ + PB - 1) / PB;
+    constexpr int kScaleLoads = BS ? (NI == 3 ? WA : 1) + (NJ == 3 || PAIRS ? WB : 1) : 0;
     typedef std::conditional_t<BS, BlockScales<WA, WB, PA, PB>, NoScales> Scales;
     Scales scales[2];
-    const int pitchA = (Rn + 127) & ~127, pitchB = (Cn + 127) & ~127;
+    const int pitchA = (Rn + 127) & ~127, pitchB = ((PAIRS ? 2 * Cn : Cn) + 127) & ~127;
     const __amdgpu_buffer_rsrc_t rsSA = BS ? make_rsrc(d_sA, (unsigned)(((T + BK - 1) / BK) * pitchA)) : rsA, rsSB = BS ? make_rsrc(d_sB, (unsigned)(((T + BK - 1) / BK) * pitchB)) : rsB;
     // first block of 16 rows of the wave (with eight waves of the two that share a register)
     const int blockA = tr * (BM / 16) + wr * MI, blockB = tc * (BN / 16) + (MJ == 2 ? (wc & ~1) * MJ : wc * MJ);
     const int sc_voff = 8 * (lane & 15);
+    // kGluForward: registers for the wave's gate blocks and then for its up blocks, each from the aligned word that holds its first block's code.  Blocks of tiles of 256 columns are whole words; those of
+    // others are shifted to the low end where they are used.  A gate block is one of 16 rows always; of loose rows an up block may lie over two of those, so every lane finds its row's code.
+    const int gate_block = tc * (BN / 32) + wc * (MJ / 2);
+    constexpr bool SHIFTED = PAIRS && PB < 4;
+    int pair_voff[PAIRS ? WB : 1], pair_shift[PAIRS ? WB : 1];
+    if constexpr (PAIRS) {
+#pragma unroll
+        for (int p = 0; p < WB; ++p) {
+            const int row = 16 * (gate_block + PB * (p % (WB / 2))) + (p >= WB / 2 ? Cn : 0) + (lane & 15);
+            pair_voff[p] = (row & ~127) + 8 * (row & 15) + ((row >> 4) & 4);
+            pair_shift[p] = 8 * ((row >> 4) & 3);
+        }
+    }
     // offset of a block's codes in a K step (a tile may reach over the last group of 128 rows: what is read there, codes of another step or zeros, goes to rows that do not exist)
     auto code_offset = [](int block) { return (block >> 3) * 128 + (block & 7); };
     auto request_operand = [&](auto three, auto& words, __amdgpu_buffer_rsrc_t rs, int block, unsigned at) __attribute__((always_inline)) {
@@ -704,7 +733,12 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     auto request_scales = [&](auto& sc, int step) __attribute__((always_inline)) {
         if constexpr (BS) {
             request_operand(BoolTag<NI == 3>{}, sc.a, rsSA, blockA, step < nk ? step * pitchA : kOutOfRange);
-            request_operand(BoolTag<NJ == 3>{}, sc.b, rsSB, blockB, step < nk ? step * pitchB : kOutOfRange);
+            if constexpr (PAIRS) {
+#pragma unroll
+                for (int p = 0; p < WB; ++p) sc.b[p] = (int)__builtin_amdgcn_raw_buffer_load_b32(rsSB, pair_voff[p], step < nk ? step * pitchB : kOutOfRange, 0);
+            } else {
+                request_operand(BoolTag<NJ == 3>{}, sc.b, rsSB, blockB, step < nk ? step * pitchB : kOutOfRange);
+            }
         }
     };
 
@@ -725,10 +759,10 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     // (T-major operand: the slab is 128 memory rows of kLines lines each, shared out the same way.)
     constexpr int kLinesOfA = TA ? BK * SA::kLines : BM, kLinesOfB = TB ? BK * SB::kLines : BN;
     const int per_wave_a = (kLinesOfA + share_a * 4 - 1) / (share_a * 4), per_wave_b = (kLinesOfB + share_b * 4 - 1) / (share_b * 4);
-    const int touch_lineA = ((tc % share_a) * 4 + wave) * per_wave_a + lane, touch_lineB = ((tr % share_b) * 4 + wave) * per_wave_b + lane;
+    const int touch_lineA = ((tc % share_a) * 4 + wave) * per_wave_a + lane, touch_lineB = PAIRS ? (tr % share_b) * per_wave_b + lane : ((tr % share_b) * 4 + wave) * per_wave_b + lane;
     const int touch_voffA = (lane >= per_wave_a || touch_lineA >= kLinesOfA) ? kOutOfRange
                             : TA ? (touch_lineA / SA::kLines) * ldA + (touch_lineA % SA::kLines) * 128 : touch_lineA * ldA;
-    const int touch_voffB = (lane >= per_wave_b || touch_lineB >= kLinesOfB) ? kOutOfRange
+    const int touch_voffB = (lane >= per_wave_b || touch_lineB >= (PAIRS ? RB : kLinesOfB)) ? kOutOfRange
                             : TB ? (touch_lineB / SB::kLines) * ldB + (touch_lineB % SB::kLines) * 128 : touch_lineB * ldB;
     int touchA[2] = {0, 0}, touchB[2] = {0, 0};   // results are only kept so that the loads stay tracked
     int touch_sink = 0;
@@ -784,7 +818,12 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         auto& aX = *(XH ? &aH : &aL);
         auto& aY = *(XH ? &aL : &aH);
         Scales sc = scales[parity];
-        if constexpr (BS && MJ == 2) {
+        if constexpr (SHIFTED) {
+#pragma unroll
+            for (int p = 0; p < WB; ++p) asm volatile("v_lshrrev_b32 %0, %1, %0" : "+v"(sc.b[p]) : "v"(pair_shift[p]));
+            asm volatile("s_nop 4");
+        }
+        if constexpr (BS && MJ == 2 && !PAIRS) {
             // eight waves: a wave's two block columns are one half of the register (written out with its distance to the MFMAs that read it)
             asm volatile("v_lshrrev_b32 %0, %1, %0\n\ts_nop 4" : "+v"(sc.b[0]) : "s"(16 * (wc & 1)));
         }
@@ -968,7 +1007,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
                 }
             };
             request(BoolTag<TA>{}, IntTag<kNextA>{}, A, ntr * BM, BM / 4, ldA, ksA, next_touch);
-            request(BoolTag<TB>{}, IntTag<kNextB>{}, B, ntc * BN, BN / 4, ldB, ksB, next_touch + kNextA);
+            request(BoolTag<TB>{}, IntTag<kNextB>{}, PAIRS ? B + ((int64_t)(wave & 1) * Cn - (int64_t)wave * RB) * ldB : B, PAIRS ? first_row_of_wave(ntc) : ntc * BN, BN / 4, ldB, ksB, next_touch + kNextA);
         }
     }
 
@@ -1289,7 +1328,9 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         if constexpr (V::kProfile) stamp(4);
     }
     };
-    if constexpr (EDGE != kNoEdge) {
+    if constexpr (V::kGlu != 0) {
+        edge_mag = V::template write_out<NI, MI, MJ, EDGE>(acc, stage_of(wave), C, plan, tr * BM + wr * 32 * NI, Rn, PAIRS ? gate_block * 16 : tc * BN + wc * 16 * MJ, Cn, lane);
+    } else if constexpr (EDGE != kNoEdge) {
         write_out(BoolTag<true>{});
     } else if (one_mul) {
         write_out(BoolTag<false>{});
@@ -1302,7 +1343,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         asm volatile("" ::"v"(next_touch[0]));
     }
     unsigned mag = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)maxabs);   // non-negative: magnitude bits
-    if constexpr (EDGE != kNoEdge) mag = (edge_mag & 0xFFFFu) > (edge_mag >> 16) ? (edge_mag & 0xFFFFu) : (edge_mag >> 16);
+    if constexpr (EDGE != kNoEdge || V::kGlu != 0) mag = (edge_mag & 0xFFFFu) > (edge_mag >> 16) ? (edge_mag & 0xFFFFu) : (edge_mag >> 16);
     if (amax_bits) {
         mag = wave_max_u32(mag);
         if (lane == 0) s_amax[wave] = mag;

@@ -39,7 +39,7 @@ EXPORTS = ["llmq_status_string", "llmq_version", "llmq_amax_workspace_bytes", "l
            "llmq_scale_from_amax", "llmq_swiglu_workspace_bytes", "llmq_swiglu_fwd", "llmq_swiglu_fwd_fp8", "llmq_swiglu_fwd_fp8_slabs",
            "llmq_swiglu_bwd", "llmq_rmsnorm_workspace_bytes", "llmq_rmsnorm_fwd", "llmq_rmsnorm_apply_fp8", "llmq_rmsnorm_apply_fp8_slabs",
            "llmq_rmsnorm_fwd_fp8_blocks", "llmq_rmsnorm_bwd_workspace_bytes", "llmq_rmsnorm_bwd",
-           "llmq_block_scales_bytes", "llmq_quantize_fp8_blocks", "llmq_fp8_gemm_blocks",
+           "llmq_block_scales_bytes", "llmq_quantize_fp8_blocks", "llmq_fp8_gemm_blocks", "llmq_fp8_gemm_blocks_swiglu_fwd", "llmq_fp8_gemm_blocks_swiglu_bwd",
            "llmq_qk_norm_rope_fwd", "llmq_qk_norm_rope_workspace_bytes", "llmq_qk_norm_rope_bwd",
            "llmq_adamw_plan_bytes", "llmq_adamw_plan", "llmq_adamw_hyper", "llmq_adamw_step",
            "llmq_calibrate_mfma", "llmq_calibrate_copy", "llmq_calibrate_gemm_phases_bytes", "llmq_calibrate_gemm_phases"]
@@ -138,6 +138,10 @@ def lib() -> ctypes.CDLL:
     L.llmq_quantize_fp8_blocks.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp, vp, vp]
     L.llmq_fp8_gemm_blocks.restype = i32
     L.llmq_fp8_gemm_blocks.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, i32, vp, vp]
+    L.llmq_fp8_gemm_blocks_swiglu_fwd.restype = i32
+    L.llmq_fp8_gemm_blocks_swiglu_fwd.argtypes = [vp, vp, i32, vp, vp, i32, i64, i64, i64, vp, vp, vp, vp]
+    L.llmq_fp8_gemm_blocks_swiglu_bwd.restype = i32
+    L.llmq_fp8_gemm_blocks_swiglu_bwd.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, vp, vp, vp, vp]
     L.llmq_qk_norm_rope_fwd.restype = i32
     L.llmq_qk_norm_rope_fwd.argtypes = [vp, i64, i64, i32, i32, i32, vp, vp, c.c_float, vp, vp, i32, i32, vp, i64, vp, i64, vp, vp]
     L.llmq_qk_norm_rope_workspace_bytes.restype = sz
@@ -568,6 +572,36 @@ def llmq_fp8_gemm_blocks(A: torch.Tensor, sA: torch.Tensor, fmtA: int, B: torch.
                                       _here(B, torch.uint8, "B"), _here(sB, torch.uint8, "sB", llmq_block_scales_bytes(C, T)), fmtB, R, C, T,
                                       _here(c, torch.bfloat16, "c"), int(bool(accumulate)), _here(d_amax_c, torch.float32, "d_amax_c", 1), _stream()),
            "llmq_fp8_gemm_blocks")
+
+
+def llmq_fp8_gemm_blocks_swiglu_fwd(A: torch.Tensor, sA: torch.Tensor, fmtA: int, W: torch.Tensor, sW: torch.Tensor, fmtW: int, h: torch.Tensor, gu: Optional[torch.Tensor] = None,
+                                    d_amax_h: Optional[torch.Tensor] = None) -> None:
+    status = _fast.fp8_gemm_blocks_swiglu_fwd(A, sA, fmtA, W, sW, fmtW, h, gu, d_amax_h)
+    if status is not None:
+        return _check(status, "llmq_fp8_gemm_blocks_swiglu_fwd") if status else None
+    M, T = _matrix(A, "A")
+    both, T2 = _matrix(W, "W")
+    I = both // 2
+    if T != T2 or both % 2 or tuple(h.shape) != (M, I) or (gu is not None and tuple(gu.shape) != (M, both)):
+        raise ValueError("shape mismatch: A %s, W %s, h %s, gu %s" % (tuple(A.shape), tuple(W.shape), tuple(h.shape), None if gu is None else tuple(gu.shape)))
+    u8, bf16 = torch.uint8, torch.bfloat16
+    _check(lib().llmq_fp8_gemm_blocks_swiglu_fwd(_here(A, u8, "A"), _here(sA, u8, "sA", llmq_block_scales_bytes(M, T)), fmtA, _here(W, u8, "W"), _here(sW, u8, "sW", llmq_block_scales_bytes(both, T)), fmtW,
+                                                 M, I, T, _here(h, bf16, "h"), _here(gu, bf16, "gu"), _here(d_amax_h, torch.float32, "d_amax_h", 1), _stream()), "llmq_fp8_gemm_blocks_swiglu_fwd")
+
+
+def llmq_fp8_gemm_blocks_swiglu_bwd(A: torch.Tensor, sA: torch.Tensor, fmtA: int, B: torch.Tensor, sB: torch.Tensor, fmtB: int, gu: torch.Tensor, dgu: torch.Tensor, h: Optional[torch.Tensor] = None,
+                                    d_amax_dgu: Optional[torch.Tensor] = None) -> None:
+    status = _fast.fp8_gemm_blocks_swiglu_bwd(A, sA, fmtA, B, sB, fmtB, gu, dgu, h, d_amax_dgu)
+    if status is not None:
+        return _check(status, "llmq_fp8_gemm_blocks_swiglu_bwd") if status else None
+    M, T = _matrix(A, "A")
+    I, T2 = _matrix(B, "B")
+    if T != T2 or tuple(gu.shape) != (M, 2 * I) or tuple(dgu.shape) != (M, 2 * I) or (h is not None and tuple(h.shape) != (M, I)):
+        raise ValueError("shape mismatch: A %s, B %s, gu %s, dgu %s, h %s" % (tuple(A.shape), tuple(B.shape), tuple(gu.shape), tuple(dgu.shape), None if h is None else tuple(h.shape)))
+    u8, bf16 = torch.uint8, torch.bfloat16
+    _check(lib().llmq_fp8_gemm_blocks_swiglu_bwd(_here(A, u8, "A"), _here(sA, u8, "sA", llmq_block_scales_bytes(M, T)), fmtA, _here(B, u8, "B"), _here(sB, u8, "sB", llmq_block_scales_bytes(I, T)), fmtB,
+                                                 _here(gu, bf16, "gu"), M, I, T, _here(dgu, bf16, "dgu"), _here(h, bf16, "h"), _here(d_amax_dgu, torch.float32, "d_amax_dgu", 1), _stream()),
+           "llmq_fp8_gemm_blocks_swiglu_bwd")
 
 
 def llmq_rmsnorm_fwd_fp8_blocks(res: torch.Tensor, x: Optional[torch.Tensor], w: torch.Tensor, eps: float, res_out: Optional[torch.Tensor], rstd: torch.Tensor, fmt: int,

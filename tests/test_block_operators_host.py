@@ -49,8 +49,29 @@ def test_norm_backward_refuses():
         assert call(**{name: P + 2}) == -3, name
 
 
+@pytest.mark.parametrize("direction", ["fwd", "bwd"])
+def test_gated_products_refuse(direction):
+    f = dict(A=P, sA=P, fa=0, B=P, sB=P, fb=0, M=4, I=8, T=64, gu=P, out=P, other=P, amax=P)
+
+    def call(**o):
+        a = dict(f, **o)
+        if direction == "fwd":
+            return llmq.lib().llmq_fp8_gemm_blocks_swiglu_fwd(a["A"], a["sA"], a["fa"], a["B"], a["sB"], a["fb"], a["M"], a["I"], a["T"], a["out"], a["gu"], a["amax"], None)
+        return llmq.lib().llmq_fp8_gemm_blocks_swiglu_bwd(a["A"], a["sA"], a["fa"], a["B"], a["sB"], a["fb"], a["gu"], a["M"], a["I"], a["T"], a["out"], a["other"], a["amax"], None)
+
+    for name in ("A", "sA", "B", "sB", "out") + (("gu",) if direction == "bwd" else ()):
+        assert call(**{name: None}) == -1, name
+    for o in (dict(M=0), dict(I=0), dict(T=0), dict(T=15), dict(T=1 << 22), dict(I=1 << 21), dict(M=1 << 31), dict(M=1 << 30, T=1 << 20), dict(M=1 << 30, I=1 << 20), dict(M=1 << 28, I=4096, T=16)):
+        assert call(**o) == -2, o
+    assert call(fa=2) == call(fb=1) == call(fb=-1) == -4
+    for name in ("A", "sA", "B", "sB", "gu", "out") + (("other",) if direction == "bwd" else ()):
+        assert call(**{name: P + 8}) == -3, name
+    assert call(amax=P + 2) == -3
+
+
 def test_tensors_on_the_host_are_refused():
     x, u, f = torch.zeros(4, 128, dtype=torch.bfloat16), torch.zeros(4, 128, dtype=torch.uint8), torch.zeros(4)
-    for call in (lambda: llmq.llmq_rmsnorm_fwd_fp8_blocks(x, None, x[0], 1e-6, None, f, 0, u, u), lambda: llmq.llmq_rmsnorm_bwd(x, None, x, x[0], f, x, None, False, 0, None, None, None)):
+    for call in (lambda: llmq.llmq_fp8_gemm_blocks_swiglu_fwd(u, u, 0, torch.cat((u, u)), u, 0, x[:, :4].contiguous()), lambda: llmq.llmq_fp8_gemm_blocks_swiglu_bwd(u, u, 0, u, u, 0, x[:, :8].contiguous(), x[:, :8].contiguous()),
+                 lambda: llmq.llmq_rmsnorm_fwd_fp8_blocks(x, None, x[0], 1e-6, None, f, 0, u, u), lambda: llmq.llmq_rmsnorm_bwd(x, None, x, x[0], f, x, None, False, 0, None, None, None)):
         with pytest.raises(ValueError, match="must live on the GPU"):
             call()
