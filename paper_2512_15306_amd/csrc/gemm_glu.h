@@ -31,41 +31,54 @@ __device__ inline float bf16_lo(unsigned w) { return __uint_as_float(w << 16); }
 __device__ inline float bf16_hi(unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ inline v2u bf16_of(const v4f& v) { return __builtin_bit_cast(v2u, __builtin_convertvector(v, bf16x4)); }
 
-// A wave's part of a BF16 matrix whose rows are `ld` elements apart, 32 rows of it at a time and eight columns to a lane and piece.
-// EDGE kinds go through a buffer that ends with the last element there is; widths that are no multiples of 8 element by element.
-template <int EDGE>
+// A wave's part of a BF16 matrix, 32 rows of it (i) in pieces of eight columns: the lane's piece k, of SLOTS pieces in a row, is one of a row 64 / SLOTS further down for every k.  It is
+// addressed by a register of the lane and a uniform offset (stores: their sum), through a buffer that ends with the part's last element.  EDGE kinds: pieces beside the matrix get an offset outside the
+// buffer.  Widths that are no multiples of 8: whole pieces at any address where the part lies inside the matrix (1000 x 4001 x 1040 backward 17.6 us, element by element 42.8), elsewhere element by element.
+template <int EDGE, int SLOTS>
 struct GluRows {
-    uint16_t* base;
+    static constexpr int kOut = 0x7FFFFF00, kRowStep = kWave / SLOTS;
+    enum Mode { kPieces, kAnyAddress, kElements };
+    uint16_t* base;                             // of the lane's piece 0
     __amdgpu_buffer_rsrc_t rs;
-    int ld, rows_left, cols_left;
-    bool vector;
-    // first element of the part; rows_left, cols_left of the whole matrix from there on (may be <= 0)
-    __device__ GluRows(const uint16_t* p, int ld_, int tile_rows, int rows_left_, int cols_left_, bool vector_)
-        : base(const_cast<uint16_t*>(p)), ld(ld_), rows_left(rows_left_), cols_left(cols_left_), vector(vector_) {
-        const int here = rows_left < tile_rows ? rows_left : tile_rows;
-        if constexpr (EDGE != kNoEdge) rs = make_rsrc(base, here > 0 && cols_left > 0 ? (unsigned)(((size_t)(here - 1) * ld + cols_left) * 2) : 0u);
+    int pitch, voff, rows_left, cols_left;      // bytes from row to row; of the lane's piece 0
+    Mode mode;
+    // part_rows x 8 SLOTS elements from p on, of which rows x cols exist (may be <= 0); rows are `ld` elements apart
+    __device__ __attribute__((always_inline)) GluRows(const uint16_t* p, int ld, int part_rows, int rows, int cols, bool vector, int lane) {
+        const int here = EDGE == kNoEdge || rows > part_rows ? part_rows : rows, r = lane / SLOTS, c = 8 * (lane % SLOTS);
+        mode = EDGE == kNoEdge || vector ? kPieces : cols >= 8 * SLOTS ? kAnyAddress : kElements;
+        if (EDGE == kNoEdge) cols = 8 * SLOTS;
+        rs = make_rsrc(p, here > 0 && cols > 0 ? (unsigned)(((size_t)(here - 1) * ld + cols) * 2) : 0u);
+        pitch = 2 * ld, rows_left = here - r, cols_left = cols - c;
+        voff = EDGE == kNoEdge || c < cols ? r * pitch + 2 * c : kOut;
+        base = const_cast<uint16_t*>(p) + (int64_t)r * ld + c;
     }
-    static constexpr int kOut = 0x7FFFFF00;
-    __device__ int offset(int r, int c) const { return c < cols_left ? (r * ld + c) * 2 : kOut; }
-    __device__ v4u load(int r, int c) const {
-        if constexpr (EDGE == kNoEdge) return *reinterpret_cast<const v4u*>(base + (size_t)r * ld + c);
-        if (vector) return __builtin_amdgcn_raw_buffer_load_b128(rs, offset(r, c), 0, 0);
+    __device__ bool vector() const { return EDGE == kNoEdge || mode == kPieces; }
+    __device__ int row(int i, int k) const { return (32 * i + k * kRowStep) * pitch; }
+    __device__ bool exists(int i, int k) const { return 32 * i + k * kRowStep < rows_left && cols_left > 0; }
+    __device__ int element(int e) const { return e < cols_left ? voff + 2 * e : kOut; }
+    __device__ v4u_at2* address(int i, int k) const { return reinterpret_cast<v4u_at2*>(reinterpret_cast<uint8_t*>(base) + (int64_t)(32 * i + k * kRowStep) * pitch); }
+    // STREAMED: past what the caches hold
+    template <bool STREAMED = false>
+    __device__ __attribute__((always_inline)) v4u load(int i, int k) const {
+        if (vector()) return __builtin_amdgcn_raw_buffer_load_b128(rs, voff, row(i, k), STREAMED ? 2 : 0);
         v4u v = {0, 0, 0, 0};
+        if (mode == kAnyAddress) {
+            if (exists(i, k)) v = *address(i, k);
+            return v;
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, offset(r, c + 2 * e), 0, 0) |
-                   (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, offset(r, c + 2 * e + 1), 0, 0) << 16;
+        for (int e = 0; e < 8; ++e) v[e >> 1] |= (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, element(e), row(i, k), 0) << (16 * (e & 1));
         return v;
     }
-    // and the magnitudes of what is stored
-    __device__ void store(int r, int c, const v4u& v, unsigned& mag) const {
-        if constexpr (EDGE == kNoEdge) {
-            *reinterpret_cast<v4u*>(base + (size_t)r * ld + c) = v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mag = pk_max_mag(mag, v[e]);
-        } else if (vector) {
-            __builtin_amdgcn_raw_buffer_store_b128(v, rs, offset(r, c), 0, 0);
-            if (r < rows_left && c < cols_left) {
+    // and, of the EDGE kinds, the magnitudes of what is stored
+    __device__ __attribute__((always_inline)) void store(int i, int k, const v4u& v, unsigned& mag) const {
+        if (vector() || mode == kAnyAddress) {
+            const bool there = EDGE != kNoEdge && exists(i, k);
+            // (The row in the lane's offset, not the uniform one: behind a wide buffer store the compiler keeps the next instruction off the stored registers only if the store has no scalar
+            // offset.  With one, a third of the runs of 1777 x 2720 x 1024 had last words of pieces that were the next piece's.)
+            if (vector()) __builtin_amdgcn_raw_buffer_store_b128(v, rs, voff + row(i, k), 0, 0);
+            else if (there) *address(i, k) = v;
+            if (there) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) mag = pk_max_mag(mag, v[e]);
             }
@@ -73,8 +86,8 @@ struct GluRows {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const unsigned short bits = (unsigned short)(e & 1 ? v[e >> 1] >> 16 : v[e >> 1]);
-                __builtin_amdgcn_raw_buffer_store_b16(bits, rs, offset(r, c + e), 0, 0);
-                if (r < rows_left && c + e < cols_left) mag = pk_max_mag(mag, (unsigned)bits);
+                __builtin_amdgcn_raw_buffer_store_b16(bits, rs, element(e), row(i, k), 0);
+                if (32 * i + k * kRowStep < rows_left && e < cols_left) mag = pk_max_mag(mag, (unsigned)bits);
             }
         }
     }
@@ -82,65 +95,71 @@ struct GluRows {
 
 // Epilogue of the forward tile.  A lane holds, of block (i, j), four consecutive pairs of a row: their gates in columns j of the wave tile and their ups in columns MJ / 2 + j.  The wave's
 // results go through its part of LDS 32 rows at a time and leave in rows (gemm_tile.h, the epilogue of the plain contraction, has the layout and its reasons).
-template <int NI, int MI, int MJ, int EDGE, class Acc>
-__device__ __attribute__((always_inline)) inline unsigned glu_forward_out(const Acc& acc, uint8_t* stage, uint16_t* h, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
-    constexpr int HJ = MJ / 2, kSlots = 2 * HJ, kPitch = 16 * kSlots, kPlane = 32 * kPitch, kPieces = 32 * kSlots / kWave;
-    static_assert(kPieces >= 1 && kWave % kSlots == 0, "every lane moves whole pieces");
-    const int fr_row = lane & 15, fr_q = lane >> 4, slot0 = fr_q >> 1, half_off = (fr_q & 1) << 3;
-    const bool vector = EDGE == kNoEdge || I % 8 == 0;
-    const GluRows<EDGE> out(h + (size_t)row0 * I + col0, I, 32 * NI, M - row0, I - col0, vector);
-    unsigned mag = 0;
-    auto body = [&](auto keep) __attribute__((always_inline)) {
-        constexpr bool KEEP = decltype(keep)::value;
-        const uint16_t* gu = KEEP ? plan.gu_out + (size_t)row0 * 2 * I + col0 : h;
-        const GluRows<EDGE> gate(gu, 2 * I, 32 * NI, M - row0, I - col0, vector), up(gu + (KEEP ? I : 0), 2 * I, 32 * NI, M - row0, I - col0, vector);
+template <int NI, int MI, int MJ, int EDGE>
+struct GluForward {
+    template <class Acc>
+    static __device__ __attribute__((always_inline)) unsigned write_out(const Acc& acc, uint8_t* stage, uint16_t* h, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
+        constexpr int HJ = MJ / 2, kSlots = 2 * HJ, kPitch = 16 * kSlots, kPlane = 32 * kPitch, kPieces = 32 * kSlots / kWave;
+        static_assert(kPieces >= 1 && kWave % kSlots == 0, "every lane moves whole pieces");
+        const int fr_row = lane & 15, fr_q = lane >> 4, slot0 = fr_q >> 1, half_off = (fr_q & 1) << 3;
+        const bool vector = EDGE == kNoEdge || I % 8 == 0;
+        typedef GluRows<EDGE, kSlots> Rows;
+        const Rows out(h + (size_t)row0 * I + col0, I, 32 * NI, M - row0, I - col0, vector, lane);
+        unsigned mag = 0;
+        float maxabs = 0.0f;
+        auto body = [&](auto keep) __attribute__((always_inline)) {
+            constexpr bool KEEP = decltype(keep)::value;
+            const uint16_t* gu = KEEP ? plan.gu_out + (size_t)row0 * 2 * I + col0 : h;
+            const Rows gate(gu, 2 * I, 32 * NI, M - row0, I - col0, vector, lane), up(gu + (KEEP ? I : 0), 2 * I, 32 * NI, M - row0, I - col0, vector, lane);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < NI; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int ii = 0; ii < 2; ++ii) {
-                const int row = 16 * ii + fr_row;
+                for (int ii = 0; ii < 2; ++ii) {
+                    const int row = 16 * ii + fr_row;
 #pragma unroll
-                for (int j = 0; j < HJ; ++j) {
-                    const v4f g = acc.get(2 * i + ii, j), u = acc.get(2 * i + ii, HJ + j);
-                    v4f y;
+                    for (int j = 0; j < HJ; ++j) {
+                        const v4f g = acc.get(2 * i + ii, j), u = acc.get(2 * i + ii, HJ + j);
+                        v4f y;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = glu_value(g[e], u[e]);
-                    uint8_t* dst = stage + row * kPitch + ((((2 * j + slot0 + row) % kSlots) << 4) | half_off);
-                    *reinterpret_cast<v2u*>(dst) = bf16_of(y);
+                        for (int e = 0; e < 4; ++e) y[e] = glu_value(g[e], u[e]);
+                        maxabs = __builtin_elementwise_maximum(__builtin_elementwise_maximum(maxabs, __builtin_fabsf(y[0])), __builtin_fabsf(y[1]));
+                        maxabs = __builtin_elementwise_maximum(__builtin_elementwise_maximum(maxabs, __builtin_fabsf(y[2])), __builtin_fabsf(y[3]));
+                        uint8_t* dst = stage + row * kPitch + ((((2 * j + slot0 + row) % kSlots) << 4) | half_off);
+                        *reinterpret_cast<v2u*>(dst) = bf16_of(y);
+                        if constexpr (KEEP) {
+                            *reinterpret_cast<v2u*>(dst + kPlane) = bf16_of(g);
+                            *reinterpret_cast<v2u*>(dst + 2 * kPlane) = bf16_of(u);
+                        }
+                    }
+                }
+                v4u piece[KEEP ? 3 : 1][kPieces];
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
+#pragma unroll
+                    for (int n = 0; n < (KEEP ? 3 : 1); ++n) piece[n][k] = *reinterpret_cast<const v4u*>(stage + n * kPlane + r * kPitch + (((sl + r) % kSlots) << 4));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                unsigned ignored = 0;
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    out.store(i, k, piece[0][k], mag);
                     if constexpr (KEEP) {
-                        *reinterpret_cast<v2u*>(dst + kPlane) = bf16_of(g);
-                        *reinterpret_cast<v2u*>(dst + 2 * kPlane) = bf16_of(u);
+                        gate.store(i, k, piece[1][k], ignored);
+                        up.store(i, k, piece[2][k], ignored);
                     }
                 }
             }
-            v4u piece[KEEP ? 3 : 1][kPieces];
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
-#pragma unroll
-                for (int n = 0; n < (KEEP ? 3 : 1); ++n) piece[n][k] = *reinterpret_cast<const v4u*>(stage + n * kPlane + r * kPitch + (((sl + r) % kSlots) << 4));
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            unsigned ignored = 0;
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                const int p = lane + k * kWave, r = 32 * i + p / kSlots, c = 8 * (p % kSlots);
-                out.store(r, c, piece[0][k], mag);
-                if constexpr (KEEP) {
-                    gate.store(r, c, piece[1][k], ignored);
-                    up.store(r, c, piece[2][k], ignored);
-                }
-            }
-        }
-    };
-    if (plan.gu_out) body(BoolTag<true>{});
-    else body(BoolTag<false>{});
-    return mag;
-}
+        };
+        if (plan.gu_out) body(BoolTag<true>{});
+        else body(BoolTag<false>{});
+        return EDGE == kNoEdge ? (unsigned)__builtin_bit_cast(uint16_t, (__bf16)maxabs) : mag;
+    }
+};
 
-// Eight columns of a row: dG, dU and h as BF16
-__device__ inline void glu_gradient8(const v4f (&dh)[2], const v4u& g, const v4u& u, v4u& dg, v4u& du, v4u& h) {
+// Eight columns of a row: dG, dU and h as BF16, and the largest magnitude of the first two before rounding (rounding is monotonic, NaN stays)
+__device__ inline void glu_gradient8(const v4f (&dh)[2], const v4u& g, const v4u& u, v4u& dg, v4u& du, v4u& h, float& maxabs) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         v4f a, b, y;
@@ -150,6 +169,7 @@ __device__ inline void glu_gradient8(const v4f (&dh)[2], const v4u& g, const v4u
             float x, z, w;
             glu_gradient(dh[half][e], e & 1 ? bf16_hi(gw) : bf16_lo(gw), e & 1 ? bf16_hi(uw) : bf16_lo(uw), x, z, w);
             a[e] = x, b[e] = z, y[e] = w;
+            maxabs = __builtin_elementwise_maximum(__builtin_elementwise_maximum(maxabs, __builtin_fabsf(x)), __builtin_fabsf(z));
         }
         const v2u wa = bf16_of(a), wb = bf16_of(b), wy = bf16_of(y);
         dg[2 * half] = wa[0], dg[2 * half + 1] = wa[1];
@@ -158,87 +178,115 @@ __device__ inline void glu_gradient8(const v4f (&dh)[2], const v4u& g, const v4u
     }
 }
 
-// Epilogue of the backward tile: dh through LDS in binary32, 32 rows at a time, so that a lane has eight consecutive columns of a row, as GU is loaded and dGU stored.
-template <int NI, int MI, int MJ, int EDGE, class Acc>
-__device__ __attribute__((always_inline)) inline unsigned glu_backward_out(const Acc& acc, uint8_t* stage, uint16_t* dgu, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
-    constexpr int kSlots = 2 * MJ, kPitch = 32 * kSlots, kPieces = 32 * kSlots / kWave, kAtOnce = kPieces < 4 ? kPieces : 4;
+// Epilogue of the backward tile: dh through LDS in binary32, 32 rows at a time, so that a lane has eight consecutive columns of a row, as GU is loaded and dGU stored.  GU is requested in parts of four such
+// pieces, AHEAD parts in advance in whole tiles (8192 x 18944 x 3584 with h: 648 us without, 631 with two, 621 with three, 622 with four), for 32 rows at a time in guarded ones.
+// STREAMED: GU past what the caches hold.
+template <int NI, int MI, int MJ, int EDGE, bool STREAMED>
+struct GluBackward {
+    static constexpr int kSlots = 2 * MJ, kPitch = 32 * kSlots, kPieces = 32 * kSlots / kWave, kAtOnce = kPieces < 4 ? kPieces : 4, kParts = kPieces / kAtOnce, kAll = NI * kParts;
+    static constexpr int AHEAD = EDGE != kNoEdge ? 0 : 3 < kAll ? 3 : kAll, kKept = AHEAD ? AHEAD + 1 : kParts;
     static_assert(kPieces >= 1 && kWave % kSlots == 0 && kPieces % kAtOnce == 0, "every lane moves whole pieces");
-    const int fr_row = lane & 15, fr_q = lane >> 4, piece0 = fr_q >> 1, unit_off = (fr_q & 1) * (16 * kSlots);
-    const bool vector = EDGE == kNoEdge || I % 8 == 0;
-    const size_t at = (size_t)row0 * 2 * I + col0;
-    const GluRows<EDGE> gate(plan.gu + at, 2 * I, 32 * NI, M - row0, I - col0, vector), up(plan.gu + at + I, 2 * I, 32 * NI, M - row0, I - col0, vector);
-    const GluRows<EDGE> dgate(dgu + at, 2 * I, 32 * NI, M - row0, I - col0, vector), dup(dgu + at + I, 2 * I, 32 * NI, M - row0, I - col0, vector);
-    const GluRows<EDGE> h(plan.h_out ? plan.h_out + (size_t)row0 * I + col0 : dgu, I, 32 * NI, M - row0, I - col0, vector);
-    unsigned mag = 0, ignored = 0;
-    auto row_of = [&](int i, int k) -> int { return 32 * i + (lane + k * kWave) / kSlots; };
-    auto col_of = [&](int k) -> int { return 8 * ((lane + k * kWave) % kSlots); };
-    auto staged = [&](int k, v4f (&dh)[2]) __attribute__((always_inline)) {
-        const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
-        const uint8_t* src = stage + r * kPitch + (((sl + r) % kSlots) << 4);
-        dh[0] = *reinterpret_cast<const v4f*>(src);
-        dh[1] = *reinterpret_cast<const v4f*>(src + 16 * kSlots);
-    };
-    auto finish = [&](int i, int k, const v4f (&dh)[2], const v4u& g, const v4u& u) __attribute__((always_inline)) {
-        v4u dg, du, y;
-        glu_gradient8(dh, g, u, dg, du, y);
-        dgate.store(row_of(i, k), col_of(k), dg, mag);
-        dup.store(row_of(i, k), col_of(k), du, mag);
-        if (plan.h_out) h.store(row_of(i, k), col_of(k), y, ignored);
-    };
+    struct Kept { v4u g[kAtOnce], u[kAtOnce]; };
+    typedef GluRows<EDGE, kSlots> Rows;
+    static __device__ __attribute__((always_inline)) void request(Kept& into, const Rows& gate, const Rows& up, int part) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        __builtin_amdgcn_sched_barrier(0);
-        v4u g[kPieces], u[kPieces];                // requested first: their way from memory hides behind the staging
-        if (vector) {
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                g[k] = gate.load(row_of(i, k), col_of(k));
-                u[k] = up.load(row_of(i, k), col_of(k));
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int ii = 0; ii < 2; ++ii) {
-            const int row = 16 * ii + fr_row;
-#pragma unroll
-            for (int j = 0; j < MJ; ++j) *reinterpret_cast<v4f*>(stage + row * kPitch + unit_off + (((2 * j + piece0 + row) % kSlots) << 4)) = acc.get(2 * i + ii, j);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (vector) {
-#pragma unroll
-            for (int k0 = 0; k0 < kPieces; k0 += kAtOnce) {
-                v4f dh[kAtOnce][2];
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) staged(k0 + k, dh[k]);
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) finish(i, k0 + k, dh[k], g[k0 + k], u[k0 + k]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            if constexpr (EDGE != kNoEdge) {
-#pragma unroll 1
-                for (int k = 0; k < kPieces; ++k) {
-                    v4f dh[2];
-                    staged(k, dh);
-                    finish(i, k, dh, gate.load(row_of(i, k), col_of(k)), up.load(row_of(i, k), col_of(k)));
-                }
-            }
+        for (int k = 0; k < kAtOnce; ++k) {
+            into.g[k] = gate.template load<STREAMED>(part / kParts, part % kParts * kAtOnce + k);
+            into.u[k] = up.template load<STREAMED>(part / kParts, part % kParts * kAtOnce + k);
         }
     }
-    return mag;
-}
+    template <class Acc>
+    static __device__ __attribute__((always_inline)) unsigned write_out(const Acc& acc, uint8_t* stage, uint16_t* dgu, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
+        const int fr_row = lane & 15, fr_q = lane >> 4, piece0 = fr_q >> 1, unit_off = (fr_q & 1) * (16 * kSlots);
+        const bool by_eight = EDGE == kNoEdge || I % 8 == 0;
+        auto rows_of = [&](const uint16_t* p, int ld) __attribute__((always_inline)) { return Rows(p + (size_t)row0 * ld + col0, ld, 32 * NI, M - row0, I - col0, by_eight, lane); };
+        const Rows gate = rows_of(plan.gu, 2 * I), up = rows_of(plan.gu + I, 2 * I), dgate = rows_of(dgu, 2 * I), dup = rows_of(dgu + I, 2 * I), h = rows_of(plan.h_out ? plan.h_out : dgu, I);
+        unsigned mag = 0, ignored = 0;
+        float maxabs = 0.0f;
+        auto body = [&](auto with_h) __attribute__((always_inline)) {
+            auto staged = [&](int k, v4f (&dh)[2]) __attribute__((always_inline)) {
+                const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
+                const uint8_t* src = stage + r * kPitch + (((sl + r) % kSlots) << 4);
+                dh[0] = *reinterpret_cast<const v4f*>(src);
+                dh[1] = *reinterpret_cast<const v4f*>(src + 16 * kSlots);
+            };
+            auto finish = [&](int i, int k, const v4f (&dh)[2], const v4u& g, const v4u& u) __attribute__((always_inline)) {
+                v4u dg, du, y;
+                glu_gradient8(dh, g, u, dg, du, y, maxabs);
+                dgate.store(i, k, dg, mag);
+                dup.store(i, k, du, mag);
+                if constexpr (decltype(with_h)::value) h.store(i, k, y, ignored);
+            };
+            Kept kept[kKept];
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) request(kept[n], gate, up, n);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (AHEAD == 0) {
+                    if (gate.vector()) {
+#pragma unroll
+                        for (int part = 0; part < kParts; ++part) request(kept[part], gate, up, i * kParts + part);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int ii = 0; ii < 2; ++ii) {
+                    const int row = 16 * ii + fr_row;
+#pragma unroll
+                    for (int j = 0; j < MJ; ++j) *reinterpret_cast<v4f*>(stage + row * kPitch + unit_off + (((2 * j + piece0 + row) % kSlots) << 4)) = acc.get(2 * i + ii, j);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (gate.vector()) {
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part) {
+                        const int n = i * kParts + part, k0 = part * kAtOnce;
+                        if constexpr (AHEAD > 0) {
+                            if (n + AHEAD < kAll) request(kept[(n + AHEAD) % kKept], gate, up, n + AHEAD);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                        v4f dh[kAtOnce][2];
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k) staged(k0 + k, dh[k]);
+#pragma unroll
+                        for (int k = 0; k < kAtOnce; ++k) {
+                            finish(i, k0 + k, dh[k], kept[n % kKept].g[k], kept[n % kKept].u[k]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                } else {
+                    if constexpr (EDGE != kNoEdge) {
+                        // two pieces at a time, whose GU is on its way together
+#pragma unroll 1
+                        for (int k = 0; k < kPieces; k += 2) {
+                            v4u g[2], u[2];
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) g[n] = gate.load(i, k + n), u[n] = up.load(i, k + n);
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) {
+                                v4f dh[2];
+                                staged(k + n, dh);
+                                finish(i, k + n, dh, g[n], u[n]);
+                            }
+                        }
+                    }
+                }
+            }
+        };
+        if (plan.h_out) body(BoolTag<true>{});
+        else body(BoolTag<false>{});
+        return EDGE == kNoEdge ? (unsigned)__builtin_bit_cast(uint16_t, (__bf16)maxabs) : mag;
+    }
+};
 
-template <int DIR, class Base, bool LOOSE = false>
+template <int DIR, class Base, int PAIR_BLOCKS = 1, bool STREAMED = false>
 struct GluTuning : Base {
     static constexpr bool kBlockScales = true;
     static constexpr int kGlu = DIR;
-    static constexpr bool kLooseRows = LOOSE;
+    static constexpr int kPairBlocks = PAIR_BLOCKS;
     typedef GluPlan Plan;
-    template <int NI, int MI, int MJ, int EDGE, class Acc>
-    static __device__ __attribute__((always_inline)) unsigned write_out(const Acc& acc, uint8_t* stage, uint16_t* c, const GluPlan& plan, int row0, int M, int col0, int I, int lane) {
-        if constexpr (DIR == kGluForward) return glu_forward_out<NI, MI, MJ, EDGE>(acc, stage, c, plan, row0, M, col0, I, lane);
-        else return glu_backward_out<NI, MI, MJ, EDGE>(acc, stage, c, plan, row0, M, col0, I, lane);
-    }
+    template <int NI, int MI, int MJ, int EDGE>
+    using Epilogue = std::conditional_t<DIR == kGluForward, GluForward<NI, MI, MJ, EDGE>, GluBackward<NI, MI, MJ, EDGE, STREAMED>>;
 };
 
 // M x I x T: rows, pairs (forward) or columns (backward), contraction
@@ -250,7 +298,7 @@ struct GluOperands {
     unsigned* amax;
 };
 
-// What a contraction takes: the kernel for few rows, else the tile.  loose: see GemmTuning::kLooseRows.
+// What a contraction takes: the kernel for few rows, else the tile.  loose: the up rows do not start at a multiple of 32.
 struct GluChoice {
     bool few;
     TilePlan tile;
@@ -272,36 +320,42 @@ static void launch_glu_tile(const GluOperands& p, bool loose, hipStream_t stream
                            reinterpret_cast<const float*>(p.sA), reinterpret_cast<const float*>(p.sB), p.amax, tiles_r, tiles_c, touch, band, next_stride, (int)p.T, (int)p.T, BK, BK, share_a, share_b,
                            plan, (int)p.M, 0);
     };
+    // blocks of B whose codes share a register (forward): whole tiles of 256 columns start at multiples of 128 pairs, of which an up row is one of 64 too; the wave of eight has one block of either kind
+    constexpr int kShared = EDGE == kNoEdge && NJ == 4 ? 4 : 2;
+    const bool forward_loose = DIR == kGluForward && loose;
     if constexpr (NI == 2 && NJ == 2 && EDGE != kEdgeUnaligned) {
         if (deep_stages(plan.n_whole, slots)) {
-            // (eight waves have a register for every block of 16 rows anyhow, and take loose rows as they are)
-            if (deep_takes_eight_waves((p.T + BK - 1) / BK, false)) launch(GluTuning<DIR, GemmDeepWideTuning, DIR == kGluForward>{}, 2 * kGemmThreads);
-            else if (DIR == kGluForward && loose) launch(GluTuning<DIR, GemmDeepTuning, DIR == kGluForward>{});
-            else launch(GluTuning<DIR, GemmDeepTuning>{});
+            if (deep_takes_eight_waves((p.T + BK - 1) / BK, false)) launch(GluTuning<DIR, GemmDeepWideTuning>{}, 2 * kGemmThreads);
+            else if (forward_loose) launch(GluTuning<DIR, GemmDeepTuning, 1>{});
+            else launch(GluTuning<DIR, GemmDeepTuning, DIR == kGluForward ? kShared : 1>{});
             return;
         }
     }
     if constexpr (DIR == kGluForward && NI == 2 && NJ == 2) {
-        if (loose) { launch(GluTuning<DIR, GemmTuning, true>{}); return; }
+        if (loose) { launch(GluTuning<DIR, GemmTuning, 1>{}); return; }
     }
-    launch(GluTuning<DIR, GemmTuning>{});
+    // (GU of more than the memory-side cache holds beside the operands is read past it: 8192 x 18944 x 3584 648 -> 627 us, of what it does hold 1777 x 2720 x 1024 17.9 -> 19.9)
+    if constexpr (DIR == kGluBackward && NI == 4 && NJ == 4 && EDGE == kNoEdge) {
+        if (4 * p.M * p.I > ((int64_t)128 << 20)) { launch(GluTuning<DIR, GemmTuning, 1, true>{}); return; }
+    }
+    launch(GluTuning<DIR, GemmTuning, DIR == kGluForward ? kShared : 1>{});
 }
 
 // ---- Few rows: see gemm_blocks_few_kernel, whose waves, slots and sums these are.  Forward: a workgroup has 16 pairs, block 0 of its columns their gate rows and block 1 their up rows.
-constexpr int kGluWaves = 4, kGluSlots = 4;
-template <int FA, int FB, int DIR, int RB, int CB, bool ALIGNED>
-__global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB,
+// WAVES share the K steps, SLOTS of which each keeps on their way.
+template <int FA, int FB, int DIR, int RB, int CB, int WAVES, int SLOTS, bool ALIGNED>
+__global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB,
                                                                        uint16_t* __restrict__ C, const GluPlan plan, int M, int I, int T, unsigned* __restrict__ amax_bits) {
     static_assert(DIR == kGluBackward || CB == 2, "gates and ups");
     constexpr bool PAIRS = DIR == kGluForward;
     constexpr int kRows = 16 * (RB + CB), kSlot = kRows * BK, kLoads = kRows / 8, kOutOfRange = 0x7FFFFF00, kGroups = PAIRS ? 2 : 1, kOfGroup = CB / kGroups;
     // one LDS object per slot, which the compiler tells apart (see the tile kernel)
-    __shared__ __attribute__((aligned(1024))) uint8_t s_0[kGluWaves * kSlot];
-    __shared__ __attribute__((aligned(1024))) uint8_t s_1[kGluWaves * kSlot];
-    __shared__ __attribute__((aligned(1024))) uint8_t s_2[kGluWaves * kSlot];
-    __shared__ __attribute__((aligned(1024))) uint8_t s_3[kGluWaves * kSlot];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_0[WAVES * kSlot];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_1[WAVES * kSlot];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_2[SLOTS > 2 ? WAVES * kSlot : 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t s_3[SLOTS > 3 ? WAVES * kSlot : 16];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int r0 = (int)blockIdx.y * (16 * RB), c0 = (int)blockIdx.x * (16 * kOfGroup), steps = (T + BK - 1) / BK, mine = (steps - wave + kGluWaves - 1) / kGluWaves;      // steps wave, wave + 4, ...
+    const int r0 = (int)blockIdx.y * (16 * RB), c0 = (int)blockIdx.x * (16 * kOfGroup), steps = (T + BK - 1) / BK, mine = (steps - wave + WAVES - 1) / WAVES;      // steps wave, wave + 4, ...
     const int rows_a = M - r0 < 16 * RB ? M - r0 : 16 * RB, rows_b = I - c0 < 16 * kOfGroup ? I - c0 : 16 * kOfGroup;      // of a group
     const uint8_t *const a0 = A + (int64_t)r0 * T, *const b0 = B + (int64_t)c0 * T;
     const int64_t group_bytes = (int64_t)I * T;
@@ -316,11 +370,11 @@ __global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const u
     for (int j = 0; j < CB; ++j) code_b[j] = (int)block_scale_offset((PAIRS && j >= kOfGroup ? I : 0) + c0 + 16 * (j % kOfGroup) + (lane & 15), 0, rows_of_b);
     struct Codes { int a[RB], b[CB]; };
     struct Chunks { v4u c[ALIGNED ? 1 : kLoads]; };
-    Codes codes[kGluSlots];
-    Chunks chunks[kGluSlots];
+    Codes codes[SLOTS];
+    Chunks chunks[SLOTS];
     const int ld_row = lane >> 3;
     auto request = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
-        const int step = wave + n * kGluWaves;
+        const int step = wave + n * WAVES;
         const bool there = n < mine;
 #pragma unroll
         for (int i = 0; i < RB; ++i) e.a[i] = (int)(unsigned char)__builtin_amdgcn_raw_buffer_load_b8(rsSA, code_a[i], there ? step * pitchA : kOutOfRange, 0);
@@ -357,7 +411,7 @@ __global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const u
     auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
         uint8_t* const slab = slot + wave * kSlot;
         if constexpr (ALIGNED) {
-            wait_vmcnt<(kGluSlots - 1) * (kLoads + RB + CB)>();
+            wait_vmcnt<(SLOTS - 1) * (kLoads + RB + CB)>();
         } else {
             static_for<kLoads>([&](auto piece) { *reinterpret_cast<v4u*>(slab + decltype(piece)::value * 8 * BK + lane * 16) = held.c[decltype(piece)::value]; });
         }
@@ -379,22 +433,16 @@ __global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const u
 #pragma unroll
             for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, 0, now.b[j], 0, now.a[i]);
         __builtin_amdgcn_sched_barrier(0);
-        request(slot, n + kGluSlots, e, held);
+        request(slot, n + SLOTS, e, held);
     };
-    request(s_0, 0, codes[0], chunks[0]);
-    request(s_1, 1, codes[1], chunks[1]);
-    request(s_2, 2, codes[2], chunks[2]);
-    request(s_3, 3, codes[3], chunks[3]);
+    auto slot_of = [&](auto k) -> uint8_t* { constexpr int K = decltype(k)::value; return K == 0 ? s_0 : K == 1 ? s_1 : K == 2 ? s_2 : s_3; };
+    static_for<SLOTS>([&](auto k) { request(slot_of(k), decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value]); });
     int n = 0;
-    for (; n + 3 < mine; n += 4) {
-        multiply(s_0, n, codes[0], chunks[0]);
-        multiply(s_1, n + 1, codes[1], chunks[1]);
-        multiply(s_2, n + 2, codes[2], chunks[2]);
-        multiply(s_3, n + 3, codes[3], chunks[3]);
-    }
-    if (n < mine) multiply(s_0, n, codes[0], chunks[0]);
-    if (n + 1 < mine) multiply(s_1, n + 1, codes[1], chunks[1]);
-    if (n + 2 < mine) multiply(s_2, n + 2, codes[2], chunks[2]);
+    for (; n + SLOTS <= mine; n += SLOTS)
+        static_for<SLOTS>([&](auto k) { multiply(slot_of(k), n + decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value]); });
+    static_for<SLOTS - 1>([&](auto k) {
+        if (n + decltype(k)::value < mine) multiply(slot_of(k), n + decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value]);
+    });
     wait_vmcnt<0>();                             // nothing lands in LDS any more
     __syncthreads();
     v4f* const s_sum = reinterpret_cast<v4f*>(s_0);                          // [wave][block][lane]
@@ -407,7 +455,7 @@ __global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const u
     auto sum_of = [&](int block) -> v4f {
         v4f y = s_sum[block * kWave + lane];
 #pragma unroll
-        for (int w = 1; w < kGluWaves; ++w) y += s_sum[(w * (RB * CB) + block) * kWave + lane];
+        for (int w = 1; w < WAVES; ++w) y += s_sum[(w * (RB * CB) + block) * kWave + lane];
         return y;
     };
     unsigned mag = 0;
@@ -428,7 +476,7 @@ __global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const u
         }
     };
     // a wave finishes every fourth block (of pairs)
-    for (int block = wave; block < RB * kOfGroup; block += kGluWaves) {
+    for (int block = wave; block < RB * kOfGroup; block += WAVES) {
         const int i = block / kOfGroup, j = block % kOfGroup, r = r0 + 16 * i + (lane & 15), c = c0 + 16 * j + (lane >> 4) * 4, left = I - c;
         const v4f sum = sum_of(i * CB + j);
         v4f other = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -473,15 +521,22 @@ __global__ __launch_bounds__(kGluWaves * kWave) void gemm_glu_few_kernel(const u
     }
 }
 
+// Workgroups of four waves and four slots fill a CU and are a chain of a quarter of the steps; workgroups of one wave and three slots lie eight to a CU and have nothing to wait for one another.
 template <int FA, int FB, int DIR, int RB, int CB>
-static void launch_glu_few(const GluOperands& p, hipStream_t stream) {
+static void launch_glu_few(const GluOperands& p, hipStream_t stream, int num_cus) {
     constexpr int kCols = DIR == kGluForward ? 8 * CB : 16 * CB;
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.I + kCols - 1) / kCols), (unsigned)((p.M + 16 * RB - 1) / (16 * RB))), dim3(kGluWaves * kWave), 0, stream, p.A, p.sA, p.B, p.sB, p.c, p.plan, (int)p.M, (int)p.I,
-                           (int)p.T, p.amax);
+    const int64_t groups = (p.I + kCols - 1) / kCols, row_groups = (p.M + 16 * RB - 1) / (16 * RB);
+    auto launch = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)row_groups), dim3(waves * kWave), 0, stream, p.A, p.sA, p.B, p.sB, p.c, p.plan, (int)p.M, (int)p.I, (int)p.T, p.amax);
     };
-    if (p.T % 16 == 0) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, true>);
-    else if constexpr (CB == 1 || DIR == kGluForward) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, false>);
+    const char* alone = tuning_env("LLMQ_GLU_FEW_ALONE");
+    if (p.T % 16 != 0) {
+        if constexpr (CB == 1 || DIR == kGluForward) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 4, 4, false>, 4);
+    } else if (alone ? atoi(alone) != 0 : groups * row_groups > num_cus && (groups * row_groups >= 2 * num_cus || p.T <= 24 * BK)) {
+        launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 1, 3, true>, 1);
+    } else {
+        launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 4, 4, true>, 4);
+    }
 }
 
 // Launches the kernel of the choice; gemm_glu_*.hip instantiate it for a pair of formats and a direction each.
@@ -489,12 +544,12 @@ template <int FA, int FB, int DIR>
 void launch_glu(const GluOperands& p, const GluChoice& choice, hipStream_t stream, int num_cus) {
     if (choice.few) {
         if constexpr (DIR == kGluForward) {
-            p.M <= 16 ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream) : launch_glu_few<FA, FB, DIR, 2, 2>(p, stream);
+            p.M <= 16 ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream, num_cus) : launch_glu_few<FA, FB, DIR, 2, 2>(p, stream, num_cus);
         } else {
             // (as in the plain contraction)
             const bool two = p.T % 16 == 0 && (p.I + 31) / 32 >= num_cus / 2;
-            if (p.M <= 16) two ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream) : launch_glu_few<FA, FB, DIR, 1, 1>(p, stream);
-            else two ? launch_glu_few<FA, FB, DIR, 2, 2>(p, stream) : launch_glu_few<FA, FB, DIR, 2, 1>(p, stream);
+            if (p.M <= 16) two ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream, num_cus) : launch_glu_few<FA, FB, DIR, 1, 1>(p, stream, num_cus);
+            else two ? launch_glu_few<FA, FB, DIR, 2, 2>(p, stream, num_cus) : launch_glu_few<FA, FB, DIR, 2, 1>(p, stream, num_cus);
         }
         return;
     }
@@ -504,7 +559,7 @@ void launch_glu(const GluOperands& p, const GluChoice& choice, hipStream_t strea
         return;
     switch (choice.tile.edge * 64 + choice.tile.ni * 8 + choice.tile.nj) {
         LLMQ_GLU_CASE(4, 4, kNoEdge) LLMQ_GLU_CASE(4, 2, kNoEdge) LLMQ_GLU_CASE(3, 4, kNoEdge) LLMQ_GLU_CASE(2, 4, kNoEdge) LLMQ_GLU_CASE(2, 2, kNoEdge)
-        LLMQ_GLU_CASE(4, 4, kEdge) LLMQ_GLU_CASE(4, 2, kEdge) LLMQ_GLU_CASE(2, 4, kEdge) LLMQ_GLU_CASE(2, 2, kEdge)
+        LLMQ_GLU_CASE(4, 4, kEdge) LLMQ_GLU_CASE(3, 4, kEdge) LLMQ_GLU_CASE(4, 2, kEdge) LLMQ_GLU_CASE(2, 4, kEdge) LLMQ_GLU_CASE(2, 2, kEdge)
         LLMQ_GLU_CASE(2, 2, kEdgeUnaligned)
         default: break;
     }

@@ -10,19 +10,15 @@ template <int DIR>
 static GluChoice choose_glu(int64_t M, int64_t I, int64_t T, int num_cus) {
     GluChoice choice{false, {0, 0, kNoEdge}, DIR == kGluForward && I % 32 != 0};
     const char* few = tuning_env("LLMQ_GLU_FEW");
-    choice.few = few ? atoi(few) != 0 && M <= 4096 : M <= 32;
+    const int64_t cols = DIR == kGluForward ? 2 * I : I, steps = (T + BK - 1) / BK, groups = (M + 31) / 32 * ((I + 15) / 16);
+    choice.few = few ? atoi(few) != 0 && M <= 4096 : M <= 32 || groups <= num_cus || (groups <= 2 * num_cus && steps <= 8);
     if (choice.few) return choice;
-    const int64_t cols = DIR == kGluForward ? 2 * I : I, steps = (T + BK - 1) / BK;
     auto form = [&](int ni, int nj) {
         const bool whole = M % (64 * ni) == 0 && cols % (64 * nj) == 0 && T % BK == 0 && !choice.loose;
         return TilePlan{ni, nj, whole ? kNoEdge : T % 16 == 0 ? kEdge : kEdgeUnaligned};
     };
-    // what is not built: guarded tiles of 192 rows; other sides than 128 for chunks that go through registers; and where up rows do not start at multiples of the rows whose codes share a
-    // register, 64 of a tile of 256 columns and 32 of others, but for 128 x 128
-    auto built = [&](const TilePlan& p) {
-        if (p.ni == 2 && p.nj == 2) return true;
-        return p.edge != kEdgeUnaligned && (p.edge == kNoEdge || p.ni != 3) && (DIR == kGluBackward || I % (p.nj == 4 ? 64 : 32) == 0);
-    };
+    // 128 x 128 is built for everything; the others for chunks that go straight to LDS, and forward where the codes of two blocks of rows can share a register
+    auto built = [&](const TilePlan& p) { return (p.ni == 2 && p.nj == 2) || (p.edge != kEdgeUnaligned && !choice.loose); };
     if (const char* e = tuning_env("LLMQ_GLU_TILE")) {
         if (e[0] >= '2' && e[0] <= '4' && e[1] == 'x' && (e[2] == '2' || e[2] == '4') && !(e[0] == '3' && e[2] == '2')) {
             const TilePlan p = form(e[0] - '0', e[2] - '0');

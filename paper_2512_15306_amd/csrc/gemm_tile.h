@@ -146,10 +146,10 @@ struct GemmTuning {
     // Operands with a scale for each block of 128 contraction bytes (gemm_blocks.h).
     static constexpr bool kBlockScales = false;
     // Contractions joined with a SwiGLU (gemm_glu.h): kGluForward pairs the columns of a tile, kGluBackward has another epilogue only.  Their tuning structs provide
-    //   template <...> static __device__ unsigned write_out(...), which returns packed magnitudes of what it stored.
+    //   template <NI, MI, MJ, EDGE> Epilogue, whose write_out returns packed magnitudes of what it stored.
     static constexpr int kGlu = 0;
-    // kGluForward: the up rows of B do not start at a multiple of 64 rows (tiles of 256 columns) or 32 (others)
-    static constexpr bool kLooseRows = false;
+    // kGluForward: of how many blocks of 16 rows of B the codes share a register, which the up rows have to start at a multiple of (1: anywhere)
+    static constexpr int kPairBlocks = 1;
     // What the launch knows of its tiles
     typedef SplitPlan Plan;
 };
@@ -694,7 +694,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     // that a lane's row of four neighbouring blocks of 16 rows is one register.  A side of 192 starts a wave's rows at a multiple of 32: there two blocks
     // share a register.  A step's registers are requested two steps ahead, into those of the step that has just ended, as its newest loads.
     static_assert(!BS || (NI <= 4 && NJ <= 4 && MODE == kWholeTiles && FA != kFmtBf16), "sides of 320 have no registers left for scales");
-    constexpr int PA = NI == 3 ? 2 : 4, PB = PAIRS ? (MJ == 2 || V::kLooseRows ? 1 : NJ) : NJ == 3 ? 2 : 4, WA = (MI + PA - 1) / PA, WB = (MJ + PB - 1) / PB;
+    constexpr int PA = NI == 3 ? 2 : 4, PB = PAIRS ? V::kPairBlocks : NJ == 3 ? 2 : 4, WA = (MI + PA - 1) / PA, WB = (MJ + PB - 1) / PB;
     constexpr int kScaleLoads = BS ? (NI == 3 ? WA : 1) + (NJ == 3 || PAIRS ? WB : 1) : 0;
     typedef std::conditional_t<BS, BlockScales<WA, WB, PA, PB>, NoScales> Scales;
     Scales scales[2];
@@ -703,8 +703,8 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     // first block of 16 rows of the wave (with eight waves of the two that share a register)
     const int blockA = tr * (BM / 16) + wr * MI, blockB = tc * (BN / 16) + (MJ == 2 ? (wc & ~1) * MJ : wc * MJ);
     const int sc_voff = 8 * (lane & 15);
-    // kGluForward: registers for the wave's gate blocks and then for its up blocks, each from the aligned word that holds its first block's code.  Blocks of tiles of 256 columns are whole words; those of
-    // others are shifted to the low end where they are used.  A gate block is one of 16 rows always; of loose rows an up block may lie over two of those, so every lane finds its row's code.
+    // kGluForward: registers for the wave's gate blocks and then for its up blocks, each from the aligned word that holds its first block's code.  Four blocks are a whole word; fewer
+    // are shifted to the low end where they are used.  A gate block is one of 16 rows always; of loose rows an up block may lie over two of those, so every lane finds its row's code.
     const int gate_block = tc * (BN / 32) + wc * (MJ / 2);
     constexpr bool SHIFTED = PAIRS && PB < 4;
     int pair_voff[PAIRS ? WB : 1], pair_shift[PAIRS ? WB : 1];
@@ -1329,7 +1329,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     }
     };
     if constexpr (V::kGlu != 0) {
-        edge_mag = V::template write_out<NI, MI, MJ, EDGE>(acc, stage_of(wave), C, plan, tr * BM + wr * 32 * NI, Rn, PAIRS ? gate_block * 16 : tc * BN + wc * 16 * MJ, Cn, lane);
+        edge_mag = V::template Epilogue<NI, MI, MJ, EDGE>::write_out(acc, stage_of(wave), C, plan, tr * BM + wr * 32 * NI, Rn, PAIRS ? gate_block * 16 : tc * BN + wc * 16 * MJ, Cn, lane);
     } else if constexpr (EDGE != kNoEdge) {
         write_out(BoolTag<true>{});
     } else if (one_mul) {
