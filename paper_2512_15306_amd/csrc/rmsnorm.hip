@@ -125,8 +125,8 @@ __device__ inline void pad_codes(const NormCodes& out, int64_t row, int64_t C, i
 // One wavefront per row, VPL vectors per lane in registers.  EDGE: any C (the rows start at any even address, the last
 // vector of a row may be a part of one); else C % 8 == 0.  HAS_X false: no addition (res is normalised as it is, res_out is not
 // written).
-template <bool HAS_X, bool EDGE, int VPL, int OUT = kNormY>
-__global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
+template <bool HAS_X, bool EDGE, int VPL, int OUT>
+__device__ __forceinline__ void rmsnorm_row(
     const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
     int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
     float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
                     if (y) store(y + row * C, idx, o);
                 }
                 put_codes<OUT - kNormCodes, EDGE>(o, idx < nvec, codes, row, idx, C);
+                __builtin_amdgcn_sched_barrier(0);               // (all vectors at once would be registers that waves are short of)
             }
         }
         if constexpr (OUT != kNormY) return;
@@ -219,6 +220,21 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
     }
 }
 
+template <bool HAS_X, bool EDGE, int VPL>
+__global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
+    const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
+    int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
+    float* __restrict__ rstd_out, unsigned* __restrict__ partial) {
+    rmsnorm_row<HAS_X, EDGE, VPL, kNormY>(res, x, w, M, C, eps, res_out, y, rstd_out, partial, NormCodes{});
+}
+template <bool HAS_X, bool EDGE, int VPL, int OUT>
+__global__ __launch_bounds__(kRnThreads) void rmsnorm_row_blocks_kernel(
+    const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
+    int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
+    float* __restrict__ rstd_out, const NormCodes codes) {
+    rmsnorm_row<HAS_X, EDGE, VPL, OUT>(res, x, w, M, C, eps, res_out, y, rstd_out, nullptr, codes);
+}
+
 // Wider rows: the four rows of a workgroup are read by all of its lanes (VPL vectors per lane and row, two rows at a time),
 // so that a lane holds a few vectors of each row instead of a whole row's share, which leaves room for more waves, and
 // reads the norm's weight once for both.  Where one wave adds up the squares of a row, it reads them from LDS; widths that had
@@ -227,8 +243,8 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_kernel(
 // one wave per row with up to 16 vectors per lane, with the addition: 16384 x 5120 137 -> 130 us (5.2 TB/s), 8192 x 3584
 // 52 -> 46, 4096 x 7680 59 -> 51, 279 x 7680 21 -> 14; all four rows at a time took 134, 48, 63 and 14.
 // PER_BLOCK: rows of a workgroup; one where there are so few that each has a workgroup to itself.
-template <bool HAS_X, bool EDGE, int VPL, bool STREAM, int OUT = kNormY, int PER_BLOCK = kRnRowsPerBlock>
-__global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
+template <bool HAS_X, bool EDGE, int VPL, bool STREAM, int OUT, int PER_BLOCK>
+__device__ __forceinline__ void rmsnorm_rows(
     const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
     int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
     float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
@@ -376,10 +392,25 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
     }
 }
 
+template <bool HAS_X, bool EDGE, int VPL, bool STREAM>
+__global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_kernel(
+    const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
+    int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
+    float* __restrict__ rstd_out, unsigned* __restrict__ partial) {
+    rmsnorm_rows<HAS_X, EDGE, VPL, STREAM, kNormY, kRnRowsPerBlock>(res, x, w, M, C, eps, res_out, y, rstd_out, partial, NormCodes{});
+}
+template <bool HAS_X, bool EDGE, int VPL, int OUT, int PER_BLOCK>
+__global__ __launch_bounds__(kRnThreads) void rmsnorm_rows_blocks_kernel(
+    const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
+    int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
+    float* __restrict__ rstd_out, const NormCodes codes) {
+    rmsnorm_rows<HAS_X, EDGE, VPL, false, OUT, PER_BLOCK>(res, x, w, M, C, eps, res_out, y, rstd_out, nullptr, codes);
+}
+
 // More than 16384 columns: one wavefront per row, element-wise strided loops; the row is read again for the second pass
 // (from res_out when the addition was done).
-template <int OUT = kNormY>
-__global__ __launch_bounds__(kRnThreads) void rmsnorm_row_generic_kernel(
+template <int OUT>
+__device__ __forceinline__ void rmsnorm_row_generic(
     const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
     int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
     float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
@@ -436,6 +467,20 @@ __global__ __launch_bounds__(kRnThreads) void rmsnorm_row_generic_kernel(
         mag = block_max_u32<kRnThreads>(mag & 0xFFFFu, s_part);
         if (threadIdx.x == 0) partial[blockIdx.x] = mag;
     }
+}
+
+__global__ __launch_bounds__(kRnThreads) void rmsnorm_row_generic_kernel(
+    const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
+    int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
+    float* __restrict__ rstd_out, unsigned* __restrict__ partial) {
+    rmsnorm_row_generic<kNormY>(res, x, w, M, C, eps, res_out, y, rstd_out, partial, NormCodes{});
+}
+template <int OUT>
+__global__ __launch_bounds__(kRnThreads) void rmsnorm_row_generic_blocks_kernel(
+    const uint16_t* res, const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
+    int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
+    float* __restrict__ rstd_out, const NormCodes codes) {
+    rmsnorm_row_generic<OUT>(res, x, w, M, C, eps, res_out, y, rstd_out, nullptr, codes);
 }
 
 // Recompute path: rstd [M] and the scale are given, no transposed copy.  Lane = 4 rows x 8 columns; M % 4 == 0, C % 8 == 0.
@@ -649,7 +694,7 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
     uint16_t* res_out = reinterpret_cast<uint16_t*>(res_out_);
     uint16_t* y = reinterpret_cast<uint16_t*>(y_);
     const dim3 grid((unsigned)rmsnorm_blocks(M)), block(kRnThreads);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, partial, NormCodes{}); };
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, partial); };
     const bool edge = C % 8 != 0;
     auto row = [&](auto vpl) {
         constexpr int V = decltype(vpl)::value;
@@ -665,7 +710,7 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
         else { if (edge) launch(rmsnorm_rows_kernel<false, true, V, false>); else if (out) launch(rmsnorm_rows_kernel<false, false, V, true>); else launch(rmsnorm_rows_kernel<false, false, V, false>); }
     };
     switch (norm_kind(M, C, x != nullptr)) {
-        case kNormGeneric: hipLaunchKernelGGL(rmsnorm_row_generic_kernel<>, grid, block, 0, stream, res, x, w, M, C, eps, res_out, y, rstd, partial, NormCodes{}); break;
+        case kNormGeneric: hipLaunchKernelGGL(rmsnorm_row_generic_kernel, grid, block, 0, stream, res, x, w, M, C, eps, res_out, y, rstd, partial); break;
         case kNormRow:
             // (As few registers as the row needs, but for a few workgroups per CU: those are dealt out evenly only if few fit
             // on one.  3000 x 3584 with 8 and 16 vectors per lane: 21.4 / 19.1 us, 4001 x 3584 24.7 / 29.4.)
@@ -685,29 +730,34 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
     return launch_amax_final(partial, (int)rmsnorm_blocks(M), fmt, d_amax, d_scale, stream);
 }
 
-// The statistics and the residual sum, and the row-wise codes with block scales if there are any (codes.q): the kernels and the order of the sums of launch_rmsnorm_fwd.
+// The statistics and the residual sum, and the row-wise codes with block scales if there are any (codes.q): the sums of launch_rmsnorm_fwd's kernels.
+//
+// Up to eight rows a CU a workgroup has one row: it ends when that row does, and the rows are dealt out evenly.  Beyond that the several rows of a workgroup hide each other's waits.  Several / one, us, M x C:
+// codes and the transposed copy 1777 x 2880 19.75 / 16.5, 1000 x 5120 19.85 / 16.4; codes alone 1000 x 5120 15.3 / 10.35, 2048 x 4096 16.05 / 15.45, 4000 x 2731 29.05 / 29.35, 8192 x 4096 44.3 / 49.8,
+// 8192 x 5120 60.5 / 64.
 template <int OUT>
 static void launch_rows_out(const uint16_t* res, const uint16_t* x, const uint16_t* w, int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* y, float* rstd, const NormCodes& codes,
                             hipStream_t stream, int cus) {
     const int64_t rows_written = OUT >= kNormCodes ? codes.padded : M;
     const bool edge = C % 8 != 0;
     auto launch = [&](auto kernel, int per_block) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows_written + per_block - 1) / per_block)), dim3(kRnThreads), 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, nullptr, codes);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows_written + per_block - 1) / per_block)), dim3(kRnThreads), 0, stream, res, x, w, M, (int)C, eps, res_out, y, rstd, codes);
     };
     auto row = [&](auto vpl) {
         constexpr int V = decltype(vpl)::value;
         if constexpr (V <= 4) {
-            if (edge) { if (x) launch(rmsnorm_row_kernel<true, true, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_kernel<false, true, V, OUT>, kRnRowsPerBlock); return; }
+            if (edge) { if (x) launch(rmsnorm_row_blocks_kernel<true, true, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_blocks_kernel<false, true, V, OUT>, kRnRowsPerBlock); return; }
         }
-        if (x) launch(rmsnorm_row_kernel<true, false, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_kernel<false, false, V, OUT>, kRnRowsPerBlock);
+        if (x) launch(rmsnorm_row_blocks_kernel<true, false, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_blocks_kernel<false, false, V, OUT>, kRnRowsPerBlock);
     };
-    const bool one = M <= 2 * cus;
+    const char* forced = tuning_env("LLMQ_NORM_ONE");            // (tests: 0 / 1)
+    const bool one = forced ? atoi(forced) != 0 : M <= 8 * cus;
     auto rows = [&](auto vpl) {
         constexpr int V = decltype(vpl)::value;
         auto of = [&](auto has_x, auto at_edge) {
             constexpr bool X = decltype(has_x)::value, E = decltype(at_edge)::value;
-            if (one) launch(rmsnorm_rows_kernel<X, E, V, false, OUT, 1>, 1);
-            else launch(rmsnorm_rows_kernel<X, E, V, false, OUT>, kRnRowsPerBlock);
+            if (one) launch(rmsnorm_rows_blocks_kernel<X, E, V, OUT, 1>, 1);
+            else launch(rmsnorm_rows_blocks_kernel<X, E, V, OUT, kRnRowsPerBlock>, kRnRowsPerBlock);
         };
         if (x) edge ? of(std::true_type{}, std::true_type{}) : of(std::true_type{}, std::false_type{});
         else edge ? of(std::false_type{}, std::true_type{}) : of(std::false_type{}, std::false_type{});
@@ -716,8 +766,8 @@ static void launch_rows_out(const uint16_t* res, const uint16_t* x, const uint16
     if (kind == kNormRow && one && C > 4 * kWave * 8) kind = kNormRows;
     switch (kind) {
         case kNormGeneric:
-            hipLaunchKernelGGL(rmsnorm_row_generic_kernel<OUT>, dim3((unsigned)((rows_written + kRnRowsPerBlock - 1) / kRnRowsPerBlock)), dim3(kRnThreads), 0, stream, res, x, w, M, C, eps, res_out, y, rstd,
-                               nullptr, codes);
+            hipLaunchKernelGGL(rmsnorm_row_generic_blocks_kernel<OUT>, dim3((unsigned)((rows_written + kRnRowsPerBlock - 1) / kRnRowsPerBlock)), dim3(kRnThreads), 0, stream, res, x, w, M, C, eps, res_out, y, rstd,
+                               codes);
             break;
         case kNormRow:
             if (C <= 4 * kWave * 8) row(IntTag<4>{});

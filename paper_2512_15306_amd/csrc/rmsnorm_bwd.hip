@@ -210,9 +210,9 @@ __global__ __launch_bounds__(kBwdThreads) void rmsnorm_bwd_wide_sums_kernel(cons
     a.dw_partial[(int64_t)blockIdx.y * a.C + c] = sum;
 }
 
-// The rows of sums: a workgroup has 16 columns and 64 lanes to each, which take every 64th row in turn and are then added pairwise: an order that the
+// The rows of sums: a workgroup has 32 columns (a line) and 32 lanes to each, which take every 32nd row in turn and are then added pairwise: an order that the
 // number of rows alone decides.  The last workgroup finds the absmax.
-constexpr int kSumCols = 16, kSumRows = 64, kSumThreads = kSumCols * kSumRows;
+constexpr int kSumCols = 32, kSumRows = 32, kSumThreads = kSumCols * kSumRows;
 __global__ __launch_bounds__(kSumThreads) void rmsnorm_bwd_final_kernel(const float* dw_partial, int rows, const unsigned* amax_partial, int words, int C, float* dw, int accumulate, float fmax,
                                                                        float* d_amax, float* d_scale) {
     __shared__ float s_sum[kSumRows][kSumCols + 1];

@@ -5,7 +5,7 @@ Tolerances.  A BF16 rounding is off by at most 2^-8 of the value (half of finfo.
   y      from the rstd that was returned: two products and a rounding: 2^-8 + 2^-22.
   codes  from the y that was returned: exact.
   dx     mean(g n) has 8 VPL <= 64 terms in a lane's chain (C / 512 in rows beyond 16384), 6 steps of the wave and 8 waves, and three roundings a term; the result four more, and BF16's.
-  dw     at most ceil(M / 64) rows in a lane's chain, 8 groups of rows, 8 rows of sums and 6 steps pairwise, and two roundings a term."""
+  dw     at most ceil(M / 64) rows in a lane's chain, 8 groups of rows, 16 rows of sums and 5 steps pairwise, and two roundings a term."""
 import numpy as np
 import pytest
 import torch
@@ -96,6 +96,23 @@ def test_forward_has_the_bytes_of_the_norm_and_the_quantizer(M, C):
             assert torch.equal(out["y"], y) and torch.equal(out["qt"], qt) and torch.equal(out["st"], st)
 
 
+@pytest.mark.parametrize("M,C", [(1, 2304), (130, 4096), (257, 2051), (2100, 2176), (2049, 8192), (3, 16384)])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_every_kernel_of_the_forward_pass_gives_the_same_bytes(monkeypatch, M, C, fmt):
+    res, x, w = inputs(M, C, 11)
+    want = None
+    for kernel in ("1", "2"):
+        for one in ("0", "1"):
+            print("norm kernel", kernel, one, M, C, fmt, flush=True)
+            monkeypatch.setenv("LLMQ_NORM_KERNEL", kernel)
+            monkeypatch.setenv("LLMQ_NORM_ONE", one)
+            out = forward(res, x, w, fmt, cols=False)
+            if want is None:
+                want = out
+                check_codes(out["y"], out["q"], out["s"], fmt)
+            assert all(torch.equal(want[k], out[k]) for k in ("res", "rstd", "y", "q", "s"))
+
+
 @pytest.mark.parametrize("C", [200, 1024, 4096])
 def test_forward_rows_that_are_not_numbers(C):
     """An Inf or NaN marks its own row's blocks with 255 and leaves the other rows' bytes; rows of zeros have codes of zero, also where eps = 0 makes NaN of them."""
@@ -145,7 +162,7 @@ def plain_backward(i):
     if i["dres"] is not None:
         dx = dx + f64(i["dres"])
         err = err + 2.0 ** -24 * np.abs(dx)
-    return dx, 2.0 ** -8 * np.abs(dx) + (1 + 2.0 ** -8) * err + 2.0 ** -133, (dy * n).sum(0), 2.0 ** -24 * (-(-M // 64) + 8 + 8 + 6 + 2) * np.abs(dy * n).sum(0)
+    return dx, 2.0 ** -8 * np.abs(dx) + (1 + 2.0 ** -8) * err + 2.0 ** -133, (dy * n).sum(0), 2.0 ** -24 * (-(-M // 64) + 8 + 16 + 5 + 2) * np.abs(dy * n).sum(0)
 
 
 @pytest.mark.parametrize("M,C", [(1, 1), (3, 100), (33, 17), (5, 264), (1, 3584), (130, 1024), (700, 512), (4100, 600), (4099, 2048), (6, 8200), (2, 16384), (3, 16401), (70, 20000), (300, 384), (70, 2730),
