@@ -257,8 +257,8 @@ int llmq_fp8_gemm_blocks(const uint8_t* A, const uint8_t* sA, int fmtA, const ui
  *     dh[m,i] = sum_t A[m,t] dA B[i,t] dB  (binary32, not rounded);   dgu[m, i] = bf16( dh u sg (1 + g (1 - sg)) ),   dgu[m, I+i] = bf16( dh g sg )
  *   dgu [M, 2 I] BF16, the dY of the gate and up projections; h [M, I] BF16 receives bf16( g sg u ) of the kept gu for the down projection's weight gradient if it is not NULL.  dgu may be gu itself.
  *   d_amax_h, d_amax_dgu [1] float or NULL: absmax of h or dgu, as llmq_amax of them has it.
- * Sums as in llmq_fp8_gemm_blocks: products exact, their error bounded by 2^-7 of the sum of the products' magnitudes; up to 32 rows take a kernel that adds in another order.  The exponential and the reciprocal are the
- *   hardware's: sg is off by at most 2^-20 + 2^-24 |g| of it; for g < -87, where |silu(g)| < 2^-118, h may be +-0.  A sum that is no number makes its own output NaN, no other.
+ * Sums as in llmq_fp8_gemm_blocks: products exact, their error bounded by 2^-7 of the sum of the products' magnitudes; few rows (up to 32) and small problems take a kernel that adds in another order.  The exponential and the reciprocal are the
+ *   hardware's: sg is off by at most 2^-20 + 2^-24 |g| of it; for g < -87, where |silu(g)| < 2^-118, silu(g) and its derivative may be +-0.  A sum that is no number makes its own output NaN, no other.
  * fmtA: E4M3 or E5M2, the weights E4M3 (LLMQ_ERR_FORMAT otherwise).  16 <= T < 2^22, I < 2^21, (rows of an operand rounded up to 128) ceil(T / 128) < 2^31 - 4096, 128 x 64 tiles of [M, I] below 2^24 (LLMQ_ERR_SHAPE).
  * Fastest with M a multiple of 256, I of 128 and T of 128; I a multiple of 32 (forward; any multiple of 8 backward) and T of 16 otherwise.  All pointers 16-byte aligned (d_amax: 4).
  */

@@ -5,21 +5,30 @@
 
 namespace llmq {
 
-// M x I x T as in GluOperands.  LLMQ_GLU_FEW=0 / 1 (tests): the kernel for few rows never, or for up to 4096 rows always; LLMQ_GLU_TILE=IxJ: that tile where it is built for the shape.
+// M x I x T as in GluOperands.  LLMQ_GLU_FEW=0 / 1 (tests): the kernel for few rows never, or for up to 4096 rows always; else LLMQ_GLU_TILE=IxJ: that tile where it is built for
+// the shape.
+//
+// The kernel for few rows reads its operands straight from memory and divides the contraction between waves, so it has no tile to fill and ends one short wait after it began.  It
+// takes what is bounded by reading the weights, and problems whose tiles of 128 x 128 would leave most of the CUs without work.  Tiles / few, us, M x I x T, forward:
+// 16 x 18944 x 3584 45.0 / 26.6, 128 x 512 x 1024 7.6 / 4.05, 200 x 300 x 600 10.7 / 5.9, 100 x 1000 x 1001 15.3 / 7.75; backward 128 x 512 x 1024 8.8 / 3.7, 100 x 1000 x 1001
+// 15.9 / 5.9; beyond the rule, forward: 64 x 18944 x 3584 45.3 / 49.4; 48 x 2816 x 1024 7.8 / 6.7 and 64 x 8192 x 2048 12.1 / 10.4 are still ahead, but every further 32 rows read the
+// weights once more.
 template <int DIR>
 static GluChoice choose_glu(int64_t M, int64_t I, int64_t T, int num_cus) {
     GluChoice choice{false, {0, 0, kNoEdge}, DIR == kGluForward && I % 32 != 0};
     const char* few = tuning_env("LLMQ_GLU_FEW");
     const int64_t cols = DIR == kGluForward ? 2 * I : I, steps = (T + BK - 1) / BK, groups = (M + 31) / 32 * ((I + 15) / 16);
-    choice.few = few ? atoi(few) != 0 && M <= 4096 : M <= 32 || groups <= num_cus || (groups <= 2 * num_cus && steps <= 8);
-    if (choice.few) return choice;
+    const bool small = M <= 32 || groups <= num_cus || (groups <= 2 * num_cus && steps <= 8);
     auto form = [&](int ni, int nj) {
         const bool whole = M % (64 * ni) == 0 && cols % (64 * nj) == 0 && T % BK == 0 && !choice.loose;
         return TilePlan{ni, nj, whole ? kNoEdge : T % 16 == 0 ? kEdge : kEdgeUnaligned};
     };
     // 128 x 128 is built for everything; the others for chunks that go straight to LDS, and forward where the codes of two blocks of rows can share a register
     auto built = [&](const TilePlan& p) { return (p.ni == 2 && p.nj == 2) || (p.edge != kEdgeUnaligned && !choice.loose); };
-    if (const char* e = tuning_env("LLMQ_GLU_TILE")) {
+    const char* e = tuning_env("LLMQ_GLU_TILE");
+    choice.few = few ? atoi(few) != 0 && M <= 4096 : small && !e;
+    if (choice.few) return choice;
+    if (e) {
         if (e[0] >= '2' && e[0] <= '4' && e[1] == 'x' && (e[2] == '2' || e[2] == '4') && !(e[0] == '3' && e[2] == '2')) {
             const TilePlan p = form(e[0] - '0', e[2] - '0');
             if (built(p)) { choice.tile = p; return choice; }

@@ -1,0 +1,130 @@
+"""Norms and gated products of tensors beyond 2^31 and 2^32 elements: what lies at their ends, against binary64 or against a call of its own."""
+import pytest
+import torch
+
+from paper_2512_15306_amd import llmq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("100 GB of device memory are not free")
+    yield
+    torch.cuda.empty_cache()
+
+
+def u8(*n):
+    return torch.zeros(n, device=DEV, dtype=torch.uint8)
+
+
+def bf(*n):
+    return torch.zeros(n, device=DEV, dtype=torch.bfloat16)
+
+
+def random(*n, seed=1, std=1.0):
+    return (torch.randn(*n, device=DEV, generator=torch.Generator(DEV).manual_seed(seed)) * std).to(torch.bfloat16)
+
+
+def scale_rows(s, rows, cols, first, count):
+    """The bytes of whole groups of 128 rows"""
+    return s.view((cols + 127) // 128, (rows + 127) // 128 * 128)[:, first : first + (count + 127) // 128 * 128]
+
+
+@pytest.mark.parametrize("M,C", [(1_100_032, 4096), (1_100_001, 4099), (262_273, 16500)])
+def test_norms(M, C):
+    """4.3 to 4.5 billion elements: the last rows alone are not zeros."""
+    n = 256 + M % 128
+    res, w = bf(M, C), random(C, seed=2).abs() + 0.5
+    res[-n:] = random(n, C)
+    q, s, qt, st, y, rstd = u8(M, C), u8(llmq.llmq_block_scales_bytes(M, C)), u8(C, M), u8(llmq.llmq_block_scales_bytes(C, M)), bf(M, C), torch.zeros(M, device=DEV)
+    llmq.llmq_rmsnorm_fwd_fp8_blocks(res, None, w, 1e-6, None, rstd, llmq.E4M3, q, s, qt, st, y)
+    r = res[-n:].double()
+    exact = 1 / ((r * r).mean(1) + 1e-6).sqrt()
+    # a lane has 64 elements behind one another, or, of a row beyond 16384 columns, C / 64; the wave, four waves and four more roundings
+    assert ((rstd[-n:].double() - exact).abs() <= 2.0 ** -24 * (max(64, -(-C // 64)) + 20) / 2 * exact).all() and (rstd[:-n] == rstd[0]).all()
+    want = r * rstd[-n:, None].double() * w.double()
+    assert ((y[-n:].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -22) * want.abs() + 2.0 ** -133).all() and not y[:-n].any()
+    part = y[-n:].clone()
+    p, ps, pt, pst = u8(n, C), u8(llmq.llmq_block_scales_bytes(n, C)), u8(C, n), u8(llmq.llmq_block_scales_bytes(C, n))
+    llmq.llmq_quantize_fp8_blocks(part, llmq.E4M3, 1, p, ps, pt, pst)
+    assert torch.equal(q[-n:], p) and torch.equal(qt[:, -n:], pt) and p.any() and not q[:-n].any() and not qt[:, :-n].any()
+    assert torch.equal(scale_rows(s, M, C, M - n, n), scale_rows(ps, n, C, 0, n)) and (scale_rows(s, M, C, 0, M - n) == 127).all()
+    assert torch.equal(st.view(-1, (C + 127) // 128 * 128)[-((n + 127) // 128) :], pst.view(-1, (C + 127) // 128 * 128))
+    del q, qt, p, pt
+
+    dy, dres, dx = y, bf(M, C), bf(M, C)                        # (y holds what dy may hold)
+    dres[-n:] = random(n, C, seed=4)
+    ws = u8(llmq.llmq_rmsnorm_bwd_workspace_bytes(M, C))
+
+    def backward(dy, dres, res, rstd, dx):
+        dw, amax, scale = torch.zeros(C, device=DEV), torch.zeros(1, device=DEV), torch.zeros(1, device=DEV)
+        llmq.llmq_rmsnorm_bwd(dy, dres, res, w, rstd, dx, dw, False, llmq.E5M2, amax, scale, ws)
+        return dw, amax, scale
+
+    dw, amax, scale = backward(dy, dres, res, rstd, dx)
+    dx2 = bf(n, C)
+    dw2, amax2, scale2 = backward(dy[-n:].clone(), dres[-n:].clone(), res[-n:].clone(), rstd[-n:].clone(), dx2)
+    assert torch.equal(dx[-n:], dx2) and dx2.any() and not dx[:-n].any() and torch.equal(amax, amax2) and torch.equal(scale, scale2)
+    # rows are added up in another order: each side has at most n + 40 binary32 roundings behind one another (rows of zeros add nothing)
+    term = part.double() * r * rstd[-n:, None].double()
+    assert ((dw - dw2).double().abs() <= 2 * 2.0 ** -24 * (n + 40) * term.abs().sum(0)).all() and dw2.any()
+
+
+def values(codes, s, rows, cols):
+    scale = s.view(-1, (rows + 127) // 128, 16, 8).transpose(2, 3).reshape(-1, (rows + 127) // 128 * 128)[:, :rows].double() - 127
+    return codes.view(torch.float8_e4m3fn).double() * torch.exp2(scale).t().repeat_interleave(128, 1)[:, :cols]
+
+
+def operand(rows, cols, seed, low=121):
+    g = torch.Generator(DEV).manual_seed(seed)
+    codes = torch.randn(rows, cols, device=DEV, generator=g).mul(30).to(torch.float8_e4m3fn).view(torch.uint8)
+    return codes, torch.randint(low, low + 3, (llmq.llmq_block_scales_bytes(rows, cols),), device=DEV, generator=g).to(torch.uint8)
+
+
+@pytest.mark.parametrize("M,I,T,n", [(540_672, 4096, 128, 512), (540_097, 4004, 144, 449), (540_097, 4001, 130, 449), (1_100_800, 128, 4096, 512)])
+def test_gated_products(M, I, T, n):
+    """Gates and ups of more than 2^32 elements, whole tiles and ragged ones, or an operand of more than 2^32 bytes.
+
+    Gates lie beyond -87 here: 1 + e^-g passes 2^126 at g = -126 log 2 = -87.3, its reciprocal is flushed, and silu(g), |g| e^g <= 87.4 2^-126 < 2^-119, is lost.  That is off by 2^-118 in silu and in
+    F = sg (1 + g (1 - sg)), |F| <= (|g| + 1) sg, and by as much times what they are multiplied with, u and dh, in h and the gradients: the last term of each tolerance."""
+    first = M - n
+    assert first % 128 == 0
+    a, part_scales = operand(n, T, 1)
+    A, sA = u8(M, T), torch.full((llmq.llmq_block_scales_bytes(M, T),), 127, device=DEV, dtype=torch.uint8)
+    A[first:] = a
+    scale_rows(sA, M, T, first, n).copy_(part_scales.view(-1, (n + 127) // 128 * 128))
+    W, sW = operand(2 * I, T, 2, 119)
+    h, gu, amax = bf(M, I) + 3, bf(M, 2 * I) + 3, torch.zeros(1, device=DEV)
+    llmq.llmq_fp8_gemm_blocks_swiglu_fwd(A, sA, 0, W, sW, 0, h, gu, amax)
+    av, steps = values(a, part_scales, n, T), -(-T // 128)
+
+    def product(b):
+        return av @ b.t(), (2.0 ** -11 + steps * 2.0 ** -23) * (av.abs() @ b.abs().t())
+
+    exact, d = product(values(W, sW, 2 * I, T))
+    assert ((gu[first:].double() - exact).abs() <= d + 2.0 ** -8 * (exact.abs() + d)).all() and not gu[:first].any() and not h[:first].any()
+    g, u, eg, eu = exact[:, :I], exact[:, I:], d[:, :I], d[:, I:]
+    silu = g * torch.sigmoid(g)
+    err = 1.1 * (u.abs() + eu) * eg + (silu.abs() + 1.1 * eg) * eu
+    assert ((h[first:].double() - silu * u).abs() <= err + (2.0 ** -8 + 2.0 ** -19 + 2.0 ** -24 * (g.abs() + eg)) * ((silu * u).abs() + err) + 2.0 ** -118 * (1 + u.abs() + eu)).all()
+    assert amax.item() == h[first:].abs().max().item()
+
+    B, sB = operand(I, T, 3)
+    dgu = gu                                                     # (in place)
+    kept = gu[first:].double()
+    llmq.llmq_fp8_gemm_blocks_swiglu_bwd(A, sA, 0, B, sB, 0, gu, dgu, h, amax)
+    dh, d = product(values(B, sB, I, T))
+    g, u = kept[:, :I], kept[:, I:]
+    sg = torch.sigmoid(g)
+    F, rel = sg * (1 + g * (1 - sg)), 2.0 ** -8 + 2.0 ** -19 + 2.0 ** -24 * g.abs()
+    room = d * (u * F).abs() + (dh.abs() + d) * u.abs() * sg * (1 + g.abs()) * (2.0 ** -19 + 2.0 ** -24 * g.abs())
+    want = dh * u * F
+    assert ((dgu[first:, :I].double() - want).abs() <= room + rel * (want.abs() + room) + 2.0 ** -118 * (1 + (dh.abs() + d) * u.abs())).all()
+    room, want = d * (g * sg).abs(), dh * g * sg
+    assert ((dgu[first:, I:].double() - want).abs() <= room + rel * (want.abs() + room) + 2.0 ** -118 * (1 + dh.abs() + d)).all()
+    want = g * sg * u
+    assert ((h[first:].double() - want).abs() <= rel * want.abs() + 2.0 ** -118 * (1 + u.abs())).all()
+    assert not dgu[:first].any() and not h[:first].any() and amax.item() == dgu[first:].abs().max().item()

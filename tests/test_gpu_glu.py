@@ -164,6 +164,16 @@ def test_few_rows_kernel_in_groups(monkeypatch, M, I, T):
     backward(20, I, T, 1, 4)
 
 
+@pytest.mark.parametrize("M,I,T", [(1, 16, 128), (16, 100, 1008), (17, 333, 1104), (32, 512, 640), (16, 5504, 272), (25, 4104, 4000), (130, 250, 2064)])
+@pytest.mark.parametrize("alone", ["0", "1"])
+def test_few_rows_kernel_with_one_wave_and_four(monkeypatch, alone, M, I, T):
+    print("glu few", alone, M, I, T, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", "1")
+    monkeypatch.setenv("LLMQ_GLU_FEW_ALONE", alone)
+    forward(M, I, T, 1, 3)
+    backward(M, I, T, 0, 4)
+
+
 @pytest.mark.parametrize("M", [20, 300])
 def test_far_gates(M):
     """Gates far from zero on both sides: silu(g) is g or nearly nothing, never NaN."""
