@@ -260,7 +260,7 @@ int llmq_fp8_gemm_blocks(const uint8_t* A, const uint8_t* sA, int fmtA, const ui
  * Sums as in llmq_fp8_gemm_blocks: products exact, their error bounded by 2^-7 of the sum of the products' magnitudes; few rows (up to 32) and small problems take a kernel that adds in another order.  The exponential and the reciprocal are the
  *   hardware's: sg is off by at most 2^-20 + 2^-24 |g| of it; for g < -87, where |silu(g)| < 2^-118, silu(g) and its derivative may be +-0.  A sum that is no number makes its own output NaN, no other.
  * fmtA: E4M3 or E5M2, the weights E4M3 (LLMQ_ERR_FORMAT otherwise).  16 <= T < 2^22, I < 2^21, (rows of an operand rounded up to 128) ceil(T / 128) < 2^31 - 4096, 128 x 64 tiles of [M, I] below 2^24 (LLMQ_ERR_SHAPE).
- * Fastest with M a multiple of 256, I of 128 and T of 128; I a multiple of 32 (forward; any multiple of 8 backward) and T of 16 otherwise.  All pointers 16-byte aligned (d_amax: 4).
+ * Fastest with M a multiple of 256, I of 128 and T of 128; I a multiple of 32 (forward; any multiple of 8 backward) and T of 16, or at least 4, otherwise.  All pointers 16-byte aligned (d_amax: 4).
  */
 int llmq_fp8_gemm_blocks_swiglu_fwd(const uint8_t* A, const uint8_t* sA, int fmtA, const uint8_t* W, const uint8_t* sW,
                                     int fmtW, int64_t M, int64_t I, int64_t T, void* h_bf16, void* gu_bf16,

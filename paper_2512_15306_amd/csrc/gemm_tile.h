@@ -365,6 +365,7 @@ constexpr int kWholeTiles = 0, kSharePieces = 1, kShareFixup = 2;
 //   kEdge           every 16-byte chunk of an operand is aligned (row pitch a multiple of 16 bytes) and goes straight to
 //                   LDS as in the unguarded kernel.  Chunks behind the operand are out of the buffer's range and arrive
 //                   as zeros; chunks behind the end of a row (last K step of a row-wise operand) get an offset that is.
+//                   Contractions joined with a SwiGLU take row pitches of whole dwords too (cut_last_slab).
 //   kEdgeUnaligned  any row pitch.  The chunks go through registers: loaded (unaligned) a whole K step before they are
 //                   written to LDS, at offsets cut to the last 16 bytes of the operand, so no load leaves it.  The last
 //                   slab is then written a second time with guarded loads (fix_last_slab) that leave zeros behind the
@@ -530,7 +531,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         ld_voffA[m] = TA ? (m < SA::kPeriod ? tmajor_voff(SA{}, m, ldA) : 0) : rows_voff(m & 1, ldA);
         ld_voffB[m] = TB ? (m < SB::kPeriod ? tmajor_voff(SB{}, m, ldB) : 0) : rows_voff(m & 1, ldB);
     }
-    // The offsets for the last K step of a row-wise operand whose rows end inside it (T % 16 == 0: a chunk exists or not)
+    // The offsets for the last K step of a row-wise operand whose rows end inside it (T % 16 == 0: a chunk exists or not; DWORDS: it may end inside a chunk, see cut_last_slab)
     const int tail = EDGE == kEdge ? T % BK : 0;
     int tail_voffA[2], tail_voffB[2];
 #pragma unroll
@@ -578,6 +579,22 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         load_base(step, baseA, baseB);
         voffs_of_step(step);
         static_for<kLoadsPerStep>([&](auto piece) { issue_load(slabA, slabB, baseA, baseB, piece); });
+    };
+    // DWORDS: rows of whole dwords that need not be whole chunks.  The last chunk of a row brings the first bytes of the next row along (behind the operand: zeros, the buffer's range ends with
+    // its last dword); a lane that asked for such a chunk clears them in LDS when it has arrived, before the barrier that shows the slab to the other waves.
+    constexpr bool DWORDS = V::kGlu != 0 && EDGE == kEdge;
+    static_assert(!DWORDS || (LA % 2 == 0 && !TA && !TB), "operands in rows, whose pieces alternate between two patterns");
+    auto cut_last_slab = [&](uint8_t* slabA, uint8_t* slabB) __attribute__((always_inline)) {
+        const int kept = T % 16, chunk = (T % BK) & ~15;
+#pragma unroll 1
+        for (int j = 0; j < LA + LB; ++j) {
+            if ((((lane & 7) ^ row_swizzle(8 * (j & 1) + ld_row)) << 4) != chunk) continue;
+            v4u* at = reinterpret_cast<v4u*>((j < LA ? slabA + wave * RA * BK + j * 8 * BK : slabB + wave * RB * BK + (j - LA) * 8 * BK) + lane * 16);
+            v4u v = *at;
+#pragma unroll
+            for (int e = 1; e < 4; ++e) v[e] = 4 * e < kept ? v[e] : 0u;
+            *at = v;
+        }
     };
     // kEdgeUnaligned: the same pieces through registers.  (A 4 x 4 tile has too few of them: the operand pointers are kept in scratch memory and read back where the last slab is rewritten.)
     const uint8_t* uaA = TA ? A + (size_t)tr * BM : A + (size_t)tr * BM * ldA;
@@ -834,6 +851,9 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         // (kEdgeUnaligned: the slab was written by ordinary LDS stores, which the barrier orders)
         // (so may the requests for scales behind them; with four stages those of the two steps between are not counted, which waits a little longer)
         if constexpr (UA) {} else if constexpr (kTouch) wait_vmcnt<2 + kScaleLoads>(); else wait_vmcnt<(ST - 2) * kLoadsPerStep + kScaleLoads>();
+        if constexpr (DWORDS) {
+            if (kt + 2 == nk && T % 16 != 0) cut_last_slab(nxtA, nxtB);
+        }
         if constexpr (ST == 2) lds_barrier(); else lds_barrier_in_flight();
         __builtin_amdgcn_sched_barrier(0);
         int baseA, baseB;
@@ -898,6 +918,9 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!UA) wait_vmcnt<(ST - 1) * kLoadsPerStep + (kTouch ? 2 : 0) + kScaleLoads>();
+    if constexpr (DWORDS) {
+        if (nk == 1 && T % 16 != 0) cut_last_slab(ldsA0, ldsB0);
+    }
     if constexpr (ST == 2) lds_barrier(); else lds_barrier_in_flight();
     read_fragsA(ldsA0, IntTag<0>{}, aL);
     read_fragsB(ldsB0, IntTag<0>{}, bL);

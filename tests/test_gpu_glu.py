@@ -126,7 +126,8 @@ TILES = ["4x4", "3x4", "4x2", "2x4", "2x2"]
 
 
 @pytest.mark.parametrize("tile", TILES)
-@pytest.mark.parametrize("M,I,T", [(768, 512, 512), (768, 256, 128), (300, 320, 384), (450, 192, 1040), (257, 96, 144), (1000, 104, 272), (520, 2720, 272)])
+@pytest.mark.parametrize("M,I,T", [(768, 512, 512), (768, 256, 128), (300, 320, 384), (450, 192, 1040), (257, 96, 144), (1000, 104, 272), (520, 2720, 272), (300, 320, 388), (450, 192, 1044), (257, 96, 20),
+                                   (520, 2720, 1000), (1000, 104, 124), (200, 64, 252)])
 def test_every_tile(monkeypatch, tile, M, I, T):
     """Whole tiles and guarded ones, with few K steps and more; sums in the order of the plain contraction: the same bytes in the kept GU."""
     print("glu tile", tile, M, I, T, flush=True)
@@ -189,6 +190,37 @@ def test_far_gates(M):
     dgu = torch.empty_like(gu)
     llmq.llmq_fp8_gemm_blocks_swiglu_bwd(a, sa, 0, w[:I].contiguous(), sw.view(2, -1)[:, :I].contiguous().view(-1), 0, gu, dgu)
     assert torch.isfinite(dgu).all() and (dgu[:, :I][x < -110].double().abs() < 2.0 ** -100).all()
+
+
+@pytest.mark.parametrize("M,I,T", [(300, 96, 68), (300, 96, 1000), (513, 2720, 132), (20, 100, 332), (300, 100, 332), (300, 96, 130)])
+def test_what_lies_behind_a_row_does_not_count(monkeypatch, M, I, T):
+    """Rows that end inside a chunk of sixteen codes: the next row's first codes, and what lies behind the last row, are NaN."""
+    monkeypatch.setenv("LLMQ_GLU_FEW", "0")
+    g = torch.Generator().manual_seed(T)
+    (a, sa, A), (w, sw, W), (b, sb, B) = operand(g, M, T, 0, 1.0), operand(g, 2 * I, T, 0, 1.5 / np.sqrt(T)), operand(g, I, T, 0, 0.5)
+    gu = (torch.randn(M, 2 * I, generator=g) * 2).to(torch.bfloat16).to(DEV)
+
+    def run(a, w, b):
+        h, kept, dgu = (torch.empty(M, n, device=DEV, dtype=torch.bfloat16) for n in (I, 2 * I, 2 * I))
+        llmq.llmq_fp8_gemm_blocks_swiglu_fwd(a, sa, 0, w, sw, 0, h, kept)
+        llmq.llmq_fp8_gemm_blocks_swiglu_bwd(a, sa, 0, b, sb, 0, gu, dgu)
+        return h, kept, dgu
+
+    def inside(t):
+        """The tensor in the middle of one of NaNs"""
+        out = torch.full((t.numel() + 8192,), 0x7F, device=DEV, dtype=torch.uint8)
+        out[4096 : 4096 + t.numel()] = t.view(-1)
+        return out[4096 : 4096 + t.numel()].view(t.shape)
+
+    want = run(a, w, b)
+    assert all(torch.equal(x, y) for x, y in zip(want, run(inside(a), inside(w), inside(b))))
+    a2, w2, b2 = a.clone(), w.clone(), b.clone()
+    a2[1::2, :16], w2[1::2, :16], b2[1::2, :16] = 0x7F, 0x7F, 0xFF
+    h, kept, dgu = run(a2, w2, b2)
+    odd = torch.arange(2 * I) % 2 == 1                       # rows of W; I is even, so its ups' too
+    assert torch.isnan(kept[1::2]).all() and torch.isnan(kept[:, odd]).all() and torch.isnan(h[1::2]).all()
+    assert torch.equal(kept[::2, ~odd], want[1][::2, ~odd]) and torch.equal(h[::2, ::2], want[0][::2, ::2])
+    assert torch.isnan(dgu[1::2]).all() and torch.isnan(dgu[:, odd]).all() and torch.equal(dgu[::2, ~odd], want[2][::2, ~odd])
 
 
 @pytest.mark.parametrize("M", [20, 300])
