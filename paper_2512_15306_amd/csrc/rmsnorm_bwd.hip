@@ -5,6 +5,9 @@
 // HBM-bound: dy, res' and dres are read once, dx is written once (8 bytes an element).  A workgroup walks over rows: a row's lanes hold it in registers between the
 // mean and the result, and the sums of dw of their columns from row to row in binary32, so that they leave the workgroup once, as a row of the workspace.  A second
 // kernel adds those rows in an order that the sizes decide.
+//
+// 8192 x 5120 with dres (336 MB): 70.9 us, of them 4 for the second kernel, where a large copy's rate is 57; 1777 x 2730 17.5, 256 x 2048 6.3, half of it the second launch.  Two workgroups of 512 lanes
+// a CU hide each other's waits: asking for the next row while one is worked on takes the registers of the second (ragged 17.9 -> 25.9 us, large 72.7 -> 73.8).
 #include "api_checks.h"
 #include "rmsnorm.h"
 
