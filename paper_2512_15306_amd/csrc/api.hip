@@ -152,7 +152,7 @@ const char* llmq_status_string(int status) {
     }
 }
 
-int llmq_version(void) { return 213; }
+int llmq_version(void) { return 214; }
 
 size_t llmq_amax_workspace_bytes(void) { return (size_t)llmq::kAmaxMaxPartials * sizeof(unsigned); }
 
