@@ -635,7 +635,26 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         if (r >= rows) return v4u{0, 0, 0, 0};
         return load16_upto(base + r * ld + (int64_t)step * ks + kin, (int64_t)T - step * BK - kin);
     };
+    // The same without a second trip to memory (contractions joined with a SwiGLU): a chunk that a row ends in, or before, is there with the next row's bytes, which are cleared in LDS; only the
+    // operand's last row was loaded from another place.
+    auto cut_last_slab_bytes = [&](uint8_t* slabA, uint8_t* slabB) __attribute__((always_inline)) {
+        static_assert(V::kGlu == 0 || !UA || (LA % 2 == 0 && !TA && !TB), "operands in rows, whose pieces alternate between two patterns");
+#pragma unroll 1
+        for (int j = 0; j < LA + LB; ++j) {
+            const bool of_a = j < LA;
+            const int kin = ((lane & 7) ^ row_swizzle(8 * (j & 1) + ld_row)) << 4, valid = T - (nk - 1) * BK - kin;
+            if (valid >= 16) continue;
+            v4u* at = reinterpret_cast<v4u*>((of_a ? slabA + wave * RA * BK + j * 8 * BK : slabB + wave * RB * BK + (j - LA) * 8 * BK) + lane * 16);
+            const int64_t row = of_a ? (int64_t)tr * BM + wave * RA + 8 * j + ld_row : (int64_t)rowB + (PAIRS ? 0 : wave * RB) + 8 * (j - LA) + ld_row;
+            v4u v = *at;
+            if (valid > 0 && row == (of_a ? Rn : PAIRS ? 2 * Cn : Cn) - 1) v = load16_upto((of_a ? A : B) + row * T + (int64_t)(nk - 1) * BK + kin, valid);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] &= valid >= 4 * e + 4 ? ~0u : valid <= 4 * e ? 0u : ~0u >> (32 - 8 * (valid - 4 * e));
+            *at = v;
+        }
+    };
     auto fix_last_slab = [&](uint8_t* slabA, uint8_t* slabB) __attribute__((always_inline)) {
+        if constexpr (V::kGlu != 0) { cut_last_slab_bytes(slabA, slabB); return; }
 #pragma unroll 1
         for (int j = 0; j < LA; ++j)
             *reinterpret_cast<v4u*>(slabA + wave * RA * BK + j * 8 * BK + lane * 16) =

@@ -192,7 +192,7 @@ def test_far_gates(M):
     assert torch.isfinite(dgu).all() and (dgu[:, :I][x < -110].double().abs() < 2.0 ** -100).all()
 
 
-@pytest.mark.parametrize("M,I,T", [(300, 96, 68), (300, 96, 1000), (513, 2720, 132), (20, 100, 332), (300, 100, 332), (300, 96, 130)])
+@pytest.mark.parametrize("M,I,T", [(300, 96, 68), (300, 96, 1000), (513, 2720, 132), (20, 100, 332), (300, 100, 332), (300, 96, 130), (300, 100, 77), (140, 64, 255), (130, 34, 389), (513, 2720, 141)])
 def test_what_lies_behind_a_row_does_not_count(monkeypatch, M, I, T):
     """Rows that end inside a chunk of sixteen codes: the next row's first codes, and what lies behind the last row, are NaN."""
     monkeypatch.setenv("LLMQ_GLU_FEW", "0")
