@@ -345,7 +345,8 @@ static void launch_glu_tile(const GluOperands& p, bool loose, hipStream_t stream
 }
 
 // ---- Few rows: see gemm_blocks_few_kernel, whose waves, slots and sums these are.  Forward: a workgroup has 16 pairs, block 0 of its columns their gate rows and block 1 their up rows.
-// WAVES share the K steps, SLOTS of which each keeps on their way.
+// WAVES share the K steps, SLOTS of which each keeps on their way.  ALIGNED: rows of whole dwords go straight to LDS; others through registers, from offsets cut to the last 16 bytes of the operand.  What a row's
+// last chunk brings along of the next row is cleared before it is multiplied.
 template <int FA, int FB, int DIR, int RB, int CB, int WAVES, int SLOTS, bool ALIGNED>
 __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB,
                                                                        uint16_t* __restrict__ C, const GluPlan plan, int M, int I, int T, unsigned* __restrict__ amax_bits) {
@@ -371,6 +372,7 @@ __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8
     for (int i = 0; i < RB; ++i) code_a[i] = (int)block_scale_offset(r0 + 16 * i + (lane & 15), 0, M);
 #pragma unroll
     for (int j = 0; j < CB; ++j) code_b[j] = (int)block_scale_offset((PAIRS && j >= kOfGroup ? I : 0) + c0 + 16 * (j % kOfGroup) + (lane & 15), 0, rows_of_b);
+    const unsigned end_a = (unsigned)(rows_a * T - 16), end_g = (unsigned)(rows_b * T - 16), end_u = end_g;      // the last 16 bytes of a group's rows
     struct Codes { int a[RB], b[CB]; };
     struct Chunks { v4u c[ALIGNED ? 1 : kLoads]; };
     Codes codes[SLOTS];
@@ -390,15 +392,12 @@ __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8
             constexpr int row0 = 8 * (of_a ? p : (p - 2 * RB) % (2 * kOfGroup));
             const int row = row0 + ld_row, k = step * BK + (((lane & 7) ^ row_swizzle(row & 15)) << 4);
             if constexpr (ALIGNED) {
-                // (T % 16 == 0: a chunk exists or not; rows behind the operand lie outside the buffer)
+                // (rows behind the operand lie outside the buffer)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(of_a ? rsA : of_up ? rsU : rsG, (lds_void*)(slot + wave * kSlot + p * 8 * BK), 16, there && k < T ? row * T + k : kOutOfRange, 0, 0, 0);
             } else {
-                held.c[p] = v4u{0, 0, 0, 0};
-                if (there && row < (of_a ? rows_a : rows_b)) {
-                    const uint8_t* src = (of_a ? a0 : of_up ? b0 + group_bytes : b0) + (int64_t)row * T + k;
-                    if (k + 16 <= T) held.c[p] = *reinterpret_cast<const v4u_any*>(src);
-                    else held.c[p] = load16_upto(src, T - k);
-                }
+                // (all lanes, whatever their chunk is: a branch around each load takes twice the time)
+                const unsigned at = (unsigned)(row * T + k), end = of_a ? end_a : of_up ? end_u : end_g;
+                if (there) held.c[p] = *reinterpret_cast<const v4u_any*>((of_a ? a0 : of_up ? b0 + group_bytes : b0) + (at < end ? at : end));
             }
         });
         __builtin_amdgcn_sched_barrier(0);
@@ -413,9 +412,32 @@ __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8
     // LDS runs a wave's accesses in order, and the direct loads that follow are requested behind the wait for the reads
     auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
         uint8_t* const slab = slot + wave * kSlot;
+        // the last K step: a row's chunk that ends in it, or (through registers) lies behind it
+        const int left = T - (wave + n * WAVES) * BK;
         if constexpr (ALIGNED) {
             wait_vmcnt<(SLOTS - 1) * (kLoads + RB + CB)>();
+            if (left < BK && T % 16 != 0) {
+                static_for<kLoads>([&](auto piece) {
+                    const int valid = left - (((lane & 7) ^ row_swizzle((8 * decltype(piece)::value + ld_row) & 15)) << 4);
+                    if (valid > 0 && valid < 16) {
+                        v4u* const at = reinterpret_cast<v4u*>(slab + decltype(piece)::value * 8 * BK + lane * 16);
+                        *at = first_bytes(*at, valid);
+                    }
+                });
+            }
         } else {
+            if (left < BK) {
+                static_for<kLoads>([&](auto piece) {
+                    constexpr int p = decltype(piece)::value;
+                    constexpr bool of_a = p < 2 * RB, of_up = PAIRS && p >= 2 * RB + 2 * kOfGroup;
+                    const int row = 8 * (of_a ? p : (p - 2 * RB) % (2 * kOfGroup)) + ld_row, kin = ((lane & 7) ^ row_swizzle(row & 15)) << 4, valid = left - kin;
+                    if (valid < 16) {
+                        // (a group's last row was loaded from another place)
+                        if (valid > 0 && row == (of_a ? rows_a : rows_b) - 1) held.c[p] = load16_upto((of_a ? a0 : of_up ? b0 + group_bytes : b0) + (int64_t)(row + 1) * T - valid, valid);
+                        held.c[p] = first_bytes(held.c[p], valid);
+                    }
+                });
+            }
             static_for<kLoads>([&](auto piece) { *reinterpret_cast<v4u*>(slab + decltype(piece)::value * 8 * BK + lane * 16) = held.c[decltype(piece)::value]; });
         }
         auto fragment = [&](int first_row) -> v8i {
@@ -535,8 +557,11 @@ static void launch_glu_few(const GluOperands& p, hipStream_t stream, int num_cus
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)row_groups), dim3(waves * kWave), 0, stream, p.A, p.sA, p.B, p.sB, p.c, p.plan, (int)p.M, (int)p.I, (int)p.T, p.amax);
     };
     const char* alone = tuning_env("LLMQ_GLU_FEW_ALONE");
-    if (p.T % 16 != 0) {
-        if constexpr (CB == 1 || DIR == kGluForward) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 4, 4, false>, 4);
+    if (p.T % 4 != 0) {
+        if constexpr (CB == 1 || DIR == kGluForward) {
+            if (alone ? atoi(alone) != 0 : groups * row_groups > num_cus && (groups * row_groups >= 2 * num_cus || p.T <= 24 * BK)) launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 1, 2, false>, 1);
+            else launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 4, 4, false>, 4);
+        }
     } else if (alone ? atoi(alone) != 0 : groups * row_groups > num_cus && (groups * row_groups >= 2 * num_cus || p.T <= 24 * BK)) {
         launch(gemm_glu_few_kernel<FA, FB, DIR, RB, CB, 1, 3, true>, 1);
     } else {
@@ -552,7 +577,7 @@ void launch_glu(const GluOperands& p, const GluChoice& choice, hipStream_t strea
             p.M <= 16 ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream, num_cus) : launch_glu_few<FA, FB, DIR, 2, 2>(p, stream, num_cus);
         } else {
             // (as in the plain contraction)
-            const bool two = p.T % 16 == 0 && (p.I + 31) / 32 >= num_cus / 2;
+            const bool two = p.T % 4 == 0 && (p.I + 31) / 32 >= num_cus / 2;
             if (p.M <= 16) two ? launch_glu_few<FA, FB, DIR, 1, 2>(p, stream, num_cus) : launch_glu_few<FA, FB, DIR, 1, 1>(p, stream, num_cus);
             else two ? launch_glu_few<FA, FB, DIR, 2, 2>(p, stream, num_cus) : launch_glu_few<FA, FB, DIR, 2, 1>(p, stream, num_cus);
         }

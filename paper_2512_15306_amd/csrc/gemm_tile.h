@@ -391,6 +391,13 @@ __device__ inline v4u load16_upto(const uint8_t* p, int64_t valid) {
     return v4u{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
 }
 
+// The first `valid` of 16 bytes (any number), zeros for the others
+__device__ inline v4u first_bytes(v4u v, int valid) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] &= valid >= 4 * e + 4 ? ~0u : valid <= 4 * e ? 0u : ~0u >> (32 - 8 * (valid - 4 * e));
+    return v;
+}
+
 // FP8 tiles of up to 6 units (2 x 2 to 3 x 2 and 2 x 3) fit twice into the LDS of a CU, and the launch bound keeps their kernels to the half of the registers that lets them.
 // Without it the accumulating ones take 276 (3 x 2) and 324 (2 x 3): 14016 x 3200 x 256 51.0 us without, 39.0 with it.  (In BF16 they fit by themselves.)
 // (A guarded tile of six units with block scales would move accumulators out of their registers to keep to it; it has its CU to itself.)
@@ -590,10 +597,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
         for (int j = 0; j < LA + LB; ++j) {
             if ((((lane & 7) ^ row_swizzle(8 * (j & 1) + ld_row)) << 4) != chunk) continue;
             v4u* at = reinterpret_cast<v4u*>((j < LA ? slabA + wave * RA * BK + j * 8 * BK : slabB + wave * RB * BK + (j - LA) * 8 * BK) + lane * 16);
-            v4u v = *at;
-#pragma unroll
-            for (int e = 1; e < 4; ++e) v[e] = 4 * e < kept ? v[e] : 0u;
-            *at = v;
+            *at = first_bytes(*at, kept);
         }
     };
     // kEdgeUnaligned: the same pieces through registers.  (A 4 x 4 tile has too few of them: the operand pointers are kept in scratch memory and read back where the last slab is rewritten.)
@@ -648,9 +652,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
             const int64_t row = of_a ? (int64_t)tr * BM + wave * RA + 8 * j + ld_row : (int64_t)rowB + (PAIRS ? 0 : wave * RB) + 8 * (j - LA) + ld_row;
             v4u v = *at;
             if (valid > 0 && row == (of_a ? Rn : PAIRS ? 2 * Cn : Cn) - 1) v = load16_upto((of_a ? A : B) + row * T + (int64_t)(nk - 1) * BK + kin, valid);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] &= valid >= 4 * e + 4 ? ~0u : valid <= 4 * e ? 0u : ~0u >> (32 - 8 * (valid - 4 * e));
-            *at = v;
+            *at = first_bytes(v, valid);
         }
     };
     auto fix_last_slab = [&](uint8_t* slabA, uint8_t* slabB) __attribute__((always_inline)) {

@@ -165,7 +165,7 @@ def test_few_rows_kernel_in_groups(monkeypatch, M, I, T):
     backward(20, I, T, 1, 4)
 
 
-@pytest.mark.parametrize("M,I,T", [(1, 16, 128), (16, 100, 1008), (17, 333, 1104), (32, 512, 640), (16, 5504, 272), (25, 4104, 4000), (130, 250, 2064)])
+@pytest.mark.parametrize("M,I,T", [(1, 16, 128), (16, 100, 1008), (17, 333, 1104), (32, 512, 640), (16, 5504, 272), (25, 4104, 4000), (130, 250, 2064), (17, 333, 1101), (2, 700, 4001), (450, 438, 223), (31, 96, 1404)])
 @pytest.mark.parametrize("alone", ["0", "1"])
 def test_few_rows_kernel_with_one_wave_and_four(monkeypatch, alone, M, I, T):
     print("glu few", alone, M, I, T, flush=True)
@@ -192,10 +192,13 @@ def test_far_gates(M):
     assert torch.isfinite(dgu).all() and (dgu[:, :I][x < -110].double().abs() < 2.0 ** -100).all()
 
 
-@pytest.mark.parametrize("M,I,T", [(300, 96, 68), (300, 96, 1000), (513, 2720, 132), (20, 100, 332), (300, 100, 332), (300, 96, 130), (300, 100, 77), (140, 64, 255), (130, 34, 389), (513, 2720, 141)])
-def test_what_lies_behind_a_row_does_not_count(monkeypatch, M, I, T):
+@pytest.mark.parametrize("M,I,T", [(300, 96, 68), (300, 96, 1000), (513, 2720, 132), (20, 100, 332), (300, 100, 332), (300, 96, 130), (300, 100, 77), (140, 64, 255), (130, 34, 389), (513, 2720, 141), (7, 40, 1004), (33, 50, 517)])
+@pytest.mark.parametrize("few,alone", [("0", "0"), ("1", "0"), ("1", "1")])
+def test_what_lies_behind_a_row_does_not_count(monkeypatch, M, I, T, few, alone):
     """Rows that end inside a chunk of sixteen codes: the next row's first codes, and what lies behind the last row, are NaN."""
-    monkeypatch.setenv("LLMQ_GLU_FEW", "0")
+    print("glu behind rows", M, I, T, few, alone, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", few)
+    monkeypatch.setenv("LLMQ_GLU_FEW_ALONE", alone)
     g = torch.Generator().manual_seed(T)
     (a, sa, A), (w, sw, W), (b, sb, B) = operand(g, M, T, 0, 1.0), operand(g, 2 * I, T, 0, 1.5 / np.sqrt(T)), operand(g, I, T, 0, 0.5)
     gu = (torch.randn(M, 2 * I, generator=g) * 2).to(torch.bfloat16).to(DEV)
