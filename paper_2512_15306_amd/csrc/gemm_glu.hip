@@ -9,16 +9,15 @@ namespace llmq {
 // the shape.
 //
 // The kernel for few rows reads its operands straight from memory and divides the contraction between waves, so it has no tile to fill and ends one short wait after it began.  It
-// takes what is bounded by reading the weights, and problems whose tiles of 128 x 128 would leave most of the CUs without work.  Tiles / few, us, M x I x T, forward:
-// 16 x 18944 x 3584 45.0 / 26.6, 128 x 512 x 1024 7.6 / 4.05, 200 x 300 x 600 10.7 / 5.9, 100 x 1000 x 1001 15.3 / 7.75; backward 128 x 512 x 1024 8.8 / 3.7, 100 x 1000 x 1001
-// 15.9 / 5.9; beyond the rule, forward: 64 x 18944 x 3584 45.3 / 49.4; 48 x 2816 x 1024 7.8 / 6.7 and 64 x 8192 x 2048 12.1 / 10.4 are still ahead, but every further 32 rows read the
-// weights once more.
+// takes what is bounded by reading the weights, and problems of up to four of its workgroups a CU.  Tiles / few, us, M x I x T: forward 16 x 18944 x 3584 45.0 / 26.6, 128 x 512 x 1024 7.6 / 4.05,
+// 300 x 800 x 400 6.2 / 4.7, 256 x 1024 x 3584 16.8 / 15.6, 2048 x 256 x 512 6.05 / 5.2, 128 x 4096 x 2048 11.7 / 11.2, 96 x 5024 x 1024 8.6 / 8.7, 64 x 3000 x 2001 20.3 / 13.9; backward 128 x 512 x 1024
+// 8.8 / 3.7, 1000 x 512 x 1024 9.6 / 7.9, 64 x 4096 x 3584 17.8 / 7.3, 248 x 1839 x 167 16.3 / 9.25; beyond the rule, forward: 64 x 18944 x 3584 45.3 / 49.4, 65 x 6675 x 868 9.5 / 11.5, 40 x 12000 x 2001 19.3 / 24.1.
 template <int DIR>
 static GluChoice choose_glu(int64_t M, int64_t I, int64_t T, int num_cus) {
     GluChoice choice{false, {0, 0, kNoEdge}, DIR == kGluForward && I % 32 != 0};
     const char* few = tuning_env("LLMQ_GLU_FEW");
     const int64_t cols = DIR == kGluForward ? 2 * I : I, steps = (T + BK - 1) / BK, groups = (M + 31) / 32 * ((I + 15) / 16);
-    const bool small = M <= 32 || groups <= num_cus || (groups <= 2 * num_cus && steps <= 8);
+    const bool small = M <= 32 || groups <= num_cus || (groups <= 4 * num_cus && groups * steps <= 64 * num_cus);
     // (Rows of whole dwords go straight to LDS.  Through registers, in tiles of 128 x 128 / straight: forward 1777 x 2720 x 1000 28.5 / 22.5 us, 4001 x 8000 with T = 2001 / 2004 279 / 154; backward
     // 1777 x 2720 x 1000 21.9 / 19.85, 4001 x 8001 with T = 2001 / 2004 221 / 175.  Through registers a tile of twice the size has 4001 x 8000 x 2001 at 263 and 1777 x 2720 x 1000 at 35.)
     auto form = [&](int ni, int nj) {
