@@ -451,7 +451,8 @@ int llmq_rmsnorm_apply_fp8_slabs(const void* res_bf16, const void* w_bf16, const
 /*
  * The same norm in front of a contraction with block scales, and its gradient.
  *
- * llmq_rmsnorm_fwd_fp8_blocks: res', rstd as llmq_rmsnorm_fwd leaves them, and y as llmq_quantize_fp8_blocks with block_rows 1 would write it, bit for bit:
+ * llmq_rmsnorm_fwd_fp8_blocks: res' as llmq_rmsnorm_fwd leaves it, rstd = 1 / sqrt(mean of the squares + eps) with sums in binary64 and one rounding (llmq_rmsnorm_fwd has sums in binary32), and
+ *   y = bf16( (res' rstd) w ) as llmq_quantize_fp8_blocks with block_rows 1 would write it, bit for bit:
  *   q [M, C] and s: codes of y with a scale for each row and 128 columns;   q_t [C, M] and s_t: of the transposed tensor, a scale for each column and 128 rows.
  *   q and s may be NULL together, or q_t and s_t; one pair must be there.  Without q_t (serving) it is one pass.  y is rounded to BF16 before its codes are made, so that both copies
  *   are made from the same values; y_bf16 receives them if it is not NULL.  x, res_out as in llmq_rmsnorm_fwd (x may be NULL, res_out may be res).  No workspace, no absmax.

@@ -42,16 +42,35 @@ __device__ inline void add_squares(const v4u& r, float& ss) {
         ss = __builtin_fmaf(b, b, ss);
     }
 }
+__device__ inline void add_squares(const v4u& r, double& ss) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const double a = rn_lo(r[j]), b = rn_hi(r[j]);
+        ss = __builtin_fma(a, a, ss);
+        ss = __builtin_fma(b, b, ss);
+    }
+}
+__device__ inline void add_square(float v, float& ss) { ss = __builtin_fmaf(v, v, ss); }
+__device__ inline void add_square(double v, double& ss) { ss = __builtin_fma(v, v, ss); }
 // The same element by element, from a row in LDS
 __device__ inline float sum_by_elements(const uint16_t* s_row, int C, int lane) {
     float ss = 0.0f;
 #pragma unroll 8
-    for (int c = lane; c < C; c += kWave) {
-        const float v = __uint_as_float((unsigned)s_row[c] << 16);
-        ss = __builtin_fmaf(v, v, ss);
-    }
+    for (int c = lane; c < C; c += kWave) add_square(__uint_as_float((unsigned)s_row[c] << 16), ss);
     return ss;
 }
+__device__ inline float wave_sum(float v) { return wave_sum_f32(v); }
+__device__ inline double wave_sum(double v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
+    return v;
+}
+__device__ inline float rstd_of(float ss, int64_t C, float eps) {
+    const float ms = ss / (float)C;
+    return 1.0f / __builtin_sqrtf(ms + eps);
+}
+// (C eps is exact: 24 bits each)
+__device__ inline float rstd_of(double ss, int64_t C, float eps) { return (float)__builtin_sqrt((double)C / (ss + (double)C * (double)eps)); }
 
 __device__ inline unsigned fold_pairs(unsigned m0, unsigned m1, unsigned m2, unsigned m3) {
     m0 = pk_max_mag(pk_max_mag(m0, m1), pk_max_mag(m2, m3));
@@ -100,6 +119,10 @@ __device__ inline void rn_store(uint16_t* row, int idx, int C, const v4u& v) {
 // What a forward kernel leaves of y: the values and a partial absmax for each workgroup; nothing (the statistics and the sum are all that is wanted: the codes are made in
 // tiles then, which hold every block of both copies whole); or codes with a scale for every 128 values of a row (kNormCodes + format), and the values if y is not NULL.
 constexpr int kNormY = 0, kNormStats = 1, kNormCodes = 2;
+// The statistic of codes with block scales is summed in binary64 and rounded once, whatever the order: a rounding of y that falls the other way can move a whole code, an eighth of its value (8192 x 3584, eight inputs:
+// 181 codes of the transposed copies differ from the exact ones with the sums of the plain norm, 127 with elementary operations in binary32, 101 with this; the sums take no longer).
+template <int OUT>
+using NormSum = std::conditional_t<OUT == kNormY, float, double>;
 struct NormCodes {
     uint8_t *q, *s;
     int64_t padded;                             // rows rounded up to a multiple of 128, bytes of a K step
@@ -132,7 +155,8 @@ __device__ __forceinline__ void rmsnorm_row(
     float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
     // res_out may be res (addition in place): every lane reads its elements before it writes them
     __shared__ unsigned s_part[kRnThreads / kWave];
-    __shared__ v4u s_rows[kRnRowsPerBlock][EDGE ? VPL * kWave : 1];
+    constexpr bool BY_ELEMENTS = EDGE && OUT == kNormY;
+    __shared__ v4u s_rows[kRnRowsPerBlock][BY_ELEMENTS ? VPL * kWave : 1];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = threadIdx.x / kWave;
     const int64_t row = (int64_t)blockIdx.x * kRnRowsPerBlock + wave;
@@ -157,25 +181,24 @@ __device__ __forceinline__ void rmsnorm_row(
                 }
             }
         }
-        float ss = 0.0f;
+        NormSum<OUT> ss = 0;
 #pragma unroll
         for (int k = 0; k < VPL; ++k) {
             const int idx = k * kWave + lane;
             if (k * kWave < nvec && idx < nvec) {
                 if constexpr (HAS_X) store(res_out + row * C, idx, r[k]);
-                if constexpr (EDGE) s_rows[wave][idx] = r[k];
+                if constexpr (BY_ELEMENTS) s_rows[wave][idx] = r[k];
                 else add_squares(r[k], ss);
             }
         }
-        if constexpr (EDGE) {
+        if constexpr (BY_ELEMENTS) {
             // only this wave reads what it wrote: no barrier, but the order of its LDS accesses has to stay
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             ss = sum_by_elements(reinterpret_cast<const uint16_t*>(s_rows[wave]), C, lane);
         }
-        ss = wave_sum_f32(ss);
-        const float ms = ss / (float)C;
-        const float rstd = 1.0f / __builtin_sqrtf(ms + eps);
+        ss = wave_sum(ss);
+        const float rstd = rstd_of(ss, C, eps);
         if (lane == 0) rstd_out[row] = rstd;
         if constexpr (OUT >= kNormCodes) {
 #pragma unroll
@@ -249,10 +272,11 @@ __device__ __forceinline__ void rmsnorm_rows(
     int64_t M, int C, float eps, uint16_t* res_out, uint16_t* __restrict__ y,
     float* __restrict__ rstd_out, unsigned* __restrict__ partial, const NormCodes codes) {
     constexpr int ROWS = VPL <= 4 && PER_BLOCK > 1 ? 2 : 1;
-    constexpr bool ONE_WAVE = !EDGE && VPL * kRnThreads * 8 <= kRnVecOrderC;        // sums a row (VPL > 4 is for wider ones)
+    constexpr bool ONE_WAVE = OUT == kNormY && !EDGE && VPL * kRnThreads * 8 <= kRnVecOrderC;        // sums a row (VPL > 4 is for wider ones)
     constexpr int kWaves = kRnThreads / kWave;
     __shared__ unsigned s_part[kWaves];
-    __shared__ float s_rstd[kRnRowsPerBlock], s_sum[kRnRowsPerBlock][kWaves];
+    __shared__ float s_rstd[kRnRowsPerBlock];
+    __shared__ NormSum<OUT> s_sum[kRnRowsPerBlock][kWaves];
     __shared__ v4u s_rows[ONE_WAVE ? ROWS : 1][ONE_WAVE ? VPL * kRnThreads : 1];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = threadIdx.x / kWave;
@@ -286,7 +310,7 @@ __device__ __forceinline__ void rmsnorm_rows(
             }
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
-            float ss = 0.0f;
+            NormSum<OUT> ss = 0;
 #pragma unroll
             for (int k = 0; k < VPL; ++k) {
                 const int idx = k * kRnThreads + threadIdx.x;
@@ -304,7 +328,7 @@ __device__ __forceinline__ void rmsnorm_rows(
                 }
             }
             if constexpr (!ONE_WAVE) {
-                ss = wave_sum_f32(ss);
+                ss = wave_sum(ss);
                 if (lane == 0) s_sum[p + i][wave] = ss;
             }
         }
@@ -312,12 +336,11 @@ __device__ __forceinline__ void rmsnorm_rows(
         float rstd[ROWS];
         if constexpr (ONE_WAVE) {
             if (wave < ROWS && row + wave < M) {
-                float ss = 0.0f;
+                NormSum<OUT> ss = 0;
 #pragma unroll 4
                 for (int idx = lane; idx < nvec; idx += kWave) add_squares(s_rows[wave][idx], ss);
-                ss = wave_sum_f32(ss);
-                const float ms = ss / (float)C;
-                const float t = 1.0f / __builtin_sqrtf(ms + eps);
+                ss = wave_sum(ss);
+                const float t = rstd_of(ss, C, eps);
                 if (lane == 0) {
                     rstd_out[row + wave] = t;
                     s_rstd[p + wave] = t;
@@ -329,11 +352,10 @@ __device__ __forceinline__ void rmsnorm_rows(
         } else {
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
-                float t = s_sum[p + i][0];
+                NormSum<OUT> t = s_sum[p + i][0];
 #pragma unroll
                 for (int v = 1; v < kWaves; ++v) t += s_sum[p + i][v];
-                const float ms = t / (float)C;
-                rstd[i] = 1.0f / __builtin_sqrtf(ms + eps);
+                rstd[i] = rstd_of(t, C, eps);
                 if (threadIdx.x == 0 && row + i < M) rstd_out[row + i] = rstd[i];
             }
         }
@@ -420,19 +442,17 @@ __device__ __forceinline__ void rmsnorm_row_generic(
     const int64_t row = (int64_t)blockIdx.x * kRnRowsPerBlock + wave;
     unsigned mag = 0;
     if (row < M) {
-        float ss = 0.0f;
+        NormSum<OUT> ss = 0;
         for (int64_t c = lane; c < C; c += kWave) {
             unsigned bits = res[row * C + c];
             if (x) {
                 bits = rn_pack(__uint_as_float(bits << 16) + __uint_as_float((unsigned)x[row * C + c] << 16), 0.0f) & 0xFFFFu;
                 res_out[row * C + c] = (uint16_t)bits;
             }
-            const float v = __uint_as_float(bits << 16);
-            ss = __builtin_fmaf(v, v, ss);
+            add_square((NormSum<OUT>)__uint_as_float(bits << 16), ss);
         }
-        ss = wave_sum_f32(ss);
-        const float ms = ss / (float)C;
-        const float rstd = 1.0f / __builtin_sqrtf(ms + eps);
+        ss = wave_sum(ss);
+        const float rstd = rstd_of(ss, C, eps);
         if (lane == 0) rstd_out[row] = rstd;
         const uint16_t* src = x ? res_out : res;          // this lane re-reads exactly the elements it wrote
         if constexpr (OUT >= kNormCodes) {
@@ -730,7 +750,7 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
     return launch_amax_final(partial, (int)rmsnorm_blocks(M), fmt, d_amax, d_scale, stream);
 }
 
-// The statistics and the residual sum, and the row-wise codes with block scales if there are any (codes.q): the sums of launch_rmsnorm_fwd's kernels.
+// The statistics and the residual sum, and the row-wise codes with block scales if there are any (codes.q).
 //
 // Up to eight rows a CU a workgroup has one row: it ends when that row does, and the rows are dealt out evenly.  Beyond that the several rows of a workgroup hide each other's waits.  Several / one, us, M x C:
 // codes and the transposed copy 1777 x 2880 19.75 / 16.5, 1000 x 5120 19.85 / 16.4; codes alone 1000 x 5120 15.3 / 10.35, 2048 x 4096 16.05 / 15.45, 4000 x 2731 29.05 / 29.35, 8192 x 4096 44.3 / 49.8,

@@ -95,7 +95,7 @@ def test_each_stage(M, C, I):
     assert torch.equal(b.res, stream)
     r, w = f64(stream), f64(b.norm)
     rstd = 1 / np.sqrt((r * r).mean(1) + EPS)
-    np.testing.assert_allclose(f64(b.rstd), rstd, rtol=2.0 ** -17, atol=0)
+    np.testing.assert_allclose(f64(b.rstd), rstd, rtol=2.0 ** -24 + C * 2.0 ** -52, atol=0)
     # codes of a value that may have been rounded the other way: half a step of BF16, 2^-17 of rstd, and half a step of E4M3, 2^-4, or, next to zero, half of its smallest step 2^-9 under the block's scale
     y = r * rstd[:, None] * w
     for transposed in (False, True):
@@ -144,15 +144,16 @@ def test_each_stage(M, C, I):
 
 
 def test_the_operators_that_are_joined_give_what_they_give_apart():
-    """Norm and quantizer; gate and up product.  h and the gradients differ by what is not rounded in between, half a step of BF16 of every factor."""
+    """Norm (from its statistic) and quantizer; gate and up product.  h and the gradients differ by what is not rounded in between, half a step of BF16 of every factor."""
     b = Half(300, 512, 640, 3)
     b.forward()
     b.backward(False)
     M, C, I = b.M, b.C, b.I
     res, y, rstd, a = bf(M, C), bf(M, C), f32(M), f32(1)
     llmq.llmq_rmsnorm_fwd(b.residual, b.x, b.norm, EPS, res, y, rstd, 0, a, None, u8(llmq.llmq_rmsnorm_workspace_bytes(M)))
-    c = Codes(M, C, 0, 1).of(y)
-    assert all(torch.equal(p, q) for p, q in ((res, b.res), (rstd, b.rstd), (c.q, b.cy.q), (c.s, b.cy.s), (c.q_t, b.cy.q_t), (c.s_t, b.cy.s_t)))
+    assert ((rstd - b.rstd).abs() <= 2.0 ** -18 * rstd).all()                 # (sums in binary32)
+    c = Codes(M, C, 0, 1).of((res.float() * b.rstd[:, None] * b.norm.float()).to(torch.bfloat16))
+    assert all(torch.equal(p, q) for p, q in ((res, b.res), (c.q, b.cy.q), (c.s, b.cy.s), (c.q_t, b.cy.q_t), (c.s_t, b.cy.s_t)))
     gu, h = bf(M, 2 * I), bf(M, I)
     llmq.llmq_fp8_gemm_blocks(c.q, c.s, 0, b.c_up.q, b.c_up.s, 0, gu)
     room = product(c.values(), b.c_up.values())[1]
