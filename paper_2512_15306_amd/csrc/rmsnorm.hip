@@ -752,9 +752,9 @@ int launch_rmsnorm_fwd(const void* res_, const void* x_, const void* w_, int64_t
 
 // The statistics and the residual sum, and the row-wise codes with block scales if there are any (codes.q).
 //
-// Up to eight rows a CU a workgroup has one row: it ends when that row does, and the rows are dealt out evenly.  Beyond that the several rows of a workgroup hide each other's waits.  Several / one, us, M x C:
-// codes and the transposed copy 1777 x 2880 19.75 / 16.5, 1000 x 5120 19.85 / 16.4; codes alone 1000 x 5120 15.3 / 10.35, 2048 x 4096 16.05 / 15.45, 4000 x 2731 29.05 / 29.35, 8192 x 4096 44.3 / 49.8,
-// 8192 x 5120 60.5 / 64.
+// Up to eight rows a CU a workgroup has one row: it ends when that row does, and the rows are dealt out evenly.  Beyond that the several rows of a workgroup hide each other's waits where there are codes to make.
+// Several / one, us, M x C: with the transposed copy (statistics alone in this pass) 1777 x 2880 20.0 / 16.3, 4096 x 3584 29.4 / 28.7, 8192 x 3584 51.1 / 48.7, 4096 x 8192 57.6 / 56.0, 16384 x 4096 110.9 / 110.1,
+// 8192 x 2304 35.1 / 35.4, ragged 4000 x 2731 29.2 / 30.0; codes 1000 x 5120 14.7 / 10.1, 2048 x 4096 16.6 / 15.0, 4096 x 3584 22.2 / 24.1, 8192 x 4096 44.0 / 45.1.
 template <int OUT>
 static void launch_rows_out(const uint16_t* res, const uint16_t* x, const uint16_t* w, int64_t M, int64_t C, float eps, uint16_t* res_out, uint16_t* y, float* rstd, const NormCodes& codes,
                             hipStream_t stream, int cus) {
@@ -771,7 +771,7 @@ static void launch_rows_out(const uint16_t* res, const uint16_t* x, const uint16
         if (x) launch(rmsnorm_row_blocks_kernel<true, false, V, OUT>, kRnRowsPerBlock); else launch(rmsnorm_row_blocks_kernel<false, false, V, OUT>, kRnRowsPerBlock);
     };
     const char* forced = tuning_env("LLMQ_NORM_ONE");            // (tests: 0 / 1)
-    const bool one = forced ? atoi(forced) != 0 : M <= 8 * cus;
+    const bool one = forced ? atoi(forced) != 0 : M <= 8 * cus || (OUT == kNormStats && !edge && M <= (int64_t)kMaxWorkgroups);
     auto rows = [&](auto vpl) {
         constexpr int V = decltype(vpl)::value;
         auto of = [&](auto has_x, auto at_edge) {
