@@ -18,8 +18,8 @@ static GluChoice choose_glu(int64_t M, int64_t I, int64_t T, int num_cus) {
     const char* few = tuning_env("LLMQ_GLU_FEW");
     const int64_t cols = DIR == kGluForward ? 2 * I : I, steps = (T + BK - 1) / BK, groups = (M + 31) / 32 * ((I + 15) / 16);
     const bool small = M <= 32 || groups <= num_cus || (groups <= 4 * num_cus && groups * steps <= 64 * num_cus);
-    // (Rows of whole dwords go straight to LDS.  Through registers, in tiles of 128 x 128 / straight: forward 1777 x 2720 x 1000 28.5 / 22.5 us, 4001 x 8000 with T = 2001 / 2004 279 / 154; backward
-    // 1777 x 2720 x 1000 21.9 / 19.85, 4001 x 8001 with T = 2001 / 2004 221 / 175.  Through registers a tile of twice the size has 4001 x 8000 x 2001 at 263 and 1777 x 2720 x 1000 at 35.)
+    // (Rows of whole dwords go straight to LDS.  Through registers, in tiles of 128 x 128 / straight: forward 1777 x 2720 x 1000 28.5 / 22.5 us, 4001 x 8000 with T = 2001 / 2004 265 / 154; backward
+    // 1777 x 2720 x 1000 21.9 / 19.85, 4001 x 8001 with T = 2001 / 2004 210 / 175.  Through registers a tile of twice the size is 5 % faster on 4001 x 8000 x 2001 and takes 35 for 1777 x 2720 x 1000.)
     auto form = [&](int ni, int nj) {
         const bool whole = M % (64 * ni) == 0 && cols % (64 * nj) == 0 && T % BK == 0 && !choice.loose;
         return TilePlan{ni, nj, whole ? kNoEdge : T % 4 == 0 ? kEdge : kEdgeUnaligned};

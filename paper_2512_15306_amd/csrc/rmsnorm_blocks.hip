@@ -3,8 +3,8 @@
 // HBM-bound.  A scale of the row-wise copy belongs to 128 values of a row, which the forward kernels have in registers: one pass (rmsnorm.hip), 4 bytes read and 2 + 1 written an
 // element.  A scale of the transposed copy belongs to 128 rows, and a row's statistic to all of its columns: no workgroup holds both, so with a transposed copy there are two passes, one
 // for the sum and its statistics, and the block quantizer's over tiles of 128 x 128 (quantize_blocks.hip), which norms what it loads: 4 + 2 bytes read, 2 + 1 + 1 written, of
-// which the 2 read again come from the memory-side cache up to about 100 MB.  8192 x 3584 with both copies 50 us (30.7 + 19.8, 5.7 and 6.0 TB/s in either pass), 1777 x 2880 16.4; 32 x 3584 along the
-// rows alone 4 us.  (The norm and the quantizer one after the other write and read y besides, 118 MB at 8192 x 3584.)
+// which the 2 read again come from the memory-side cache up to about 100 MB.  8192 x 3584 with both copies 48.5 us (6.0 TB/s in either pass), 1777 x 2880 16.2; 32 x 3584 along the
+// rows alone 3.7 us.  (The norm and the quantizer one after the other write and read y besides, 118 MB at 8192 x 3584.)
 #include "api_checks.h"
 #include "llmq_kernels.h"
 
