@@ -129,6 +129,19 @@ def check_store_data(src: str, asm: str) -> None:
         raise RuntimeError("%s: registers of a buffer store written right behind it:\n  %s" % (src, "\n  ".join(bad[:20])))
 
 
+def check_store_offsets(src: str, asm: str) -> None:
+    """Rows and columns behind an output are dropped by the buffer's range, with which only the lane's offset of a store is documented to be compared.  A buffer store whose offset includes a
+    scalar register is a build error."""
+    bad = []
+    for m in re.finditer(r"^(_ZN4llmq\w*):[^\n]*\n(.*?)^\.Lfunc_end", asm, re.S | re.M):
+        for l in m.group(2).splitlines():
+            store = re.match(r"\s*buffer_store_\w+ .*s\[\d+:\d+\], (\w+)", l)
+            if store and store.group(1) != "0":
+                bad.append("%s: %s" % (m.group(1), l.split(";")[0].strip()))
+    if bad:
+        raise RuntimeError("%s: buffer stores with a scalar offset:\n  %s" % (src, "\n  ".join(bad[:20])))
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     work = tempfile.mkdtemp(prefix="llmq_build_")
@@ -205,6 +218,7 @@ def _build_in(work: str, hipcc: str, verbose: bool) -> str:
         check_accumulator_reads(src, asm)
         check_scale_operands(src, asm)
         check_store_data(src, asm)
+        check_store_offsets(src, asm)
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", new_lib])
     binding_built = binding_built and _finish_binding(_run_binding(link_binding))
     # Both are there (or the module is not going to be): now they replace the old ones.  A module of another build must not stay

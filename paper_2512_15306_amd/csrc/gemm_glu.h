@@ -35,8 +35,8 @@ __device__ inline float bf16_hi(unsigned w) { return __uint_as_float(w & 0xFFFF0
 __device__ inline v2u bf16_of(const v4f& v) { return __builtin_bit_cast(v2u, __builtin_convertvector(v, bf16x4)); }
 
 // A wave's part of a BF16 matrix, 32 rows of it (i) in pieces of eight columns: the lane's piece k, of SLOTS pieces in a row, is one of a row 64 / SLOTS further down for every k.  It is
-// addressed by a register of the lane and a uniform offset (stores: their sum), through a buffer that ends with the part's last element.  EDGE kinds: pieces beside the matrix get an offset outside the
-// buffer.  Widths that are no multiples of 8: whole pieces at any address where the part lies inside the matrix (1000 x 4001 x 1040 backward 17.6 us, element by element 42.8), elsewhere element by element.
+// addressed by an offset of the lane through a buffer that ends with the part's last element.  EDGE kinds: pieces beside the matrix get an offset outside the buffer, and rows behind it are outside by
+// themselves.  Only the lane's offset is documented to be compared with the buffer's end, so the row is part of it; where every row exists, loads have the row in the uniform offset.  Widths that are no multiples of 8: whole pieces at any address where the part lies inside the matrix (1000 x 4001 x 1040 backward 17.6 us, element by element 42.8), elsewhere element by element.
 template <int EDGE, int SLOTS>
 struct GluRows {
     static constexpr int kOut = 0x7FFFFF00, kRowStep = kWave / SLOTS;
@@ -56,30 +56,32 @@ struct GluRows {
         base = const_cast<uint16_t*>(p) + (int64_t)r * ld + c;
     }
     __device__ bool vector() const { return EDGE == kNoEdge || mode == kPieces; }
-    __device__ int row(int i, int k) const { return (32 * i + k * kRowStep) * pitch; }
+    __device__ int row(int i, int k) const { return (32 * i + k * kRowStep) * pitch; }              // (below 2^30: kOut and a row are below 2^32)
     __device__ bool exists(int i, int k) const { return 32 * i + k * kRowStep < rows_left && cols_left > 0; }
-    __device__ int element(int e) const { return e < cols_left ? voff + 2 * e : kOut; }
+    __device__ int piece(int i, int k) const { return (int)((unsigned)voff + (unsigned)row(i, k)); }
+    __device__ int element(int i, int k, int e) const { return (int)((unsigned)(e < cols_left ? voff + 2 * e : kOut) + (unsigned)row(i, k)); }
     __device__ v4u_at2* address(int i, int k) const { return reinterpret_cast<v4u_at2*>(reinterpret_cast<uint8_t*>(base) + (int64_t)(32 * i + k * kRowStep) * pitch); }
     // STREAMED: past what the caches hold
     template <bool STREAMED = false>
     __device__ __attribute__((always_inline)) v4u load(int i, int k) const {
-        if (vector()) return __builtin_amdgcn_raw_buffer_load_b128(rs, voff, row(i, k), STREAMED ? 2 : 0);
+        if (EDGE == kNoEdge) return __builtin_amdgcn_raw_buffer_load_b128(rs, voff, row(i, k), STREAMED ? 2 : 0);
+        if (vector()) return __builtin_amdgcn_raw_buffer_load_b128(rs, piece(i, k), 0, STREAMED ? 2 : 0);
         v4u v = {0, 0, 0, 0};
         if (mode == kAnyAddress) {
             if (exists(i, k)) v = *address(i, k);
             return v;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e >> 1] |= (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, element(e), row(i, k), 0) << (16 * (e & 1));
+        for (int e = 0; e < 8; ++e) v[e >> 1] |= (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, element(i, k, e), 0, 0) << (16 * (e & 1));
         return v;
     }
     // and, of the EDGE kinds, the magnitudes of what is stored
     __device__ __attribute__((always_inline)) void store(int i, int k, const v4u& v, unsigned& mag) const {
         if (vector() || mode == kAnyAddress) {
             const bool there = EDGE != kNoEdge && exists(i, k);
-            // (The row in the lane's offset, not the uniform one: behind a wide buffer store the compiler keeps the next instruction off the stored registers only if the store has no scalar
+            // (The row in the lane's offset of whole tiles too: behind a wide buffer store the compiler keeps the next instruction off the stored registers only if the store has no scalar
             // offset.  With one, a third of the runs of 1777 x 2720 x 1024 had last words of pieces that were the next piece's.)
-            if (vector()) __builtin_amdgcn_raw_buffer_store_b128(v, rs, voff + row(i, k), 0, 0);
+            if (vector()) __builtin_amdgcn_raw_buffer_store_b128(v, rs, piece(i, k), 0, 0);
             else if (there) *address(i, k) = v;
             if (there) {
 #pragma unroll
@@ -89,7 +91,7 @@ struct GluRows {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const unsigned short bits = (unsigned short)(e & 1 ? v[e >> 1] >> 16 : v[e >> 1]);
-                __builtin_amdgcn_raw_buffer_store_b16(bits, rs, element(e), row(i, k), 0);
+                __builtin_amdgcn_raw_buffer_store_b16(bits, rs, element(i, k, e), 0, 0);
                 if (32 * i + k * kRowStep < rows_left && e < cols_left) mag = pk_max_mag(mag, (unsigned)bits);
             }
         }

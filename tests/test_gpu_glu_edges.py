@@ -1,0 +1,29 @@
+"""GPU parity of the gated products where their tiles end: rows and columns behind the outputs in every kernel and with longer contractions (formulas, inputs and tolerances: test_gpu_glu.py)."""
+import pytest
+import torch
+
+from tests import test_gpu_glu as glu
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(autouse=True)
+def rows_behind(monkeypatch):
+    """Outputs with 160 rows of rubbish behind them, more than a wave's part of any tile."""
+
+    def empty(rows, cols):
+        t = torch.full((rows + 160, cols), -7.0, device=DEV, dtype=torch.bfloat16)
+        return t[:rows], t[rows:]
+
+    monkeypatch.setattr(glu, "empty", empty)
+
+
+@pytest.mark.parametrize("M,I,T", [(20, 100, 144), (33, 37, 256), (130, 333, 272), (250, 65, 128), (140, 100, 77), (257, 129, 389)])
+@pytest.mark.parametrize("few", ["0", "1"])
+def test_nothing_is_written_behind_the_last_row(monkeypatch, few, M, I, T):
+    print("glu rows behind", few, M, I, T, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", few)
+    glu.forward(M, I, T, 0, 3)
+    glu.backward(M, I, T, 1, 4)
+    glu.backward(M, I, T, 0, 5, want_h=False, in_place=True)
