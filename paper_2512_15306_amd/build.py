@@ -31,6 +31,8 @@ TILE_SOURCES += ["gemm_glu_%s.hip" % kind for kind in ("fwd_e4m3_e4m3", "fwd_e5m
 SOURCES = TILE_SOURCES + ["gemm.hip", "gemm_blocks.hip", "gemm_glu.hip", "gemm_tmajor.hip", "quantize_blocks.hip", "api.hip", "amax.hip", "quantize.hip", "swiglu.hip", "rmsnorm.hip", "rmsnorm_blocks.hip", "rmsnorm_bwd.hip", "qk_norm_rope.hip", "adamw.hip", "calibrate.hip"]
 # Sources that hold tile kernels (see check_accumulator_reads).
 CHECKED_SOURCES = set(TILE_SOURCES) | {"gemm.hip"}
+# Sources of kernels whose output may be one of their inputs (see check_in_place).
+IN_PLACE_SOURCES = {src for src in TILE_SOURCES if src.startswith("gemm_glu_bwd_")}
 # packed-fp32 VALU ops are disabled on purpose (they have produced silent wrong results on this
 # hardware pool); never add -ffast-math: the scale needs a correctly rounded division.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
@@ -171,6 +173,21 @@ def check_store_offsets(src: str, asm: str) -> None:
         raise RuntimeError("%s: buffer stores with a scalar offset:\n  %s" % (src, "\n  ".join(bad[:20])))
 
 
+def check_in_place(src: str, asm: str) -> None:
+    """A kernel that may write over one of its inputs must not promise the compiler otherwise.  The metadata calls a pointer write-only where it is declared apart from all others and only
+    written: in these sources a build error."""
+    bad = []
+    for kernel in re.split(r"\n  - ", asm[asm.find("amdhsa.kernels:"):]):
+        name = re.search(r"\.name:\s+(\S+)", kernel)
+        for access, offset in re.findall(r"\.actual_access:\s+(\w+)\n(?:\s+\.\w+:\s+\w+\n)*?\s+\.offset:\s+(\d+)", kernel):
+            if access != "read_only":
+                bad.append("%s: the pointer at %s" % (name.group(1) if name else "?", offset))
+    if "amdhsa.kernels:" not in asm:
+        bad.append("no metadata in the generated assembly")
+    if bad:
+        raise RuntimeError("%s: an output is declared apart from the inputs that it may be:\n  %s" % (src, "\n  ".join(bad[:20])))
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     work = tempfile.mkdtemp(prefix="llmq_build_")
@@ -248,6 +265,8 @@ def _build_in(work: str, hipcc: str, verbose: bool) -> str:
         check_scale_operands(src, asm)
         check_store_data(src, asm, STORE_WAIT_STATES)
         check_store_offsets(src, asm)
+        if src in IN_PLACE_SOURCES:
+            check_in_place(src, asm)
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", new_lib])
     binding_built = binding_built and _finish_binding(_run_binding(link_binding))
     # Both are there (or the module is not going to be): now they replace the old ones.  A module of another build must not stay

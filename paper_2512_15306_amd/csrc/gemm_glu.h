@@ -21,6 +21,10 @@ struct GluPlan {
     uint16_t *gu_out, *h_out;                   // forward: GU, backward: h; or NULL
 };
 
+// Backward, dGU may be GU: every element of GU is read, by the lane that stores its gradient, before that store, and the pointers are not declared apart, so that stores keep their place behind the loads.
+template <int DIR>
+using GluOut = std::conditional_t<DIR == kGluBackward, uint16_t*, uint16_t* __restrict__>;
+
 __device__ inline float glu_sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g)); }
 __device__ inline float glu_value(float g, float u) { return g * glu_sigmoid(g) * u; }
 // dG and dU, and h
@@ -290,6 +294,7 @@ struct GluTuning : Base {
     static constexpr int kGlu = DIR;
     static constexpr int kPairBlocks = PAIR_BLOCKS;
     typedef GluPlan Plan;
+    typedef GluOut<DIR> Out;
     template <int NI, int MI, int MJ, int EDGE>
     using Epilogue = std::conditional_t<DIR == kGluForward, GluForward<NI, MI, MJ, EDGE>, GluBackward<NI, MI, MJ, EDGE, STREAMED>>;
 };
@@ -351,7 +356,7 @@ static void launch_glu_tile(const GluOperands& p, bool loose, hipStream_t stream
 // last chunk brings along of the next row is cleared before it is multiplied.
 template <int FA, int FB, int DIR, int RB, int CB, int WAVES, int SLOTS, bool ALIGNED>
 __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8_t* __restrict__ A, const uint8_t* __restrict__ sA, const uint8_t* __restrict__ B, const uint8_t* __restrict__ sB,
-                                                                       uint16_t* __restrict__ C, const GluPlan plan, int M, int I, int T, unsigned* __restrict__ amax_bits) {
+                                                                       GluOut<DIR> C, const GluPlan plan, int M, int I, int T, unsigned* __restrict__ amax_bits) {
     static_assert(DIR == kGluBackward || CB == 2, "gates and ups");
     constexpr bool PAIRS = DIR == kGluForward;
     constexpr int kRows = 16 * (RB + CB), kSlot = kRows * BK, kLoads = kRows / 8, kOutOfRange = 0x7FFFFF00, kGroups = PAIRS ? 2 : 1, kOfGroup = CB / kGroups;

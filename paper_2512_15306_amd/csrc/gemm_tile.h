@@ -152,6 +152,8 @@ struct GemmTuning {
     static constexpr int kPairBlocks = 1;
     // What the launch knows of its tiles
     typedef SplitPlan Plan;
+    // The output: apart from everything the kernel reads by other pointers
+    typedef uint16_t* __restrict__ Out;
 };
 constexpr int kGluForward = 1, kGluBackward = 2;
 
@@ -403,7 +405,7 @@ __device__ inline v4u first_bytes(v4u v, int valid) {
 // (A guarded tile of six units with block scales would move accumulators out of their registers to keep to it; it has its CU to itself.)
 template <int FA, int FB, int NI, int NJ, bool ACCUM, class V = GemmTuning, bool TA = false, bool TB = false, int MODE = kWholeTiles, int EDGE = kNoEdge>
 __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 && V::kStages == 2 && EDGE != kEdgeUnaligned && FA != kFmtBf16 && !(V::kBlockScales && EDGE == kEdge && NI * NJ == 6)) ? 2 : 1) void gemm_tile_kernel(
-    const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, uint16_t* __restrict__ C,
+    const uint8_t* __restrict__ A, const uint8_t* __restrict__ B, typename V::Out C,
     int Cn, int T, const float* __restrict__ d_sA, const float* __restrict__ d_sB,
     unsigned* __restrict__ amax_bits, int tiles_r, int tiles_c, int touch_ahead, int band_rows, int next_stride,
     int ldA, int ldB, int ks_a, int ks_b, int share_a, int share_b, const typename V::Plan plan, int Rn, int accumulate) {

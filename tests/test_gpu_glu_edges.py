@@ -27,3 +27,17 @@ def test_nothing_is_written_behind_the_last_row(monkeypatch, few, M, I, T):
     glu.forward(M, I, T, 0, 3)
     glu.backward(M, I, T, 1, 4)
     glu.backward(M, I, T, 0, 5, want_h=False, in_place=True)
+
+
+@pytest.mark.parametrize("kernel", ["few", "one wave", "4x4", "3x4", "4x2", "2x4", "2x2"])
+@pytest.mark.parametrize("M,I,T", [(768, 512, 512), (450, 192, 1040), (520, 333, 388), (200, 101, 130), (300, 2049, 2052)])
+def test_the_gradient_may_be_written_over_what_was_kept(monkeypatch, kernel, M, I, T):
+    """In place: the bytes of the same call with a buffer of its own."""
+    print("glu in place", kernel, M, I, T, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", "1" if kernel in ("few", "one wave") else "0")
+    monkeypatch.setenv("LLMQ_GLU_FEW_ALONE", "1" if kernel == "one wave" else "0")
+    if "x" in kernel:
+        monkeypatch.setenv("LLMQ_GLU_TILE", kernel)
+    for h in (True, False):
+        want, got = (glu.backward(M, I, T, 1, 7, want_h=h, in_place=here) for here in (False, True))
+        assert torch.equal(want[5], got[5]) and torch.equal(want[6], got[6])
