@@ -80,10 +80,10 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Qua
         v4u wv;
         float rs[kPatchRows];
         if constexpr (GUARD) {
-            // (what does not exist counts as zero times zero)
-            wv = load8_upto(t.w + c0, c0, cols - c0);
+            // (what does not exist is zero times zero, also in a row whose statistic, or a column whose weight, is no number or infinite)
+            wv = load8_upto(t.w + c0, c0, r0 < t.rows ? cols - c0 : 0);
 #pragma unroll
-            for (int i = 0; i < kPatchRows; ++i) rs[i] = r0 + i < t.rows ? t.rstd[r0 + i] : 0.0f;
+            for (int i = 0; i < kPatchRows; ++i) rs[i] = r0 + i < t.rows && c0 < cols ? t.rstd[r0 + i] : 0.0f;
         } else {
             wv = *reinterpret_cast<const v4u*>(t.w + c0);
 #pragma unroll
@@ -95,6 +95,18 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Qua
         }
 #pragma unroll
         for (int i = 0; i < kPatchRows; ++i) in[i] = normalize8(in[i], rs[i], wv);
+        if constexpr (GUARD) {
+            // (in patches that the tensor ends in; the same answer for the whole launch)
+            if (cols % 8 != 0) {
+#pragma unroll
+                for (int i = 0; i < kPatchRows; ++i) in[i] = keep_upto(in[i], cols - c0 < 8 ? (int)(cols - c0) : 8);
+            }
+            if (t.rows % kPatchRows != 0) {
+#pragma unroll
+                for (int i = 0; i < kPatchRows; ++i)
+                    if (r0 + i >= t.rows) in[i] = v4u{0, 0, 0, 0};
+            }
+        }
         if (t.y) {
             uint16_t* dst = t.y + r0 * cols + c0;
             if constexpr (GUARD) {
