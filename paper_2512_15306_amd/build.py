@@ -188,6 +188,66 @@ def check_in_place(src: str, asm: str) -> None:
         raise RuntimeError("%s: an output is declared apart from the inputs that it may be:\n  %s" % (src, "\n  ".join(bad[:20])))
 
 
+def check_counted_waits(src: str, asm: str) -> int:
+    """The tile kernels wait for their direct-to-LDS loads by counting what they have requested since (a written-out `s_waitcnt vmcnt(N)`), so every other load must be there as often, and where, the
+    kernel's own arithmetic has it: where the compiler makes one load of two, a slab is read before it has landed.  Of the N newest requests in front of such a wait, on any path, no more may be loads to
+    LDS than the stages that stay in flight have (of two stages one, of four three in front of the loop, and one less in it); others are a build error.  Returns the number of kernels it looked at."""
+    bad = []
+    checked = 0
+    for m in re.finditer(r"^(_ZN4llmq16gemm_tile_kernel\w*):[^\n]*\n(.*?)^\.Lfunc_end", asm, re.S | re.M):
+        stages = 4 if "Deep" in m.group(1) else 2
+        code, written_out = [], False                 # (kind, value): of what counts, and of the control flow
+        for l in m.group(2).splitlines():
+            if "#ASMSTART" in l or "#ASMEND" in l:
+                written_out = "#ASMSTART" in l
+                continue
+            l = l.split(";")[0].strip()
+            wait = re.match(r"s_waitcnt vmcnt\((\d+)\)$", l)
+            if wait and written_out:
+                code.append(("wait", int(wait.group(1))))
+            elif re.match(r"(buffer|global|flat|scratch)_", l):
+                code.append(("lds" if re.search(r" lds\b", l) else "vm", 0))
+            elif re.match(r"\.LBB\w+:", l):
+                code.append(("label", l[:-1]))
+            elif re.match(r"s_c?branch", l):
+                code.append(("jump" if l.startswith("s_branch") else "maybe", l.split()[-1]))
+            elif l.startswith("s_endpgm"):
+                code.append(("end", 0))
+        waits = [i for i, (kind, n) in enumerate(code) if kind == "wait" and n > 0]
+        slab = sum(kind == "lds" for kind, _ in code[:waits[0]]) // stages if waits else 0
+        if not slab:
+            continue                                  # operands through registers
+        checked += 1
+        jumps = {}
+        for i, (kind, target) in enumerate(code):
+            if kind in ("jump", "maybe"):
+                jumps.setdefault(target, []).append(i)
+        for i in waits:
+            allowed = (stages - (1 if i == waits[0] else 2)) * slab
+            paths, seen = [(i - 1, code[i][1], 0)], set()
+            while paths:
+                k, left, found = paths.pop()
+                if (k, left, found) in seen or k < 0:
+                    continue
+                seen.add((k, left, found))
+                kind, value = code[k]
+                if kind in ("jump", "end"):
+                    continue                          # (what falls through comes from elsewhere)
+                if kind in ("vm", "lds"):
+                    left, found = left - 1, found + (kind == "lds")
+                    if found > allowed:
+                        bad.append("%s: vmcnt(%d)" % (m.group(1), code[i][1]))
+                        break
+                    if left == 0:
+                        continue
+                if kind == "label":
+                    paths += [(j - 1, left, found) for j in jumps.get(value, ())]
+                paths.append((k - 1, left, found))
+    if bad:
+        raise RuntimeError("%s: a counted wait leaves loads to LDS on their way that are read behind it:\n  %s" % (src, "\n  ".join(bad[:20])))
+    return checked
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     work = tempfile.mkdtemp(prefix="llmq_build_")
@@ -265,6 +325,7 @@ def _build_in(work: str, hipcc: str, verbose: bool) -> str:
         check_scale_operands(src, asm)
         check_store_data(src, asm, STORE_WAIT_STATES)
         check_store_offsets(src, asm)
+        check_counted_waits(src, asm)
         if src in IN_PLACE_SOURCES:
             check_in_place(src, asm)
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", new_lib])

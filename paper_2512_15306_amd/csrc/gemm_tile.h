@@ -754,6 +754,8 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
             const int row = 16 * (gate_block + PB * (p % (WB / 2))) + (p >= WB / 2 ? Cn : 0) + (lane & 15);
             pair_voff[p] = (row & ~127) + 8 * (row & 15) + ((row >> 4) & 4);
             pair_shift[p] = 8 * ((row >> 4) & 3);
+            // (a wave's gate blocks lie in one word: seen to be the same, their loads would be one, and the waits, which count loads, a load short)
+            if constexpr (PB == 1) asm volatile("" : "+v"(pair_voff[p]));
         }
     }
     // offset of a block's codes in a K step (a tile may reach over the last group of 128 rows: what is read there, codes of another step or zeros, goes to rows that do not exist)
@@ -931,6 +933,7 @@ __global__ __launch_bounds__(128 * V::kWavesC, V::kWavesC == 4 || (NI * NJ <= 6 
     }
     }
     if constexpr (kTouch) {                       // keep "two touch loads are the newest" true from the start
+        if constexpr (V::kGlu != 0) __builtin_amdgcn_sched_barrier(0);
         const bool on = touch_ahead > 0 && 2 < nk;
         touchA[1] = __builtin_amdgcn_raw_buffer_load_b32(rsA, touch_voffA, on ? (kb + 2) * ksA : kOutOfRange, 0);
         touchB[1] = __builtin_amdgcn_raw_buffer_load_b32(rsB, touch_voffB, on ? (kb + 2) * ksB : kOutOfRange, 0);

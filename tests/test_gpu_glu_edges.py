@@ -41,3 +41,38 @@ def test_the_gradient_may_be_written_over_what_was_kept(monkeypatch, kernel, M, 
     for h in (True, False):
         want, got = (glu.backward(M, I, T, 1, 7, want_h=h, in_place=here) for here in (False, True))
         assert torch.equal(want[5], got[5]) and torch.equal(want[6], got[6])
+
+
+@pytest.mark.parametrize("M,I,T", [(256, 256, 2048), (384, 192, 4096), (300, 320, 2048), (300, 320, 2052), (200, 96, 2060), (257, 160, 2064), (130, 100, 2064), (250, 104, 2052), (129, 333, 2048), (140, 37, 2076), (300, 64, 1924), (140, 72, 3972)])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_four_stages_and_four_waves(monkeypatch, M, I, T, fmt):
+    """Contractions of more than 15 K steps in tiles of 128 x 128 that have their CU to themselves: against binary64, and the bytes of the form with two stages."""
+    print("glu deep", M, I, T, fmt, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", "0")
+    monkeypatch.setenv("LLMQ_GLU_TILE", "2x2")
+    got = []
+    for deep in ("1", "0"):
+        monkeypatch.setenv("LLMQ_GEMM_DEEP", deep)
+        f, b = glu.forward(M, I, T, fmt, 3), glu.backward(M, I, T, fmt, 4)
+        got.append([f[4], f[5], f[6], b[5], b[6]])
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
+@pytest.mark.parametrize("tile", glu.TILES)
+@pytest.mark.parametrize("M,I,T", [(450, 333, 388), (520, 2721, 1000), (300, 129, 132), (257, 260, 20), (768, 1001, 256), (64, 68, 516)])
+def test_widths_of_no_whole_pieces_in_every_tile(monkeypatch, tile, M, I, T):
+    """Backward tiles take any width: pieces at any address inside the matrix, element by element in its last columns."""
+    print("glu tile", tile, M, I, T, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", "0")
+    monkeypatch.setenv("LLMQ_GLU_TILE", tile)
+    for fmt, want_h, in_place in ((0, True, False), (1, False, True), (1, True, True)):
+        glu.backward(M, I, T, fmt, 5, want_h, in_place)
+
+
+@pytest.mark.parametrize("M,I,T", glu.RAGGED + glu.WHOLE)
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_tiles_of_problems_that_the_other_kernel_takes(monkeypatch, M, I, T, fmt):
+    print("glu tiles", M, I, T, fmt, flush=True)
+    monkeypatch.setenv("LLMQ_GLU_FEW", "0")
+    glu.forward(M, I, T, fmt, M + I + T, keep=fmt == 0)
+    glu.backward(M, I, T, fmt, M + I + T, want_h=fmt == 0, in_place=fmt == 1)
