@@ -190,12 +190,14 @@ def check_in_place(src: str, asm: str) -> None:
 
 def check_counted_waits(src: str, asm: str) -> int:
     """The tile kernels wait for their direct-to-LDS loads by counting what they have requested since (a written-out `s_waitcnt vmcnt(N)`), so every other load must be there as often, and where, the
-    kernel's own arithmetic has it: where the compiler makes one load of two, a slab is read before it has landed.  Of the N newest requests in front of such a wait, on any path, no more may be loads to
-    LDS than the stages that stay in flight have (of two stages one, of four three in front of the loop, and one less in it); others are a build error.  Returns the number of kernels it looked at."""
+    kernel's own arithmetic has it: where the compiler makes one load of two, or drops some, a slab is read before it has landed.  Of the N newest requests in front of such a wait, on any path, no more
+    may be loads to LDS than the stages that stay in flight have (gemm_tile_kernel: of two stages one, of four three in front of the loop, and one less in it; gemm_mini_kernel: as many of N as of the
+    wait that leaves all stages but one in flight); others are a build error.  Returns the number of kernels it looked at."""
     bad = []
     checked = 0
-    for m in re.finditer(r"^(_ZN4llmq16gemm_tile_kernel\w*):[^\n]*\n(.*?)^\.Lfunc_end", asm, re.S | re.M):
-        stages = 4 if "Deep" in m.group(1) else 2
+    for m in re.finditer(r"^(_ZN4llmq16gemm_(?:tile|mini)_kernel\w*):[^\n]*\n(.*?)^\.Lfunc_end", asm, re.S | re.M):
+        mini = "gemm_mini_kernel" in m.group(1)
+        stages = 4 if ("ELi32E" if mini else "Deep") in m.group(1) else 2
         code, written_out = [], False                 # (kind, value): of what counts, and of the control flow
         for l in m.group(2).splitlines():
             if "#ASMSTART" in l or "#ASMEND" in l:
@@ -223,7 +225,7 @@ def check_counted_waits(src: str, asm: str) -> int:
             if kind in ("jump", "maybe"):
                 jumps.setdefault(target, []).append(i)
         for i in waits:
-            allowed = (stages - (1 if i == waits[0] else 2)) * slab
+            allowed = code[i][1] * (stages - 1) * slab // max(code[w][1] for w in waits) if mini else (stages - (1 if i == waits[0] else 2)) * slab
             paths, seen = [(i - 1, code[i][1], 0)], set()
             while paths:
                 k, left, found = paths.pop()

@@ -186,8 +186,9 @@ __global__ __launch_bounds__(kGemmThreads, 1) void gemm_mini_kernel(
     for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    auto stage_step = [&](uint8_t* bufA, uint8_t* bufB, int stage, StageScales& sc) __attribute__((always_inline)) {
-        wait_vmcnt<(ST - 1) * (kLoads + kScaleLoads)>();                                 // this stage has landed, the later ones are on their way
+    // behind: stages requested after this one.  The last stages (fewer than ST - 1 behind, or the first of them) request none: their codes would be no use to anybody and dropped by the compiler, but counted here.
+    auto stage_step = [&](uint8_t* bufA, uint8_t* bufB, int stage, StageScales& sc, auto behind, auto more) __attribute__((always_inline)) {
+        wait_vmcnt<decltype(behind)::value * (kLoads + kScaleLoads)>();                  // this stage has landed, the later ones are on their way
         lds_barrier_in_flight();
         v8i a[kMiniSteps][NB], b[kMiniSteps][NB];
 #pragma unroll
@@ -214,19 +215,24 @@ __global__ __launch_bounds__(kGemmThreads, 1) void gemm_mini_kernel(
                         acc[i][k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j][k], a[j][i], acc[i][k], FB, FA, 0, 0, 0, 0);
                     }
                 }
-        lds_barrier_in_flight();                                         // everybody has read the stage: it may be overwritten
-        issue_stage(bufA, bufB, stage + ST, sc);                             // (beyond the last stage: nothing is fetched, zeros are written)
+        if constexpr (decltype(more)::value) {
+            lds_barrier_in_flight();                                     // everybody has read the stage: it may be overwritten
+            issue_stage(bufA, bufB, stage + ST, sc);                         // (beyond the last stage: nothing is fetched, zeros are written)
+        }
     };
+    typedef IntTag<ST - 1> All;
+    typedef BoolTag<true> More;
+    typedef BoolTag<false> Last;
     auto half = [&](uint8_t* buf) { return SIDE == 64 ? buf : buf + kOperand; };
     if constexpr (SIDE == 64) {
         issue_stage(s_0, s_1, 0, scales[0]);
         issue_stage(s_2, s_3, 1, scales[1]);
         int st = 0;
         for (; st + 1 < ns; st += 2) {                                   // (the same order of loads on every way round: the compiler counts them)
-            stage_step(s_0, s_1, st, scales[0]);
-            stage_step(s_2, s_3, st + 1, scales[1]);
+            stage_step(s_0, s_1, st, scales[0], All{}, More{});
+            stage_step(s_2, s_3, st + 1, scales[1], All{}, More{});
         }
-        if (st < ns) stage_step(s_0, s_1, st, scales[0]);
+        if (st < ns) stage_step(s_0, s_1, st, scales[0], All{}, Last{});
     } else {
         issue_stage(s_0, half(s_0), 0, scales[0]);
         issue_stage(s_1, half(s_1), 1, scales[1]);
@@ -234,14 +240,14 @@ __global__ __launch_bounds__(kGemmThreads, 1) void gemm_mini_kernel(
         issue_stage(s_3, half(s_3), 3, scales[ST == 4 ? 3 : 0]);
         int st = 0;
         for (; st + 3 < ns; st += 4) {
-            stage_step(s_0, half(s_0), st, scales[0]);
-            stage_step(s_1, half(s_1), st + 1, scales[1]);
-            stage_step(s_2, half(s_2), st + 2, scales[ST == 4 ? 2 : 0]);
-            stage_step(s_3, half(s_3), st + 3, scales[ST == 4 ? 3 : 0]);
+            stage_step(s_0, half(s_0), st, scales[0], All{}, More{});
+            stage_step(s_1, half(s_1), st + 1, scales[1], All{}, More{});
+            stage_step(s_2, half(s_2), st + 2, scales[ST == 4 ? 2 : 0], All{}, More{});
+            stage_step(s_3, half(s_3), st + 3, scales[ST == 4 ? 3 : 0], All{}, More{});
         }
-        if (st < ns) stage_step(s_0, half(s_0), st, scales[0]);
-        if (st + 1 < ns) stage_step(s_1, half(s_1), st + 1, scales[1]);
-        if (st + 2 < ns) stage_step(s_2, half(s_2), st + 2, scales[ST == 4 ? 2 : 0]);
+        if (st < ns) stage_step(s_0, half(s_0), st, scales[0], IntTag<3>{}, Last{});
+        if (st + 1 < ns) stage_step(s_1, half(s_1), st + 1, scales[1], IntTag<2>{}, Last{});
+        if (st + 2 < ns) stage_step(s_2, half(s_2), st + 2, scales[ST == 4 ? 2 : 0], IntTag<1>{}, Last{});
     }
     wait_vmcnt<0>();                                                     // nothing lands in LDS behind the workgroup's end
     const float inv_a = 1.0f / scale_a, inv_b = 1.0f / scale_b, inv_ab = inv_a * inv_b;

@@ -56,3 +56,19 @@ def test_a_path_with_a_load_less_fails_the_build():
 
 def test_kernels_without_loads_to_lds_are_none_of_its_business():
     assert build.check_counted_waits("good.hip", kernel(TWO, 2, 2, 2).replace(LDS, SCALE)) == 0
+
+
+MINI = "_ZN4llmq16gemm_mini_kernelILi0ELi0ELi32ELb1EEEvPKhS2_PtiiiPKfS5_iPjiiiiii"
+
+
+def mini(tail):
+    """Four stages of two slab loads and three others, which the loop's and the last stages' waits count together."""
+    stage = SCALE * 3 + LDS * 2
+    return ("%s:                                ; @x\n; %%bb.0:\n" % MINI + stage * 4 + "\ts_cbranch_scc1 .LBB0_2\n.LBB0_1:\n" + (wait(15) + stage) * 4 + "\ts_cbranch_scc1 .LBB0_1\n.LBB0_2:\n" + tail + wait(0)
+            + "\ts_endpgm\n.Lfunc_end0:\n")
+
+
+def test_last_stages_whose_codes_nobody_needs():
+    assert build.check_counted_waits("good.hip", mini(wait(15) + wait(10) + wait(5))) == 1
+    with pytest.raises(RuntimeError, match="counted wait"):
+        build.check_counted_waits("bad.hip", mini(wait(15) + LDS * 2 + wait(15)))
