@@ -188,12 +188,13 @@ __device__ inline void glu_gradient8(const v4f (&dh)[2], const v4u& g, const v4u
 }
 
 // Epilogue of the backward tile: dh through LDS in binary32, 32 rows at a time, so that a lane has eight consecutive columns of a row, as GU is loaded and dGU stored.  GU is requested in parts of four such
-// pieces, AHEAD parts in advance in whole tiles (8192 x 18944 x 3584 with h: 648 us without, 631 with two, 621 with three, 622 with four), for 32 rows at a time in guarded ones.
+// pieces, ahead parts in advance in whole tiles (8192 x 18944 x 3584 with h: 648 us without, 631 with two, 621 with three, 622 with four), for 32 rows at a time in guarded ones, and in 128 x 128, where that
+// is half of all, if h is not wanted (both halves in advance / one at a time: 512 x 8192 x 1024 14.4 / 13.6, x 2048 17.5 / 17.0, 1024 x 4096 x 4096 24.5 / 23.7; with h 512 x 8192 x 2048 18.07 / 18.2).
 // STREAMED: GU past what the caches hold.
 template <int NI, int MI, int MJ, int EDGE, bool STREAMED>
 struct GluBackward {
     static constexpr int kSlots = 2 * MJ, kPitch = 32 * kSlots, kPieces = 32 * kSlots / kWave, kAtOnce = kPieces < 4 ? kPieces : 4, kParts = kPieces / kAtOnce, kAll = NI * kParts;
-    static constexpr int AHEAD = EDGE != kNoEdge ? 0 : 3 < kAll ? 3 : kAll, kKept = AHEAD ? AHEAD + 1 : kParts;
+    static constexpr int ahead(bool with_h) { return EDGE != kNoEdge || (kAll <= 2 && !with_h) ? 0 : 3 < kAll ? 3 : kAll; }
     static_assert(kPieces >= 1 && kWave % kSlots == 0 && kPieces % kAtOnce == 0, "every lane moves whole pieces");
     struct Kept { v4u g[kAtOnce], u[kAtOnce]; };
     typedef GluRows<EDGE, kSlots> Rows;
@@ -213,6 +214,7 @@ struct GluBackward {
         unsigned mag = 0, ignored = 0;
         float maxabs = 0.0f;
         auto body = [&](auto with_h) __attribute__((always_inline)) {
+            constexpr int AHEAD = ahead(decltype(with_h)::value), kKept = AHEAD ? AHEAD + 1 : kParts;
             auto staged = [&](int k, v4f (&dh)[2]) __attribute__((always_inline)) {
                 const int p = lane + k * kWave, r = p / kSlots, sl = p % kSlots;
                 const uint8_t* src = stage + r * kPitch + (((sl + r) % kSlots) << 4);
