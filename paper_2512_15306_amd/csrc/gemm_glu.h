@@ -557,7 +557,7 @@ __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8
 
 // Workgroups of four waves and four slots fill a CU and are a chain of a quarter of the steps; workgroups of one wave and three slots lie eight to a CU and have nothing to wait for one another: better where all
 // of them have work and no wave's chain is the whole time.  Four waves / one, us, I x T: 16 rows 18944 x 3584 35.0 / 26.7, 11008 x 2048 14.0 / 9.6, 5504 x 2048 9.3 / 7.7, 8192 x 512 5.2 / 3.7; the other way
-// 2736 x 2048 4.92 / 7.43, 4096 x 2048 6.1 / 7.6, 5504 x 8192 22.8 / 29.4; 32 rows 18944 x 3584 40.7 / 31.2, 5504 x 3584 13.3 / 13.9.  Through registers (two slots): 16 rows 18944 x 3581 49.4 / 40.8,
+// 2736 x 2048 4.92 / 7.43, 4096 x 2048 6.1 / 7.6, 5504 x 8192 22.8 / 29.4; 32 rows 18944 x 3584 40.7 / 31.2, 5504 x 3584 13.3 / 13.9.  Through registers (four waves with four slots, one with two): 16 rows 18944 x 3581 49.4 / 40.8,
 // 5504 x 2047 12.2 / 12.2, 24 rows 11007 x 1023 15.1 / 10.1, 450 rows 438 x 223 backward 7.9 / 5.9.
 template <int FA, int FB, int DIR, int RB, int CB>
 static void launch_glu_few(const GluOperands& p, hipStream_t stream, int num_cus) {
