@@ -250,6 +250,26 @@ def check_counted_waits(src: str, asm: str) -> int:
     return checked
 
 
+def check_few_rows_waits(src: str, asm: str) -> int:
+    """The kernels for few rows count their requests too.  Each wave waits for its own loads only, and a step's loads stand in two branches of which one is taken, so check_counted_waits has no use for
+    them; but as many steps stay in flight behind the last ones as were requested behind those, and no more: every multiple of a step's requests, up to all slots but one, is a written-out wait, and no other.
+    Returns the number of kernels it looked at."""
+    bad = []
+    checked = 0
+    for m in re.finditer(r"^(_ZN4llmq\d+gemm_(blocks|glu)_few_kernelI((?:L\w\d+E)+)E\w*):[^\n]*\n(.*?)^\.Lfunc_end", asm, re.S | re.M):
+        numbers = [int(n) for n in re.findall(r"L\w(\d+)E", m.group(3))]
+        slots = numbers[6] if m.group(2) == "glu" else 4
+        if not re.search(r"^\s*buffer_load_\w+ .* lds\b", m.group(4), re.M):
+            continue                                  # operands through registers
+        checked += 1
+        waits = sorted({int(n) for n in re.findall(r"#ASMSTART\n\s*s_waitcnt vmcnt\((\d+)\)\n", m.group(4))} - {0})
+        if not waits or waits != [waits[0] * k for k in range(1, slots)]:
+            bad.append("%s: vmcnt %s" % (m.group(1), waits))
+    if bad:
+        raise RuntimeError("%s: waits that do not count the steps in flight:\n  %s" % (src, "\n  ".join(bad[:20])))
+    return checked
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     work = tempfile.mkdtemp(prefix="llmq_build_")
@@ -328,6 +348,7 @@ def _build_in(work: str, hipcc: str, verbose: bool) -> str:
         check_store_data(src, asm, STORE_WAIT_STATES)
         check_store_offsets(src, asm)
         check_counted_waits(src, asm)
+        check_few_rows_waits(src, asm)
         if src in IN_PLACE_SOURCES:
             check_in_place(src, asm)
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", new_lib])

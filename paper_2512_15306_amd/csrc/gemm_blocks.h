@@ -136,10 +136,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
 #pragma unroll
         for (int j = 0; j < CB; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     // LDS runs a wave's accesses in order, and the direct loads that follow are requested behind the wait for the reads
-    auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
+    // behind: steps requested after this one.  The last steps request none, whose codes would be no use to anybody and dropped by the compiler, but counted here.
+    auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held, auto behind, auto more) __attribute__((always_inline)) {
         uint8_t* const slab = slot + wave * kSlot;
         if constexpr (ALIGNED) {
-            wait_vmcnt<(kFewSlots - 1) * (kLoads + RB + CB)>();
+            wait_vmcnt<decltype(behind)::value * (kLoads + RB + CB)>();
         } else {
             static_for<kLoads>([&](auto piece) { *reinterpret_cast<v4u*>(slab + decltype(piece)::value * 8 * BK + lane * 16) = held.c[decltype(piece)::value]; });
         }
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
 #pragma unroll
             for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, 0, now.b[j], 0, now.a[i]);
         __builtin_amdgcn_sched_barrier(0);
-        request(slot, n + kFewSlots, e, held);
+        if constexpr (decltype(more)::value) request(slot, n + kFewSlots, e, held);
     };
     request(s_0, 0, codes[0], chunks[0]);
     request(s_1, 1, codes[1], chunks[1]);
@@ -169,14 +170,14 @@ __global__ __launch_bounds__(kFewWaves * kWave) void gemm_blocks_few_kernel(cons
     request(s_3, 3, codes[3], chunks[3]);
     int n = 0;
     for (; n + 3 < mine; n += 4) {
-        multiply(s_0, n, codes[0], chunks[0]);
-        multiply(s_1, n + 1, codes[1], chunks[1]);
-        multiply(s_2, n + 2, codes[2], chunks[2]);
-        multiply(s_3, n + 3, codes[3], chunks[3]);
+        multiply(s_0, n, codes[0], chunks[0], IntTag<3>{}, BoolTag<true>{});
+        multiply(s_1, n + 1, codes[1], chunks[1], IntTag<3>{}, BoolTag<true>{});
+        multiply(s_2, n + 2, codes[2], chunks[2], IntTag<3>{}, BoolTag<true>{});
+        multiply(s_3, n + 3, codes[3], chunks[3], IntTag<3>{}, BoolTag<true>{});
     }
-    if (n < mine) multiply(s_0, n, codes[0], chunks[0]);
-    if (n + 1 < mine) multiply(s_1, n + 1, codes[1], chunks[1]);
-    if (n + 2 < mine) multiply(s_2, n + 2, codes[2], chunks[2]);
+    if (n < mine) multiply(s_0, n, codes[0], chunks[0], IntTag<3>{}, BoolTag<false>{});
+    if (n + 1 < mine) multiply(s_1, n + 1, codes[1], chunks[1], IntTag<2>{}, BoolTag<false>{});
+    if (n + 2 < mine) multiply(s_2, n + 2, codes[2], chunks[2], IntTag<1>{}, BoolTag<false>{});
     wait_vmcnt<0>();                             // nothing lands in LDS any more
     __syncthreads();
     v4f* const s_sum = reinterpret_cast<v4f*>(s_0);                          // [wave][block][lane]

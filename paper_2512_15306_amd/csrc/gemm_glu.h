@@ -419,12 +419,13 @@ __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8
 #pragma unroll
         for (int j = 0; j < CB; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     // LDS runs a wave's accesses in order, and the direct loads that follow are requested behind the wait for the reads
-    auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held) __attribute__((always_inline)) {
+    // behind: steps requested after this one.  The last steps request none, whose codes would be no use to anybody and dropped by the compiler, but counted here.
+    auto multiply = [&](uint8_t* slot, int n, Codes& e, Chunks& held, auto behind, auto more) __attribute__((always_inline)) {
         uint8_t* const slab = slot + wave * kSlot;
         // the last K step: a row's chunk that ends in it, or (through registers) lies behind it
         const int left = T - (wave + n * WAVES) * BK;
         if constexpr (ALIGNED) {
-            wait_vmcnt<(SLOTS - 1) * (kLoads + RB + CB)>();
+            wait_vmcnt<decltype(behind)::value * (kLoads + RB + CB)>();
             if (left < BK && T % 16 != 0) {
                 static_for<kLoads>([&](auto piece) {
                     const int valid = left - (((lane & 7) ^ row_swizzle((8 * decltype(piece)::value + ld_row) & 15)) << 4);
@@ -467,15 +468,15 @@ __global__ __launch_bounds__(WAVES * kWave) void gemm_glu_few_kernel(const uint8
 #pragma unroll
             for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, 0, now.b[j], 0, now.a[i]);
         __builtin_amdgcn_sched_barrier(0);
-        request(slot, n + SLOTS, e, held);
+        if constexpr (decltype(more)::value) request(slot, n + SLOTS, e, held);
     };
     auto slot_of = [&](auto k) -> uint8_t* { constexpr int K = decltype(k)::value; return K == 0 ? s_0 : K == 1 ? s_1 : K == 2 ? s_2 : s_3; };
     static_for<SLOTS>([&](auto k) { request(slot_of(k), decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value]); });
     int n = 0;
     for (; n + SLOTS <= mine; n += SLOTS)
-        static_for<SLOTS>([&](auto k) { multiply(slot_of(k), n + decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value]); });
+        static_for<SLOTS>([&](auto k) { multiply(slot_of(k), n + decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value], IntTag<SLOTS - 1>{}, BoolTag<true>{}); });
     static_for<SLOTS - 1>([&](auto k) {
-        if (n + decltype(k)::value < mine) multiply(slot_of(k), n + decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value]);
+        if (n + decltype(k)::value < mine) multiply(slot_of(k), n + decltype(k)::value, codes[decltype(k)::value], chunks[decltype(k)::value], IntTag<SLOTS - 1 - decltype(k)::value>{}, BoolTag<false>{});
     });
     wait_vmcnt<0>();                             // nothing lands in LDS any more
     __syncthreads();

@@ -72,3 +72,18 @@ def test_last_stages_whose_codes_nobody_needs():
     assert build.check_counted_waits("good.hip", mini(wait(15) + wait(10) + wait(5))) == 1
     with pytest.raises(RuntimeError, match="counted wait"):
         build.check_counted_waits("bad.hip", mini(wait(15) + LDS * 2 + wait(15)))
+
+
+BLOCKS, GLU = "_ZN4llmq22gemm_blocks_few_kernelILi0ELi0ELi1ELi2ELb1EEEvPKhS2_S2_S2_PtiiiiPj", "_ZN4llmq19gemm_glu_few_kernelILi0ELi0ELi1ELi1ELi2ELi1ELi3ELb1EEEvPKhS2_S2_S2_PtNS_7GluPlanEiiiPj"
+
+
+def few(name, *counts):
+    return "%s:                                ; @x\n; %%bb.0:\n" % name + "".join(SCALE * 3 + LDS * 6 + wait(n) for n in counts) + wait(0) + "\ts_endpgm\n.Lfunc_end0:\n"
+
+
+@pytest.mark.parametrize("name,good,bad", [(BLOCKS, (27, 27, 27, 27, 27, 18, 9), (27, 27, 27, 27, 27, 27, 27)), (BLOCKS, (27, 18, 9), (27, 18)), (GLU, (18, 18, 18, 18, 9), (18, 18, 18, 18, 18)), (GLU, (9, 18), (9, 18, 15))])
+def test_last_steps_of_the_kernels_for_few_rows(name, good, bad):
+    assert build.check_few_rows_waits("good.hip", few(name, *good)) == 1
+    with pytest.raises(RuntimeError, match="steps in flight"):
+        build.check_few_rows_waits("bad.hip", few(name, *bad))
+    assert build.check_few_rows_waits("good.hip", few(name, *bad).replace(LDS, SCALE)) == 0
