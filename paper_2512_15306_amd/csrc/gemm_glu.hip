@@ -9,9 +9,9 @@ namespace llmq {
 // the shape.
 //
 // The kernel for few rows reads its operands straight from memory and divides the contraction between waves, so it has no tile to fill and ends one short wait after it began.  It
-// takes what is bounded by reading the weights, and problems of up to four of its workgroups a CU.  Tiles / few, us, M x I x T: forward 16 x 18944 x 3584 45.0 / 26.6, 128 x 512 x 1024 7.6 / 4.05,
+// takes what is bounded by reading the weights, and problems of up to four of its workgroups a CU.  Tiles / few, us, M x I x T: forward 16 x 18944 x 3584 45.0 / 26.6, 128 x 512 x 1024 7.6 / 3.9,
 // 300 x 800 x 400 6.2 / 4.7, 256 x 1024 x 3584 16.8 / 15.6, 2048 x 256 x 512 6.05 / 5.2, 128 x 4096 x 2048 11.7 / 11.2, 96 x 5024 x 1024 8.6 / 8.7, 64 x 3000 x 2001 20.3 / 13.9; backward 128 x 512 x 1024
-// 8.8 / 3.7, 1000 x 512 x 1024 9.6 / 7.9, 64 x 4096 x 3584 17.8 / 7.3, 248 x 1839 x 167 16.3 / 9.25; beyond the rule, forward: 64 x 18944 x 3584 45.3 / 49.4, 65 x 6675 x 868 9.5 / 11.5, 40 x 12000 x 2001 19.3 / 24.1.
+// 8.8 / 3.7, 1000 x 512 x 1024 9.6 / 7.9, 64 x 4096 x 3584 17.8 / 7.1, 248 x 1839 x 167 16.3 / 9.25; beyond the rule, forward: 64 x 18944 x 3584 45.3 / 49.4, 65 x 6675 x 868 9.5 / 11.5, 40 x 12000 x 2001 19.3 / 24.1.
 template <int DIR>
 static GluChoice choose_glu(int64_t M, int64_t I, int64_t T, int num_cus) {
     GluChoice choice{false, {0, 0, kNoEdge}, DIR == kGluForward && I % 32 != 0};
